@@ -408,6 +408,65 @@ ATTT_API attt_status attt_kl_drift(const attt_bf16 *d_hp, const attt_bf16 *d_hq,
                                    void *d_ws, size_t ws_bytes, attt_stream stream);
 
 /* ------------------------------------------------------------------------ */
+/* Log probabilities through the frozen LM head: of given tokens, with the  */
+/* entropy and the most probable alternatives of every row, and the         */
+/* gradient of the hidden states that they are a function of (a policy-     */
+/* gradient update of the adapter on the agent's own text).                 */
+/* ------------------------------------------------------------------------ */
+
+/* Alternatives per row, at most. */
+#define ATTT_LOGPROB_MAX_TOP 20
+
+/* Workspace bytes of the two calls below.  0 for sizes that they refuse. */
+ATTT_API size_t attt_logprob_workspace_bytes(int64_t L, int64_t d, int64_t V, int topk);
+ATTT_API size_t attt_logprob_grad_workspace_bytes(int64_t L, int64_t d, int64_t V);
+
+/*
+ * With h = d_h (bf16, row j at d_h + j h_ld, d values), W = d_W (bf16 [V, d]),
+ * z_j = h_j W^T and p_j = softmax(z_j inv_temp) (inv_temp = 1 / temperature):
+ *   d_lse[j]     = log sum_v exp(z_jv inv_temp)                       (fp32 [L])
+ *   d_logp[j]    = z_{j,t_j} inv_temp - lse_j for the given token t_j = d_tgt[j]
+ *                  in [0, V); 0 for t_j = -1 (a row without one)      (fp32 [L])
+ *   d_entropy[j] = -sum_v p_jv log p_jv                               (fp32 [L])
+ *   d_top_id[j, i], d_top_logp[j, i], i < topk: the topk largest logits of the
+ *     row in descending order, the lower id first among equal ones, and their
+ *     log probabilities (int32 and fp32 [L, topk]).  Logits that are NaN or -inf
+ *     are never alternatives; places left over hold id -1 and, where the row has
+ *     a finite lse, -inf.
+ * Outputs may be NULL: d_logp together with d_tgt, d_top_logp and d_top_id
+ * together with topk = 0; at least one is wanted.  bf16 products, fp32 sums; a
+ * row with a NaN or +inf logit, or without a finite one, has lse, logp (of a
+ * given token) and entropy NaN or -inf as the formulas have.  Requirements: L >= 1,
+ * V >= 1, d >= 8 and d % 8 == 0, h_ld >= d and a multiple of 8, d_h and d_W
+ * 16-byte aligned, 0 < inv_temp <= 10,000, 0 <= topk <= ATTT_LOGPROB_MAX_TOP and
+ * <= V, d_ws at least attt_logprob_workspace_bytes(L, d, V, topk) bytes and
+ * 256-byte aligned.  Another token sets ATTT_ERR_TOKEN_RANGE in the device
+ * status word and makes its logp NaN.
+ */
+ATTT_API attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 *d_W,
+                                          const int32_t *d_tgt, int64_t L, int64_t d, int64_t V, float inv_temp,
+                                          int topk, float *d_logp, float *d_entropy, float *d_lse,
+                                          float *d_top_logp, int32_t *d_top_id, void *d_ws, size_t ws_bytes,
+                                          attt_stream stream);
+
+/*
+ * The gradient of sum_j glogp_j logp_j + gent_j entropy_j with respect to h, from
+ * the forward call's d_lse and d_entropy (same h, W, tgt and inv_temp):
+ *   dz_jv = inv_temp (a_j [v = t_j] - p_jv (a_j + gent_j (log p_jv + entropy_j)))
+ *   d_dh[j, :] = sum_v dz_jv W_v                                   (bf16 [L, d])
+ * with a_j = glogp_j, or 0 where t_j = -1.  d_gent (and then d_entropy) may be
+ * NULL: no entropy term.  dz is rounded to bf16 once; products are bf16, sums
+ * fp32.  No gradient for W (it is frozen).  Requirements as above, d_dh 16-byte
+ * aligned, d_ws at least attt_logprob_grad_workspace_bytes(L, d, V) bytes.
+ * Another token sets ATTT_ERR_TOKEN_RANGE and makes its row NaN.
+ */
+ATTT_API attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 *d_W,
+                                             const int32_t *d_tgt, const float *d_lse, const float *d_entropy,
+                                             const float *d_glogp, const float *d_gent, int64_t L, int64_t d,
+                                             int64_t V, float inv_temp, attt_bf16 *d_dh, void *d_ws,
+                                             size_t ws_bytes, attt_stream stream);
+
+/* ------------------------------------------------------------------------ */
 /* Update-text repetition (Eq. 6), novelty (Eq. 7) and the sequence-level   */
 /* filter of Sec. 4 (skip an update whose novelty is below tau; Appendix C: */
 /* tau = 0.5), over the episode's word sets.                                */

@@ -122,6 +122,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "attt_episode_pending_tokens": (i64, [P]),
             "attt_kl_workspace_bytes": (sz, [i64, i64, i64]),
             "attt_kl_drift": (i32, [P, P, P, i64, i64, i64, P, P, P, sz, P]),
+            "attt_logprob_workspace_bytes": (sz, [i64, i64, i64, i32]),
+            "attt_logprob_grad_workspace_bytes": (sz, [i64, i64, i64]),
+            "attt_logprob_forward": (i32, [P, i64, P, P, i64, i64, i64, f32, i32, P, P, P, P, P, P, sz, P]),
+            "attt_logprob_input_grad": (i32, [P, i64, P, P, P, P, P, P, i64, i64, i64, f32, P, P, sz, P]),
             "attt_batch_create": (i32, [ctypes.POINTER(BatchConfig), P, P, P, P, ctypes.POINTER(P)]),
             "attt_batch_destroy": (i32, [P]),
             "attt_batch_reset": (i32, [P, i32, P]),
@@ -190,6 +194,26 @@ def _expect(t: Optional[torch.Tensor], shape, dtype, name: str) -> None:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+
+
+def _rows_ptr(t: torch.Tensor, name: str) -> Tuple[int, int]:
+    """(address, row pitch in elements) of a 2-D CUDA tensor whose rows are
+    contiguous and do not overlap (a slice of a wider tensor's columns, say)."""
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else max(cols, 1)
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise ValueError(f"{name}: expected rows that are contiguous and do not overlap")
+    return t.data_ptr(), ld
+
+
+def _out_f32(t: Optional[torch.Tensor], shape, name: str, dev) -> torch.Tensor:
+    """`t`, checked, or a new float32 tensor of that shape."""
+    if t is None:
+        return torch.empty(shape, dtype=torch.float32, device=dev)
+    _expect(t, shape, torch.float32, name)
+    return t
 
 
 # --------------------------------------------------------------------------
@@ -732,6 +756,87 @@ def attt_kl_drift(hp: torch.Tensor, hq: torch.Tensor, W: torch.Tensor, kl: Optio
     _check((_lib or load_library()).attt_kl_drift(_bf16(hp), _bf16(hq), _bf16(W), L, d, V, _ptr(kl), _ptr(kl_mean),
                                         _ptr(workspace), workspace.numel(), _stream(stream)), "attt_kl_drift")
     return kl, kl_mean
+
+
+# --------------------------------------------------------------------------
+# log probabilities through the LM head
+# --------------------------------------------------------------------------
+
+LOGPROB_MAX_TOP = 20
+
+
+def attt_logprob_workspace_bytes(L: int, d: int, V: int, topk: int = 0) -> int:
+    return int(load_library().attt_logprob_workspace_bytes(int(L), int(d), int(V), int(topk)))
+
+
+def attt_logprob_grad_workspace_bytes(L: int, d: int, V: int) -> int:
+    return int(load_library().attt_logprob_grad_workspace_bytes(int(L), int(d), int(V)))
+
+
+def _logprob_check(h: torch.Tensor, W: torch.Tensor, tgt: Optional[torch.Tensor]):
+    if h.dim() != 2 or W.dim() != 2:
+        raise ValueError("h and W: expected 2-D tensors")
+    L, d = h.shape
+    V = W.shape[0]
+    _expect(h, (L, d), torch.bfloat16, "h")
+    _expect(W, (V, d), torch.bfloat16, "W")
+    _expect(tgt, (L,), torch.int32, "tgt")
+    return L, d, V
+
+
+def attt_logprob_forward(h: torch.Tensor, W: torch.Tensor, tgt: Optional[torch.Tensor] = None, topk: int = 0,
+                         inv_temp: float = 1.0, logp: Optional[torch.Tensor] = None,
+                         entropy: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         top_logp: Optional[torch.Tensor] = None, top_id: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None, stream=None):
+    """Log probabilities of the tokens `tgt` (int32 [L], -1: none) under softmax(h
+    W^T inv_temp), with every row's entropy, logsumexp and `topk` most probable
+    tokens.  h (bf16 [L, d]) may be a slice of wider rows.  Returns (logp, entropy,
+    lse, top_logp, top_id): fp32 [L] three times (logp None without tgt), fp32 and
+    int32 [L, topk]."""
+    L, d, V = _logprob_check(h, W, tgt)
+    dev = h.device
+    topk = int(topk)
+    if tgt is None and logp is not None:
+        raise ValueError("logp: there are no given tokens")
+    if tgt is not None:
+        logp = _out_f32(logp, (L,), "logp", dev)
+    entropy = _out_f32(entropy, (L,), "entropy", dev)
+    lse = _out_f32(lse, (L,), "lse", dev)
+    top_logp = _out_f32(top_logp, (L, topk), "top_logp", dev)
+    _expect(top_id, (L, topk), torch.int32, "top_id")
+    if top_id is None:
+        top_id = torch.empty(L, topk, dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(attt_logprob_workspace_bytes(L, d, V, topk), dtype=torch.uint8, device=dev)
+    ph, ld = _rows_ptr(h, "h")
+    _check((_lib or load_library()).attt_logprob_forward(
+        ph, ld, _ptr(W), _ptr(tgt), L, d, V, float(inv_temp), topk, _ptr(logp), _ptr(entropy), _ptr(lse),
+        _ptr(top_logp) if topk else None, _ptr(top_id) if topk else None, _ptr(workspace), workspace.numel(),
+        _stream(stream)), "attt_logprob_forward")
+    return logp, entropy, lse, top_logp, top_id
+
+
+def attt_logprob_input_grad(h: torch.Tensor, W: torch.Tensor, tgt: torch.Tensor, lse: torch.Tensor,
+                            glogp: torch.Tensor, entropy: Optional[torch.Tensor] = None,
+                            gent: Optional[torch.Tensor] = None, inv_temp: float = 1.0,
+                            dh: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                            stream=None) -> torch.Tensor:
+    """The gradient (bf16 [L, d]) of sum_j glogp_j logp_j + gent_j entropy_j with
+    respect to h, from the forward call's lse and (with gent) entropy.  Returns dh."""
+    L, d, V = _logprob_check(h, W, tgt)
+    for t, name in ((lse, "lse"), (glogp, "glogp"), (entropy, "entropy"), (gent, "gent")):
+        _expect(t, (L,), torch.float32, name)
+    _expect(dh, (L, d), torch.bfloat16, "dh")
+    if dh is None:
+        dh = torch.empty(L, d, dtype=torch.bfloat16, device=h.device)
+    if workspace is None:
+        workspace = torch.empty(attt_logprob_grad_workspace_bytes(L, d, V), dtype=torch.uint8, device=h.device)
+    ph, ld = _rows_ptr(h, "h")
+    _check((_lib or load_library()).attt_logprob_input_grad(
+        ph, ld, _ptr(W), _ptr(tgt), _ptr(lse), _ptr(entropy), _ptr(glogp), _ptr(gent), L, d, V, float(inv_temp),
+        _ptr(dh), _ptr(workspace), workspace.numel(), _stream(stream)), "attt_logprob_input_grad")
+    return dh
 
 
 # --------------------------------------------------------------------------

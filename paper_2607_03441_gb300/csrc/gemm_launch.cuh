@@ -226,10 +226,10 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
             ok = make_tmap_bf16(&tb2, p.b2, (uint64_t)p.b2_rows, (uint64_t)p.b2_k, (uint64_t)p.b2_rows_ld * 2, 64, 64);
         if (!ok) return ATTT_ERR_INVALID_ARG;
     }
-    // EPI_CE_EXP writes E through TMA stores: [M, G_ld] bf16, 32 x 32 boxes
+    // EPI_CE_EXP and EPI_LOGP_GRAD write their block through TMA stores: [M, G_ld] bf16, 32 x 32 boxes
     // EPI_F32_ACC reads and writes `out` through TMA: [M, N] fp32 of pitch out_ld, 32 x 32 boxes
     CUtensorMap tc = tb;
-    if (EPI == EPI_CE_EXP) {
+    if (epi_block(EPI)) {
         if (!make_tmap_bf16(&tc, ep.G, (uint64_t)ep.G_ld, (uint64_t)p.M, (uint64_t)ep.G_ld * 2, 32, 32, 64))
             return ATTT_ERR_INVALID_ARG;
     } else if (EPI == EPI_F32_ACC) {
@@ -251,7 +251,7 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
     g.BN = p.BN;
     // B rows one CTA stages (whole 64-column boxes when MN-major)
     const int bn_cta = !p.pair ? p.BN : B_MN ? (int)round_up(p.BN / 2, 64) : p.BN / 2;
-    g.e_stage_bytes = (EPI == EPI_CE_EXP || EPI == EPI_BF16) ? SETS * kEStageBytes
+    g.e_stage_bytes = (epi_block(EPI) || EPI == EPI_BF16) ? SETS * kEStageBytes
                       : (EPI == EPI_F32_ACC || EPI == EPI_F32_PART) ? kF32StageBytes
                       : EPI == EPI_KL                        ? kKlXBytes
                                                              : 0u;

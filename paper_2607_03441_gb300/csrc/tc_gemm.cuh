@@ -36,7 +36,17 @@ enum EpiKind : int {
     EPI_BF16 = 5,      // out16[m, n] = bf16(alpha * acc)  (row-major, through TMA boxes)
     EPI_F32_PART = 3,  // K piece of every tile: its fp32 accumulator to the piece's region of `out` (split_reduce.cu)
     EPI_KL = 6,        // A tile = 64 rows of A over the same 64 rows of A2: per (row, tile) max, sum of exp, cross term
+    EPI_LOGP = 7,      // per (row, column set): max, sum of exp, its first moment, target logit
+    EPI_LOGP_TOP8 = 8,    // the same with the set's 8 largest logits
+    EPI_LOGP_TOP20 = 9,   // the same with the set's 20 largest logits
+    EPI_LOGP_GRAD = 10,   // gradient block of log probabilities and entropies, bf16
 };
+
+// Largest logits that a log-probability epilogue keeps per row and column set.
+__host__ __device__ constexpr int epi_top(int epi) { return epi == EPI_LOGP_TOP8 ? 8 : epi == EPI_LOGP_TOP20 ? 20 : 0; }
+__host__ __device__ constexpr bool epi_logp(int epi) { return epi >= EPI_LOGP && epi <= EPI_LOGP_TOP20; }
+// Epilogues that write a bf16 block G through staged TMA stores.
+__host__ __device__ constexpr bool epi_block(int epi) { return epi == EPI_CE_EXP || epi == EPI_LOGP_GRAD; }
 
 constexpr int kMaxProj = 8;
 
@@ -66,6 +76,17 @@ struct EpiParams {
     // EPI_KL: five planes of [tiles, M] fp32 (m_p, s_p, m_q, s_q, x), kl_plane apart
     float *kl_part;
     int64_t kl_plane;
+    // EPI_LOGP*: three planes of [column sets, M] fp32 (max, sum, moment), lp_plane
+    // apart, and [column sets, M, top_ld] values and ids (tgt, ztgt as for CE)
+    float *lp_part;
+    int64_t lp_plane;
+    float *top_v;
+    int32_t *top_i;
+    int top_ld;  // a multiple of 4
+    float inv_temp;
+    // EPI_LOGP_GRAD: [M] each; gent nullptr: no entropy term
+    const float *lse, *entropy, *glogp, *gent;
+    int V;  // valid targets are below V (tgt, v0, G, G_ld, inv_temp as above)
 };
 
 struct GemmArgs {
@@ -481,6 +502,215 @@ __device__ __forceinline__ void epilogue_tile(const GemmArgs &g, int gm_base, in
     }
 }
 
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The K largest values that one row was offered, descending, the first offered
+// before later equal ones.  NaN and -inf are never taken; empty places hold (-inf, -1).
+template <int K>
+struct TopList {
+    float v[K > 0 ? K : 1];
+    int id[K > 0 ? K : 1];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            v[j] = -INFINITY;
+            id[j] = -1;
+        }
+    }
+    __device__ __forceinline__ float least() const { return v[K > 0 ? K - 1 : 0]; }
+    __device__ __forceinline__ void insert(float x, int i) {
+#pragma unroll
+        for (int j = K - 1; j >= 0; --j) {
+            const bool here = x > v[j];
+            const bool above = j > 0 && x > v[j > 0 ? j - 1 : 0];
+            if (here) {
+                v[j] = above ? v[j > 0 ? j - 1 : 0] : x;
+                id[j] = above ? id[j > 0 ? j - 1 : 0] : i;
+            }
+        }
+    }
+};
+
+// EPI_LOGP*: one pass over the set's columns, 32 at a time, with a running max.
+// With z the accumulator, c = log2 e / T, m the max: s = sum 2^((z - m) c) and
+// t = sum 2^((z - m) c) (z - m) c, so that lse = m / T + ln s and the entropy is
+// ln s - ln 2 t / s, both without a difference of large numbers.  A block's terms
+// are formed as 2^(z c - m2) with m2 = fl(m c), one FMA each, and what m2 was
+// rounded by is taken out of the sums.  -inf (also of columns past N) adds 0 to both
+// sums; NaN reaches s.  K > 0: a block's largest value joins the row's list as long
+// as it beats the list's least one; what it costs is instructions, not loads.
+template <int K, int SETS>
+__device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn, int set, uint32_t taddr) {
+    const EpiParams &ep = g.ep;
+    const bool rv = gm < g.M;
+    const int n_base = tn * g.BN;
+    const int c0 = set * (g.BN / SETS), c1 = c0 + g.BN / SETS;
+    const int n_end = min(g.N, n_base + c1);
+    const float c2 = ep.inv_temp * kLog2e;
+    const int t = ep.tgt && rv ? __ldg(ep.tgt + gm) : -1;
+    TopList<K> top;
+    top.clear();
+    float m = -INFINITY, s = 0.f, mom = 0.f, zt = 0.f;
+    bool hit = false;
+    for (int c = c0; c < c1 && n_base + c < n_end; c += 32) {
+        float v[32];
+        tmem_ld_x32(taddr + (uint32_t)c, v);
+        const int col0 = n_base + c;
+        if (col0 + 32 > n_end) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col0 + i >= n_end) v[i] = -INFINITY;
+        }
+        const int tc = t - col0;
+        if (tc >= 0 && tc < 32 && t < n_end) {
+            hit = true;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (tc == i) zt = v[i];
+        }
+        float b4[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b4[k] = v[k];
+#pragma unroll
+        for (int i = 4; i < 32; ++i) b4[i & 3] = fmaxf(b4[i & 3], v[i]);
+        float bm = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]));
+        const float mn = fmaxf(m, bm);
+        const float ref = mn == -INFINITY ? 0.f : mn, m2 = ref * c2;
+        float s4[4] = {0.f, 0.f, 0.f, 0.f}, t4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float d = fmaf(v[i], c2, -m2);
+            const float e = ex2(d);
+            s4[i & 3] += e;
+            t4[i & 3] = fmaf(e, fmaxf(d, -1e4f), t4[i & 3]);
+        }
+        // terms are 2^(-r) too large, r = m c - m2; the moment's (z - m) c is r too large
+        const float r = fmaf(ref, c2, -m2), rs = ex2(-r);
+        float bs = (s4[0] + s4[1]) + (s4[2] + s4[3]), bt = (t4[0] + t4[1]) + (t4[2] + t4[3]);
+        bt = rs * fmaf(-r, bs, bt);
+        bs *= rs;
+        if (m == mn || m == -INFINITY) {
+            s += bs;
+            mom += bt;
+        } else {
+            const float dm = (m - mn) * c2, f = ex2(dm);
+            mom = fmaf(f, fmaf(s, fmaxf(dm, -1e4f), mom), bt);
+            s = fmaf(s, f, bs);
+        }
+        m = mn;
+        if constexpr (K > 0) {
+            if (!rv) bm = -INFINITY;
+            while (bm > top.least()) {
+                int at = 31;
+#pragma unroll
+                for (int i = 30; i >= 0; --i)
+                    if (v[i] == bm) at = i;
+                top.insert(bm, col0 + at);
+                float nx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    if (i == at) v[i] = -INFINITY;
+                    nx[i & 3] = fmaxf(nx[i & 3], v[i]);
+                }
+                bm = fmaxf(fmaxf(nx[0], nx[1]), fmaxf(nx[2], nx[3]));
+            }
+            __syncwarp();
+        }
+    }
+    if (!rv || n_base + c0 >= g.N) return;
+    const int64_t o = (int64_t)(SETS * tn + set) * g.M + gm;
+    if (!ATTT_GUARD(o < ep.lp_plane, g.status)) return;
+    ep.lp_part[o] = m;
+    ep.lp_part[ep.lp_plane + o] = s;
+    ep.lp_part[2 * ep.lp_plane + o] = mom;
+    if (hit && ep.ztgt) ep.ztgt[gm] = zt;
+    if constexpr (K > 0) {
+#pragma unroll
+        for (int j = 0; j < K; j += 4)
+            if (j < ep.top_ld) {
+                *reinterpret_cast<float4 *>(ep.top_v + o * ep.top_ld + j) =
+                    make_float4(top.v[j], top.v[j + 1], top.v[j + 2], top.v[j + 3]);
+                *reinterpret_cast<int4 *>(ep.top_i + o * ep.top_ld + j) =
+                    make_int4(top.id[j], top.id[j + 1], top.id[j + 2], top.id[j + 3]);
+            }
+    }
+}
+
+// EPI_LOGP_GRAD: with p = exp(z / T - lse), the gradient of sum_j a_j logp_j + b_j
+// H_j with respect to z_jv,
+//   g = (a [v = t] - p (a + b (log p + H))) / T,
+// formed in fp32, rounded once to bf16 and stored as the block G that the second
+// contraction reads (relative errors of 2^-8 at most, independent over the
+// vocabulary: dh is off by 6e-4 of its norm, its own rounding to bf16 by 1.7e-3).
+// Columns past N within the tile are stored as zeros.  A row without a given token
+// (t < 0) has a = 0; an invalid target makes its row NaN.
+template <int SETS>
+__device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_base, int tn, int set, int row,
+                                                   uint32_t taddr, const CUtensorMap *tmE, uint32_t sE,
+                                                   uint32_t &ec) {
+    const EpiParams &ep = g.ep;
+    const int gm = gm_base + row;
+    const bool rv = gm < g.M;
+    const int n_base = tn * g.BN;
+    const int c0 = set * (g.BN / SETS), c1 = c0 + g.BN / SETS;
+    const int n_end = min(g.N, n_base + c1);
+    const int lane = row & 31, y = gm - lane;
+    if (y >= g.M) return;  // every row of this warp lies past M (warp-uniform)
+    // log p = fl(z / T - lse) first: one rounding of a small number, and not those of
+    // z / T log2 e and lse log2 e, which peaked rows (lse 130) feel in 1 - p
+    float lse = 0.f, A = 0.f, B = 0.f, at = 0.f;
+    int t = -1;
+    if (rv) {
+        t = __ldg(ep.tgt + gm);
+        float a = t == -1 ? 0.f : __ldg(ep.glogp + gm);
+        if (t < -1 || t >= ep.V) {
+            if (tn == 0 && set == 0) record_error(g.status, ATTT_ERR_TOKEN_RANGE);
+            a = __int_as_float(0x7fc00000);
+        }
+        lse = __ldg(ep.lse + gm);
+        at = a * ep.inv_temp;
+        A = at;
+        if (ep.gent) {
+            const float b = __ldg(ep.gent + gm);
+            A = fmaf(b * ep.inv_temp, __ldg(ep.entropy + gm), at);
+            B = b * ep.inv_temp;
+        }
+        t -= ep.v0;
+    }
+    for (int c = c0; c < c1; c += 32) {
+        float v[32];
+        tmem_ld_x32(taddr + (uint32_t)c, v);
+        const int col0 = n_base + c;
+        const int tc = t - col0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float lp = fmaf(v[i], ep.inv_temp, -lse);
+            v[i] = -ex2(lp * kLog2e) * fmaf(B, fmaxf(lp, -1e4f), A);
+        }
+        if (tc >= 0 && tc < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (tc == i) v[i] += at;
+        }
+        if (col0 + 32 > n_end) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col0 + i >= n_end) v[i] = 0.f;
+        }
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            __nv_bfloat162 b = __floats2bfloat162_rn(v[i], v[i + 1]);
+            pk[i / 2] = *reinterpret_cast<uint32_t *>(&b);
+        }
+        e_block_store(tmE, sE, (int)(ec++), lane, pk, col0, y);
+    }
+}
+
 // EPI_KL.  The CTA's 128 accumulator rows are 64 rows of z_p = h_p W^T
 // (TMEM lanes 0-63: warp quarters 0, 1) over the same 64 rows of z_q =
 // h_q W^T (lanes 64-127: quarters 2, 3), so quarter q and quarter q + 2 hold
@@ -810,6 +1040,11 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
                 const int gm = wi.tm * 128 + row;
                 bf16_tile_store(g, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec, lane, gm - lane, wi.tn * g.BN,
                                 min(g.N, (wi.tn + 1) * g.BN), taddr);
+            } else if constexpr (epi_logp(EPI)) {
+                epilogue_logp<epi_top(EPI), SETS>(g, wi.tm * 128 + row, wi.tn, set, taddr);
+            } else if constexpr (EPI == EPI_LOGP_GRAD) {
+                epilogue_logp_grad<SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC,
+                                         smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else {
                 epilogue_tile<EPI, SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);
@@ -1073,6 +1308,11 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
             } else if constexpr (EPI == EPI_BF16) {
                 bf16_tile_store(g, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec, lane, gm_base + 32 * q,
                                 wi.tn * g.BN, min(g.N, (wi.tn + 1) * g.BN), taddr);
+            } else if constexpr (epi_logp(EPI)) {
+                epilogue_logp<epi_top(EPI), SETS>(g, gm_base + row, wi.tn, set, taddr);
+            } else if constexpr (EPI == EPI_LOGP_GRAD) {
+                epilogue_logp_grad<SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC,
+                                         smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else {
                 epilogue_tile<EPI, SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);
