@@ -334,6 +334,36 @@ ATTT_API attt_status attt_lora_adamw_step(float *d_A32, float *d_B32, const floa
                                           double weight_decay, int step, attt_bf16 *d_A16, attt_bf16 *d_B16,
                                           attt_stream stream);
 
+/* Workspace bytes attt_lora_muon_step needs.  0 for sizes that it refuses. */
+ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, const int64_t *dout, int r);
+
+/*
+ * A step along orthogonalised momentum (Muon) as a third alternative, for nproj
+ * projections at once (host arrays of nproj device pointers and sizes): for each
+ * matrix X of A_p [din[p], r] and B_p [r, dout[p]] with gradient g and momentum m
+ * (fp32, caller-owned, zero before the first step):
+ *   m <- momentum m + g;  u = g + momentum m (nesterov != 0) or m
+ *   X_0 = u / (|u|_F + eps)
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X, ns_steps times, with
+ *        (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *   p <- p (1 - lr weight_decay) - lr rms sqrt(max(rows, columns)) X
+ * so that the update's root mean square is about lr rms.  The bf16 copies are
+ * refreshed (round to nearest even) when the arrays d_A16, d_B16 and their
+ * entries are not NULL.  fp32 products and sums; a zero gradient with zero
+ * momentum (the dA of B = 0) gives X = 0.  A matrix with a NaN or an infinity in u,
+ * or with |u|_F^2 beyond fp32, becomes NaN as a whole; the others do not feel it.
+ * Requirements: 1 <= nproj <= 8, 1 <= r <= 64, 1 <= din, dout <= 2^31,
+ * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps > 0, 1 <= ns_steps <= 16, all
+ * finite, no two matrices alike, d_ws at least attt_lora_muon_workspace_bytes(...)
+ * bytes and 256-byte aligned.  One launch.
+ */
+ATTT_API attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_B32,
+                                         const float *const *d_dA, const float *const *d_dB, float *const *d_mA,
+                                         float *const *d_mB, const int64_t *din, const int64_t *dout, int r, float lr,
+                                         float momentum, int nesterov, float weight_decay, float rms, float eps,
+                                         int ns_steps, attt_bf16 *const *d_A16, attt_bf16 *const *d_B16, void *d_ws,
+                                         size_t ws_bytes, attt_stream stream);
+
 /* ------------------------------------------------------------------------ */
 /* The adapted projection of a chained update: the LoRA-adapted linear map   */
 /* y = x W0 + s (x A) B (Appendix C adapter; W0 frozen) whose output is the  */
@@ -406,6 +436,47 @@ ATTT_API size_t attt_kl_workspace_bytes(int64_t L, int64_t d, int64_t V);
 ATTT_API attt_status attt_kl_drift(const attt_bf16 *d_hp, const attt_bf16 *d_hq, const attt_bf16 *d_W,
                                    int64_t L, int64_t d, int64_t V, float *d_kl, float *d_kl_mean,
                                    void *d_ws, size_t ws_bytes, attt_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Layer norm: the norm between the adapted projection and the LM head, and */
+/* its gradients.                                                           */
+/* ------------------------------------------------------------------------ */
+
+typedef enum attt_dtype { ATTT_BF16 = 0, ATTT_F32 = 1 } attt_dtype;
+
+/*
+ * For each of L rows x_j (d values of type `dtype` at d_x + j x_ld elements):
+ *   mean_j = mean(x_j),  rstd_j = 1 / sqrt(mean((x_j - mean_j)^2) + eps)
+ *   y_j = (x_j - mean_j) rstd_j gamma + beta   (type `dtype`, at d_y + j y_ld)
+ * gamma and beta fp32 [d] (beta NULL: none), d_mean and d_rstd fp32 [L] (either may
+ * be NULL).  All sums fp32, one rounding at the end.  Requirements: L >= 0 (0
+ * launches nothing), 1 <= d <= 2^24, x_ld, y_ld >= d, eps >= 0, pointers aligned to
+ * their type.  Rows whose addresses are multiples of 16 bytes are read and
+ * written 16 bytes at a time, others value by value.
+ */
+ATTT_API attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, const float *d_gamma,
+                                             const float *d_beta, int64_t L, int64_t d, float eps, int dtype,
+                                             void *d_y, int64_t y_ld, float *d_mean, float *d_rstd,
+                                             attt_stream stream);
+
+/* Workspace bytes attt_layer_norm_backward needs. */
+ATTT_API size_t attt_layer_norm_workspace_bytes(int64_t L, int64_t d);
+
+/*
+ * The gradients of the forward call's x, gamma and beta from that of y (dy, rows
+ * dy_ld apart), with the forward call's mean and rstd; xh = (x - mean) rstd:
+ *   dx_j = rstd_j (g - mean(g) - xh_j mean(g xh_j)),  g = dy_j gamma   (`dtype`)
+ *   dgamma = sum_j dy_j xh_j,  dbeta = sum_j dy_j       (fp32 [d], either may be
+ *                                                        NULL; zeros for L = 0)
+ * The sums over the rows are fp32 in a fixed order.  Requirements as above, d_ws at
+ * least attt_layer_norm_workspace_bytes(L, d) bytes and 256-byte aligned.  Two
+ * launches.
+ */
+ATTT_API attt_status attt_layer_norm_backward(const void *d_dy, int64_t dy_ld, const void *d_x, int64_t x_ld,
+                                              const float *d_gamma, const float *d_mean, const float *d_rstd,
+                                              int64_t L, int64_t d, int dtype, void *d_dx, int64_t dx_ld,
+                                              float *d_dgamma, float *d_dbeta, void *d_ws, size_t ws_bytes,
+                                              attt_stream stream);
 
 /* ------------------------------------------------------------------------ */
 /* Log probabilities through the frozen LM head: of given tokens, with the  */

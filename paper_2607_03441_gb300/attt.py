@@ -122,6 +122,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "attt_episode_pending_tokens": (i64, [P]),
             "attt_kl_workspace_bytes": (sz, [i64, i64, i64]),
             "attt_kl_drift": (i32, [P, P, P, i64, i64, i64, P, P, P, sz, P]),
+            "attt_lora_muon_workspace_bytes": (sz, [i32, P, P, i32]),
+            "attt_lora_muon_step": (i32, [i32, P, P, P, P, P, P, P, P, i32, f32, f32, i32, f32, f32, f32, i32, P, P, P,
+                                          sz, P]),
+            "attt_layer_norm_forward": (i32, [P, i64, P, P, i64, i64, f32, i32, P, i64, P, P, P]),
+            "attt_layer_norm_workspace_bytes": (sz, [i64, i64]),
+            "attt_layer_norm_backward": (i32, [P, i64, P, i64, P, P, P, i64, i64, i32, P, i64, P, P, P, sz, P]),
             "attt_logprob_workspace_bytes": (sz, [i64, i64, i64, i32]),
             "attt_logprob_grad_workspace_bytes": (sz, [i64, i64, i64]),
             "attt_logprob_forward": (i32, [P, i64, P, P, i64, i64, i64, f32, i32, P, P, P, P, P, P, sz, P]),
@@ -759,6 +765,77 @@ def attt_kl_drift(hp: torch.Tensor, hq: torch.Tensor, W: torch.Tensor, kl: Optio
 
 
 # --------------------------------------------------------------------------
+# layer norm
+# --------------------------------------------------------------------------
+
+_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _norm_check(x: torch.Tensor, gamma: torch.Tensor):
+    if x.dim() != 2:
+        raise ValueError(f"x: expected a 2-D [L, d] tensor, got shape {tuple(x.shape)}")
+    L, d = x.shape
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"x: expected bfloat16 or float32, got {x.dtype}")
+    _expect(gamma, (d,), torch.float32, "gamma")
+    return L, d, dtype
+
+
+def attt_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None,
+                            eps: float = 1e-5, y: Optional[torch.Tensor] = None,
+                            mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm of the rows of x (bf16 or fp32 [L, d], rows may lie inside wider
+    ones), gamma and beta fp32 [d].  Returns (y, mean, rstd): y of x's type, fp32 [L]
+    twice."""
+    L, d, dtype = _norm_check(x, gamma)
+    _expect(beta, (d,), torch.float32, "beta")
+    _expect(y, (L, d), x.dtype, "y")
+    if y is None:
+        y = torch.empty(L, d, dtype=x.dtype, device=x.device)
+    mean = _out_f32(mean, (L,), "mean", x.device)
+    rstd = _out_f32(rstd, (L,), "rstd", x.device)
+    px, x_ld = _rows_ptr(x, "x")
+    py, y_ld = _rows_ptr(y, "y")
+    _check((_lib or load_library()).attt_layer_norm_forward(
+        px, x_ld, _ptr(gamma), _ptr(beta), L, d, eps, dtype, py, y_ld, _ptr(mean), _ptr(rstd), _stream(stream)),
+        "attt_layer_norm_forward")
+    return y, mean, rstd
+
+
+def attt_layer_norm_workspace_bytes(L: int, d: int) -> int:
+    return int(load_library().attt_layer_norm_workspace_bytes(int(L), int(d)))
+
+
+def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, mean: torch.Tensor,
+                             rstd: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                             dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of the layer norm's x, gamma and beta from dy (bf16 or fp32 [L, d]),
+    with the forward call's mean and rstd.  Returns (dx, dgamma, dbeta): dx of x's
+    type, fp32 [d] twice."""
+    L, d, dtype = _norm_check(x, gamma)
+    dev = x.device
+    _expect(dy, (L, d), x.dtype, "dy")
+    _expect(mean, (L,), torch.float32, "mean")
+    _expect(rstd, (L,), torch.float32, "rstd")
+    _expect(dx, (L, d), x.dtype, "dx")
+    if dx is None:
+        dx = torch.empty(L, d, dtype=x.dtype, device=dev)
+    dgamma = _out_f32(dgamma, (d,), "dgamma", dev)
+    dbeta = _out_f32(dbeta, (d,), "dbeta", dev)
+    if workspace is None:
+        workspace = torch.empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=dev)
+    pg, g_ld = _rows_ptr(dy, "dy")
+    px, x_ld = _rows_ptr(x, "x")
+    po, o_ld = _rows_ptr(dx, "dx")
+    _check((_lib or load_library()).attt_layer_norm_backward(
+        pg, g_ld, px, x_ld, _ptr(gamma), _ptr(mean), _ptr(rstd), L, d, dtype, po, o_ld, _ptr(dgamma), _ptr(dbeta),
+        _ptr(workspace), workspace.numel(), _stream(stream)), "attt_layer_norm_backward")
+    return dx, dgamma, dbeta
+
+
+# --------------------------------------------------------------------------
 # log probabilities through the LM head
 # --------------------------------------------------------------------------
 
@@ -991,3 +1068,63 @@ def attt_lora_adamw_step(A32: torch.Tensor, B32: torch.Tensor, dA: torch.Tensor,
         float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step),
         _bf16(A16) if A16 is not None else None, _bf16(B16) if B16 is not None else None, _stream(stream)),
         "attt_lora_adamw_step")
+
+
+# --------------------------------------------------------------------------
+# the step along orthogonalised momentum (Muon)
+# --------------------------------------------------------------------------
+
+def attt_lora_muon_workspace_bytes(dins: Sequence[int], douts: Sequence[int], r: int) -> int:
+    k = len(dins)
+    if len(douts) != k:
+        raise ValueError("dins and douts must have one entry per projection")
+    arr = (ctypes.c_int64 * (2 * k))(*[int(x) for x in dins], *[int(x) for x in douts])
+    base = ctypes.addressof(arr)
+    return int(load_library().attt_lora_muon_workspace_bytes(k, base, base + 8 * k, int(r)))
+
+
+def attt_lora_muon_step(A32s: Sequence[torch.Tensor], B32s: Sequence[torch.Tensor], dAs: Sequence[torch.Tensor],
+                        dBs: Sequence[torch.Tensor], mAs: Sequence[torch.Tensor], mBs: Sequence[torch.Tensor],
+                        lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                        rms: float = 0.2, eps: float = 1e-7, ns_steps: int = 5,
+                        A16s: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                        B16s: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """In-place Muon step of the adapters of some projections (A [din, r], B [r, dout],
+    one rank): fp32 masters and momenta, bf16 refresh."""
+    k = len(A32s)
+    if k < 1 or any(len(ts) != k for ts in (B32s, dAs, dBs, mAs, mBs)) or (A16s is not None and len(A16s) != k) \
+            or (B16s is not None and len(B16s) != k):
+        raise ValueError("every list must have one entry per projection")
+    f32, bf16 = torch.float32, torch.bfloat16
+    if A32s[0].dim() != 2:
+        raise ValueError(f"A32s[0]: expected a 2-D [din, r] tensor, got shape {tuple(A32s[0].shape)}")
+    r = A32s[0].shape[1]
+    dins, douts = [], []
+    for i in range(k):
+        A, B = A32s[i], B32s[i]
+        if A.dim() != 2 or B.dim() != 2:
+            raise ValueError(f"A32s[{i}], B32s[{i}]: expected 2-D tensors")
+        sa, sb = (A.shape[0], r), (r, B.shape[1])
+        dins.append(sa[0])
+        douts.append(sb[1])
+        for ts, shape, dtype, name in ((A32s, sa, f32, "A32s"), (dAs, sa, f32, "dAs"), (mAs, sa, f32, "mAs"),
+                                       (B32s, sb, f32, "B32s"), (dBs, sb, f32, "dBs"), (mBs, sb, f32, "mBs"),
+                                       (A16s, sa, bf16, "A16s"), (B16s, sb, bf16, "B16s")):
+            t = ts[i] if ts is not None else None
+            if t is not None and (t.shape != shape or t.dtype != dtype):
+                _expect(t, shape, dtype, f"{name}[{i}]")
+    if workspace is None:
+        workspace = torch.empty(attt_lora_muon_workspace_bytes(dins, douts, r), dtype=torch.uint8,
+                                device=A32s[0].device)
+    vals = dins + douts
+    for ts in (A32s, B32s, dAs, dBs, mAs, mBs, A16s or (), B16s or ()):
+        vals += [_ptr(t) or 0 for t in ts]
+    buf = (ctypes.c_int64 * len(vals))(*vals)
+    base = ctypes.addressof(buf)
+    at = [base + 8 * k * i for i in range(9)]
+    p16a = at[8] if A16s is not None else None
+    p16b = base + 8 * k * (9 if A16s is not None else 8) if B16s is not None else None
+    _check((_lib or load_library()).attt_lora_muon_step(
+        k, at[2], at[3], at[4], at[5], at[6], at[7], at[0], at[1], r, lr, momentum, 1 if nesterov else 0, weight_decay,
+        rms, eps, ns_steps, p16a, p16b, _ptr(workspace), workspace.numel(), _stream(stream)), "attt_lora_muon_step")
