@@ -4,8 +4,8 @@ Bounds, u = 2^-24: a row's sum goes through at most 32 additions in a thread, te
 in shuffles and one per 1,024 threads' worth of longer rows, so it is off by at
 most 64 u of the sum of its terms' sizes (rows of up to 21,000 values); what follows
 adds a few u.  Results rounded to bf16 (8 bits) are off by 2^-8 of themselves.  A
-weight's sum over the rows takes at most 24 additions per block (14,000 rows in 608
-blocks), 40 more across blocks and 8 between groups: 256 u of its terms."""
+weight's sum over the rows takes at most 93 additions in a thread (14,000 rows in 152
+blocks), 26 across blocks and 16 between groups: 256 u of its terms."""
 import numpy as np
 import pytest
 import torch
