@@ -20,13 +20,20 @@
 // A matrix belongs to one cluster; each CTA holds a range of columns in shared
 // memory from the first read of g and m to the update of p (what does not fit
 // goes through a workspace that stays in L2).  The CTAs' Gram matrices are summed
-// through distributed shared memory in CTA order; at r > 32 each CTA forms a slab of
-// rows of every r x r product and stores it to all of them, below that all form
-// all of it, which takes less time than a barrier.  fp32 FMA throughout: the
-// Gram matrices need their 24 bits.
-// Bound: fp32 FMA issue at r 64 (6 r^2 n of them), barriers below.
+// through distributed shared memory in CTA order: each CTA gets its slab of rows from
+// all of them, sums, and gives it to all.  At r > 32 the r x r products are formed in
+// slabs too; below that every CTA forms all of it, which takes less time than an
+// exchange.  Exchanges are bulk copies between the CTAs' shared memories counted on
+// mbarriers (measured at 8 / 12 to 16 CTAs of 512 threads, 17 KB to each: 0.8 us; plain
+// stores and a cluster barrier 1.1 / 1.6).  fp32 FMA throughout: the Gram matrices need
+// their 24 bits.
+// Bound: fp32 FMA issue at r 64 (5 r^2 n of them), exchanges and launch below.
 #include <algorithm>
+#include <array>
 #include <cmath>
+#include <map>
+#include <mutex>
+#include <utility>
 
 #include "attt_common.cuh"
 #include "attt_host.h"
@@ -34,8 +41,9 @@
 namespace attt {
 
 constexpr int kMuonMats = 16;  // two per projection
-constexpr int kMuonCols = 128;  // columns of a tile
 constexpr int kMuonThreads = 512;
+constexpr int kMuonStage = 128;  // columns of a tile that does not stay
+constexpr int kMuonMaxCluster = 16;
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 
 struct MuonMat {
@@ -46,47 +54,97 @@ struct MuonMat {
     int64_t n;   // width beside r
     int64_t per; // columns of a CTA, a multiple of 8
     int tall;    // [n, r] (A), else [r, n] (B)
+    int vec;     // whether four neighbours in memory may move at once
     float step;  // lr rms sqrt(max(rows, columns))
 };
 
 struct MuonArgs {
     MuonMat mat[kMuonMats];
-    int r, nesterov, steps, slots, cluster;
+    int r, nesterov, steps, cluster;
+    int room;        // columns that fit in shared memory
+    uint32_t inv_r;  // ceil(2^32 / r), r > 1: e / r is the high half of e inv_r for e < 2^26
     float mu, keep, eps;  // keep = 1 - lr wd
+    int *status;
 };
 
 template <int RP>
 struct MuonShape {
     static constexpr int LD = RP + 4;  // rows of 16-byte groups that start 4 banks apart
     static constexpr bool kSlabs = RP > 32;
-    static constexpr int TJ = RP > 32 ? 8 : 4;                       // a thread's Gram tile: 4 x TJ
-    static constexpr int kTiles = (RP / 4) * (RP / TJ);              // threads of a Gram matrix
-    static constexpr int kSubs = kMuonThreads / kTiles;              // that many share the columns
-    static constexpr int NC = RP * kMuonCols / 4 / kMuonThreads;     // a thread's product tile: NC columns x 4
-    static constexpr int CL = kMuonCols / NC;
-    static constexpr int kMat = RP * LD, kTile = kMuonCols * LD;     // floats
-    static constexpr int kScratch = kSubs * RP * RP;
-    // G, B, T over the scratch of the subsets' sums (never needed together); then the
-    // CTA's part of the Gram matrix, two in turn where no barrier follows its reads
+    // A thread's Gram tile: 4 x TJ.  At r 64 a warp forms one of three 32 x 32 quadrants
+    // (the fourth is the second's mirror image): 3 bank-conflict-free reads for 32 FMAs.
+    static constexpr int TJ = RP > 32 ? 8 : 4;
+    static constexpr int kTiles = RP > 32 ? 96 : (RP / 4) * (RP / 4);
+    static constexpr int kSubs = kMuonThreads / kTiles;  // that many threads share a tile's columns
+    static constexpr int CL = kMuonThreads / (RP / 8);   // product: columns at a time, 8 rows of X per thread
+    static constexpr int kMat = RP * LD;                 // floats
+    static constexpr int kScratch = kSubs * kTiles * 4 * TJ;
+    // G, B, T over the scratch of the threads' sums (never needed together); the CTA's own
+    // Gram matrix; what the others send of its slab of theirs
     static constexpr int kFirst = 3 * kMat > kScratch ? 3 * kMat : kScratch;
-    static constexpr int kParts = kSlabs ? 1 : 2;
-    static constexpr int kFixed = kFirst + kParts * RP * RP;
+    // (cluster x rows of a slab, which are not even: up to RP + cluster rows)
+    static constexpr int kRecv = (RP + kMuonMaxCluster) * RP;
+    static constexpr int kFixed = kFirst + RP * RP + kRecv;
+    // Row and column of a Gram tile's first element.
+    __device__ static __forceinline__ void tile(int t, int &i0, int &j0) {
+        if constexpr (RP > 32) {
+            const int quad = t / 32, lane = t % 32;
+            i0 = (quad == 2 ? 32 : 0) + lane / 4 * 4;
+            j0 = (quad >= 1 ? 32 : 0) + lane % 4 * 8;
+        } else {
+            i0 = t / (RP / 4) * 4;
+            j0 = t % (RP / 4) * 4;
+        }
+    }
 };
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(addr)
-                 : "memory");
-    return v;
-}
+// Rows [first, second) of an r x r matrix that CTA `rank` of `cluster` forms.
+__device__ __forceinline__ int muon_row(int RP, int rank, int cluster) { return rank * RP / cluster; }
 
-__device__ __forceinline__ void st_cluster_f4(uint32_t addr, float4 v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z),
-                 "f"(v.w)
-                 : "memory");
-}
+// Exchanges of the cluster: number `n` (0, 1, ..) is counted on barrier n & 1.  A CTA
+// sends for exchange n + 1 when it has all of exchange n, and so has nothing more to
+// read of what exchange n came from; what CTAs send for exchange n + 2 follows this
+// CTA's own data of n + 1.
+struct MuonLink {
+    uint32_t bar0;
+    int cluster, rank;
+    volatile int *abort_flag;
+    int *status;
+
+    // One thread: `bytes` will come in exchange n.
+    __device__ __forceinline__ void expect(uint32_t n, uint32_t bytes) const {
+        mbar_arrive_expect_tx(bar0 + 8u * (n & 1u), bytes);
+    }
+    // One thread per receiver: copies `bytes` of this CTA's shared memory to `dst` (an
+    // address of this CTA's own) in CTA `to`.
+    __device__ __forceinline__ void send(uint32_t n, uint32_t dst, uint32_t src, uint32_t bytes, int to) const {
+        asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                         mapa_shared(dst, to)),
+                     "r"(src), "r"(bytes), "r"(mapa_shared(bar0 + 8u * (n & 1u), to))
+                     : "memory");
+    }
+    // All threads: exchange n has arrived.  If it does not within the limit, the status word
+    // says so and the CTA goes on to its end on garbage, waiting for nothing.
+    __device__ __forceinline__ void receive(uint32_t n) const {
+        if (!mbar_wait(bar0 + 8u * (n & 1u), (n >> 1) & 1u, abort_flag)) {
+            *abort_flag = 1;
+            record_error(status, ATTT_ERR_TIMEOUT);
+        }
+    }
+    // All threads: this CTA's rows [r0, r1) of z (LD floats each) to all CTAs, and theirs
+    // of `total` from them.
+    template <int LD>
+    __device__ __forceinline__ void share(uint32_t n, const float *z, int r0, int r1, int total) const {
+        fence_proxy_async_smem();
+        __syncthreads();
+        if (threadIdx.x == 0) expect(n, (uint32_t)((total - (r1 - r0)) * LD * 4));
+        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank && r1 > r0) {
+            const uint32_t at = smem_u32(z + r0 * LD);
+            send(n, at, at, (uint32_t)((r1 - r0) * LD * 4), threadIdx.x);
+        }
+        receive(n);
+    }
+};
 
 __device__ __forceinline__ float4 shfl_xor4(float4 v, int o) {
     return make_float4(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o),
@@ -97,58 +155,177 @@ __device__ __forceinline__ float4 add4(float4 a, float4 b) {
     return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
 }
 
-// Calls f(at, c, k) for the elements of columns [0, cols) of the tile from c0: `at` the
-// index in global memory, c < cols, k < r.  Threads of a warp take neighbours in
-// memory whose places s[c][k] lie in different banks.
-template <int RP, class F>
-__device__ __forceinline__ void muon_elements(const MuonMat &t, int r, int64_t c0, int cols, F &&f) {
-    if (t.tall) {
-        for (int e = threadIdx.x; e < cols * r; e += kMuonThreads) {
-            const int c = e / r;
-            f(c0 * r + e, c, e - c * r);
+// Shared memory is named by its place in s_muon: functions of their own know no other
+// way that an address is not global.
+extern __shared__ float4 s_muon[];
+__device__ __forceinline__ float *muon_smem(int at) { return reinterpret_cast<float *>(s_muon) + at; }
+
+// The elements of columns [0, cols) from column c0 on, U items of 1 (or, V4, 4
+// neighbours in memory) per thread at a time: first(u, at) for each of them, then
+// second(u, at, so), so that U loads are on their way together.  `at`: index from the
+// first column's first element in global memory; so: place in shared memory.
+// Neighbours are the rows k .. k + 3 of a column (tall), or the columns c .. c + 3.
+template <int RP, int U, bool V4, class F, class S>
+__device__ __forceinline__ void muon_items(const MuonMat &t, int r, uint32_t inv_r, int cols, F &&first, S &&second) {
+    constexpr int W = V4 ? 4 : 1, LD = MuonShape<RP>::LD;
+    // a warp of a wide matrix's items: 8 columns x 4 rows, or 4 x 4 columns x 8 rows
+    constexpr int KR = V4 ? 8 : 4, CW = V4 ? 16 : 8;
+    const int groups = (cols + CW - 1) / CW, width = (int)t.n;
+    const int items = t.tall ? cols * r / W : groups * (RP / KR) * 32;
+    for (int e0 = threadIdx.x; e0 < items; e0 += U * kMuonThreads) {
+        uint32_t at[U];
+        int so[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = e0 + u * kMuonThreads;
+            if (t.tall) {
+                const int c = r == 1 ? e : (int)__umulhi((uint32_t)(W * e), inv_r);
+                at[u] = (uint32_t)(W * e);
+                so[u] = c * LD + W * e - c * r;
+                in[u] = e < items;
+            } else {
+                const int b = e >> 5, lane = e & 31, kb = b / groups;
+                const int k = kb * KR + (V4 ? lane >> 2 : lane >> 3);
+                const int c = (b - kb * groups) * CW + (V4 ? (lane & 3) * 4 : lane & 7);
+                at[u] = (uint32_t)k * (uint32_t)width + (uint32_t)c;
+                so[u] = c * LD + k;
+                in[u] = e < items && k < r && c < cols;
+            }
+            if (in[u]) first(u, at[u]);
         }
-    } else {  // a warp: 8 columns x 4 rows
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = (cols + 7) / 8;
-        for (int b = warp; b < groups * (RP / 4); b += kMuonThreads / 32) {
-            const int k = b / groups * 4 + (lane >> 3), c = b % groups * 8 + (lane & 7);
-            if (k < r && c < cols) f(k * t.n + c0 + c, c, k);
-        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (in[u]) second(u, at[u], so[u]);
     }
 }
 
-// u of a tile into s (rows of r..RP stay 0), m updated when `first`.
+// The first column's first element.
+__device__ __forceinline__ int64_t muon_origin(const MuonMat &t, int r, int64_t c0) { return t.tall ? c0 * r : c0; }
+
+// u of the columns into s (rows of r..RP stay 0), m updated when `first`.  (The passes over
+// columns are functions of their own: inlined, what lives across them spills inside
+// their loops.)
+template <int RP, bool V4>
+__device__ __forceinline__ void muon_load_as(const MuonArgs &a, const MuonMat &t, float *s, int64_t c0, int cols,
+                                             bool first) {
+    constexpr int LD = MuonShape<RP>::LD, W = V4 ? 4 : 1, U = V4 ? 3 : 6;
+    const int64_t o = muon_origin(t, a.r, c0);
+    const float *pg = t.g + o;
+    float *pm = t.m + o;
+    float g[U][W], m[U][W];
+    muon_items<RP, U, V4>(
+        t, a.r, a.inv_r, cols,
+        [&](int u, uint32_t at) {
+            if constexpr (V4) {
+                const float4 x = __ldg(reinterpret_cast<const float4 *>(pg + at));
+                const float4 y = *reinterpret_cast<const float4 *>(pm + at);
+                g[u][0] = x.x; g[u][1] = x.y; g[u][2] = x.z; g[u][3] = x.w;
+                m[u][0] = y.x; m[u][1] = y.y; m[u][2] = y.z; m[u][3] = y.w;
+            } else {
+                g[u][0] = __ldg(pg + at);
+                m[u][0] = pm[at];
+            }
+        },
+        [&](int u, uint32_t at, int so) {
+            if (first) {
+#pragma unroll
+                for (int w = 0; w < W; ++w) m[u][w] = fmaf(a.mu, m[u][w], g[u][w]);
+                if constexpr (V4)
+                    *reinterpret_cast<float4 *>(pm + at) = make_float4(m[u][0], m[u][1], m[u][2], m[u][3]);
+                else
+                    pm[at] = m[u][0];
+            }
+            if (a.nesterov)
+#pragma unroll
+                for (int w = 0; w < W; ++w) m[u][w] = fmaf(a.mu, m[u][w], g[u][w]);
+            if (V4 && t.tall) {
+                *reinterpret_cast<float4 *>(s + so) = make_float4(m[u][0], m[u][W / 4], m[u][W / 2], m[u][W - 1]);
+            } else {
+#pragma unroll
+                for (int w = 0; w < W; ++w) s[so + w * LD] = m[u][w];
+            }
+        });
+}
+
 template <int RP>
-__device__ __forceinline__ void muon_load(const MuonArgs &a, const MuonMat &t, float *s, int64_t c0, int cols,
-                                          bool first) {
+__device__ __noinline__ void muon_load(const MuonArgs &a, const MuonMat &t, int s_at, int64_t c0, int cols,
+                                       bool first) {
     constexpr int LD = MuonShape<RP>::LD;
+    float *s = muon_smem(s_at);
     if (a.r < RP)
         for (int e = threadIdx.x; e < cols * (RP - a.r); e += kMuonThreads)
             s[e / (RP - a.r) * LD + a.r + e % (RP - a.r)] = 0.f;
-    muon_elements<RP>(t, a.r, c0, cols, [&](int64_t at, int c, int k) {
-        const float g = __ldg(t.g + at);
-        float m = t.m[at];
-        if (first) {
-            m = fmaf(a.mu, m, g);
-            t.m[at] = m;
-        }
-        s[c * LD + k] = a.nesterov ? fmaf(a.mu, m, g) : m;
-    });
+    if (t.vec) muon_load_as<RP, true>(a, t, s, c0, cols, first);
+    else muon_load_as<RP, false>(a, t, s, c0, cols, first);
 }
 
-// acc += the tile's columns' part of X X^T, this thread's 4 x TJ elements and its
-// share of the columns.
+// p <- keep p - step X for the columns, and the bf16 copy.
+template <int RP, bool V4>
+__device__ __forceinline__ void muon_update_as(const MuonArgs &a, const MuonMat &t, const float *s, int64_t c0,
+                                               int cols) {
+    constexpr int LD = MuonShape<RP>::LD, W = V4 ? 4 : 1, U = V4 ? 5 : 6;
+    const int64_t o = muon_origin(t, a.r, c0);
+    float *pp = t.p + o;
+    __nv_bfloat16 *ph = t.p16 ? t.p16 + o : nullptr;
+    float p[U][W];
+    muon_items<RP, U, V4>(
+        t, a.r, a.inv_r, cols,
+        [&](int u, uint32_t at) {
+            if constexpr (V4) {
+                const float4 x = *reinterpret_cast<const float4 *>(pp + at);
+                p[u][0] = x.x; p[u][1] = x.y; p[u][2] = x.z; p[u][3] = x.w;
+            } else {
+                p[u][0] = pp[at];
+            }
+        },
+        [&](int u, uint32_t at, int so) {
+            float x[W];
+            if (V4 && t.tall) {
+                const float4 q = *reinterpret_cast<const float4 *>(s + so);
+                x[0] = q.x; x[W / 4] = q.y; x[W / 2] = q.z; x[W - 1] = q.w;
+            } else {
+#pragma unroll
+                for (int w = 0; w < W; ++w) x[w] = s[so + w * LD];
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) p[u][w] = fmaf(-t.step, x[w], p[u][w] * a.keep);
+            if constexpr (V4) {
+                *reinterpret_cast<float4 *>(pp + at) = make_float4(p[u][0], p[u][1], p[u][2], p[u][3]);
+                if (ph) {
+                    __nv_bfloat162 h[2] = {__floats2bfloat162_rn(p[u][0], p[u][1]),
+                                           __floats2bfloat162_rn(p[u][2], p[u][3])};
+                    *reinterpret_cast<uint2 *>(ph + at) = *reinterpret_cast<uint2 *>(h);
+                }
+            } else {
+                pp[at] = p[u][0];
+                if (ph) ph[at] = __float2bfloat16_rn(p[u][0]);
+            }
+        });
+}
+
+template <int RP>
+__device__ __noinline__ void muon_update(const MuonArgs &a, const MuonMat &t, int s_at, int64_t c0, int cols) {
+    if (t.vec) muon_update_as<RP, true>(a, t, muon_smem(s_at), c0, cols);
+    else muon_update_as<RP, false>(a, t, muon_smem(s_at), c0, cols);
+}
+
+// acc += the columns' part of X X^T, this thread's 4 x TJ elements and its share of the
+// columns.
 template <int RP>
 __device__ __forceinline__ void muon_gram(const float *s, int cols, float (&acc)[4][MuonShape<RP>::TJ]) {
     using S = MuonShape<RP>;
-    const int tile = threadIdx.x % S::kTiles, sub = threadIdx.x / S::kTiles;
-    const int i0 = tile / (RP / S::TJ) * 4, j0 = tile % (RP / S::TJ) * 4;
-#pragma unroll 4
+    const int sub = threadIdx.x / S::kTiles;
+    if (sub >= S::kSubs) return;
+    int i0, j0;
+    S::tile(threadIdx.x % S::kTiles, i0, j0);
+#pragma unroll 2
     for (int c = sub; c < cols; c += S::kSubs) {
         const float4 x = *reinterpret_cast<const float4 *>(s + c * S::LD + i0);
         const float xv[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int h = 0; h < S::TJ / 4; ++h) {  // columns j0 .. + 3 and, at TJ 8, j0 + RP / 2 ..
-            const float4 y = *reinterpret_cast<const float4 *>(s + c * S::LD + j0 + h * (RP / 2));
+        for (int h = 0; h < S::TJ / 4; ++h) {
+            const float4 y = *reinterpret_cast<const float4 *>(s + c * S::LD + j0 + 4 * h);
             const float yv[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -158,148 +335,208 @@ __device__ __forceinline__ void muon_gram(const float *s, int cols, float (&acc)
     }
 }
 
-// The cluster's Gram matrix into G of every CTA, from the threads' shares.
+// The cluster's Gram matrix into G of every CTA, from the threads' shares (exchanges n and
+// n + 1).  `part`: RP x RP floats, `recv`: kRecv.
 template <int RP>
 __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP>::TJ], float *scratch, float *part,
-                                              float *G, int cluster, int rank) {
+                                              float *recv, float *G, const MuonLink &link, uint32_t n) {
     using S = MuonShape<RP>;
-    const int tile = threadIdx.x % S::kTiles, sub = threadIdx.x / S::kTiles;
-    const int i0 = tile / (RP / S::TJ) * 4, j0 = tile % (RP / S::TJ) * 4;
+    constexpr int kVecs = S::kTiles * S::TJ;  // vectors of 4 of one set of tiles
+    const int sub = threadIdx.x / S::kTiles, tile = threadIdx.x % S::kTiles;
     __syncthreads();  // scratch aliases matrices that other threads may still read
+    if (sub < S::kSubs) {  // vector v of a tile at [v][tile]: neighbours write neighbours
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int h = 0; h < S::TJ / 4; ++h)
-            *reinterpret_cast<float4 *>(scratch + sub * RP * RP + (i0 + i) * RP + j0 + h * (RP / 2)) =
-                make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+            for (int h = 0; h < S::TJ / 4; ++h)
+                *reinterpret_cast<float4 *>(scratch + 4 * (sub * kVecs + (i * (S::TJ / 4) + h) * S::kTiles + tile)) =
+                    make_float4(acc[i][4 * h], acc[i][4 * h + 1], acc[i][4 * h + 2], acc[i][4 * h + 3]);
+    }
     __syncthreads();
-    for (int e = threadIdx.x; e < RP * RP / 4; e += kMuonThreads) {
+    for (int e = threadIdx.x; e < kVecs; e += kMuonThreads) {
         float4 v = *reinterpret_cast<const float4 *>(scratch + 4 * e);
-        for (int k = 1; k < S::kSubs; ++k)
-            v = add4(v, *reinterpret_cast<const float4 *>(scratch + k * RP * RP + 4 * e));
-        *reinterpret_cast<float4 *>(part + 4 * e) = v;
-    }
-    cluster_sync();  // every part is there (and nobody reads the aliased matrices)
-    const int rows = S::kSlabs ? RP / cluster : RP, outs = rows * RP / 4, subs = kMuonThreads / outs;
-    const int o = threadIdx.x / subs, q = threadIdx.x % subs;
-    const int i = (S::kSlabs ? rank * rows : 0) + o / (RP / 4), j = o % (RP / 4) * 4;
-    const uint32_t src = smem_u32(part + i * RP + j);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = q; c < cluster; c += subs) v = add4(v, ld_cluster_f4(mapa_shared(src, c)));
-    for (int s = 1; s < subs; s <<= 1) v = add4(v, shfl_xor4(v, s));
-    if constexpr (S::kSlabs) {
-        const uint32_t dst = smem_u32(G + i * S::LD + j);
-        for (int c = q; c < cluster; c += subs) st_cluster_f4(mapa_shared(dst, c), v);
-        cluster_sync();
-    } else {
-        if (q == 0) *reinterpret_cast<float4 *>(G + i * S::LD + j) = v;
-        __syncthreads();
-    }
-}
-
-// z = alpha x y (+ beta w) + diag I in every CTA, x and y symmetric and commuting, z
-// none of the others.
-template <int RP>
-__device__ __forceinline__ void muon_product(const float *x, const float *y, float *z, float alpha, const float *w,
-                                             float beta, float diag, int cluster, int rank) {
-    using S = MuonShape<RP>;
-    const int rows = S::kSlabs ? RP / cluster : RP, outs = rows * RP / 4, subs = kMuonThreads / outs;
-    const int o = threadIdx.x / subs, q = threadIdx.x % subs;
-    const int i = (S::kSlabs ? rank * rows : 0) + o / (RP / 4), j = o % (RP / 4) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int k = q; k < RP; k += subs) {
-        const float xv = x[i * S::LD + k];
-        const float4 yv = *reinterpret_cast<const float4 *>(y + k * S::LD + j);
-        v.x = fmaf(xv, yv.x, v.x); v.y = fmaf(xv, yv.y, v.y);
-        v.z = fmaf(xv, yv.z, v.z); v.w = fmaf(xv, yv.w, v.w);
-    }
-    for (int s = 1; s < subs; s <<= 1) v = add4(v, shfl_xor4(v, s));
-    v.x *= alpha; v.y *= alpha; v.z *= alpha; v.w *= alpha;
-    if (w) {
-        const float4 u = *reinterpret_cast<const float4 *>(w + i * S::LD + j);
-        v.x = fmaf(beta, u.x, v.x); v.y = fmaf(beta, u.y, v.y);
-        v.z = fmaf(beta, u.z, v.z); v.w = fmaf(beta, u.w, v.w);
-    }
-    if (i == j) v.x += diag;
-    if (i == j + 1) v.y += diag;
-    if (i == j + 2) v.z += diag;
-    if (i == j + 3) v.w += diag;
-    if constexpr (S::kSlabs) {
-        const uint32_t dst = smem_u32(z + i * S::LD + j);
-        for (int c = q; c < cluster; c += subs) st_cluster_f4(mapa_shared(dst, c), v);
-        cluster_sync();
-    } else {
-        if (q == 0) *reinterpret_cast<float4 *>(z + i * S::LD + j) = v;
-        __syncthreads();
-    }
-}
-
-// X <- P X for a tile, in place.
-template <int RP>
-__device__ __forceinline__ void muon_apply(float *s, const float *P, int cols) {
-    using S = MuonShape<RP>;
-    const int cl = threadIdx.x % S::CL, i0 = threadIdx.x / S::CL * 4;
-    float acc[S::NC][4] = {};
 #pragma unroll 4
-    for (int k = 0; k < RP; k += 4) {
-        float pv[4][4];
+        for (int k = 1; k < S::kSubs; ++k) v = add4(v, *reinterpret_cast<const float4 *>(scratch + 4 * (k * kVecs + e)));
+        int i, j;
+        S::tile(e % S::kTiles, i, j);
+        const int at = e / S::kTiles;
+        i += at / (S::TJ / 4);
+        j += at % (S::TJ / 4) * 4;
+        *reinterpret_cast<float4 *>(part + i * RP + j) = v;
+        if (RP > 32 && i < 32 && j >= 32) {
+            part[j * RP + i] = v.x;
+            part[(j + 1) * RP + i] = v.y;
+            part[(j + 2) * RP + i] = v.z;
+            part[(j + 3) * RP + i] = v.w;
+        }
+    }
+    fence_proxy_async_smem();
+    __syncthreads();
+    const int cluster = link.cluster, rank = link.rank;
+    const int r0 = muon_row(RP, rank, cluster), r1 = muon_row(RP, rank + 1, cluster), rows = r1 - r0;
+    // every CTA's rows of this one's Gram matrix to it: place `rank` of its recv
+    if (threadIdx.x == 0) link.expect(n, (uint32_t)((cluster - 1) * rows * RP * 4));
+    if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank) {
+        const int o0 = muon_row(RP, threadIdx.x, cluster), o = muon_row(RP, threadIdx.x + 1, cluster) - o0;
+        if (o > 0)
+            link.send(n, smem_u32(recv + rank * o * RP), smem_u32(part + o0 * RP), (uint32_t)(o * RP * 4), threadIdx.x);
+    }
+    link.receive(n);
+    for (int e = threadIdx.x; e < rows * RP / 4; e += kMuonThreads) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < cluster; ++c)
+            v = add4(v, *reinterpret_cast<const float4 *>(c == rank ? part + r0 * RP + 4 * e
+                                                                   : recv + c * rows * RP + 4 * e));
+        *reinterpret_cast<float4 *>(G + (r0 + e / (RP / 4)) * S::LD + e % (RP / 4) * 4) = v;
+    }
+    link.share<S::LD>(n + 1, G, r0, r1, RP);
+}
+
+// z = alpha x y (+ beta w, w_at >= 0) + diag I in every CTA, x and y symmetric and
+// commuting, z none of the others (exchange n where the CTAs form slabs of it).
+template <int RP>
+__device__ __noinline__ void muon_product(int x_at, int y_at, int z_at, float alpha, int w_at, float beta, float diag,
+                                          const MuonLink &link, uint32_t n) {
+    using S = MuonShape<RP>;
+    const float *x = muon_smem(x_at), *y = muon_smem(y_at), *w = w_at < 0 ? nullptr : muon_smem(w_at);
+    float *z = muon_smem(z_at);
+    const int r0 = S::kSlabs ? muon_row(RP, link.rank, link.cluster) : 0,
+              r1 = S::kSlabs ? muon_row(RP, link.rank + 1, link.cluster) : RP;
+    // threads per vector of 4 results: all of them, as far as a power of two allows
+    const int subs = RP == 16 ? 8 : RP == 32 ? 2 : link.cluster >= 8 ? 4 : 2;
+    const int o = threadIdx.x / subs, q = threadIdx.x % subs;
+    const int i = r0 + o / (RP / 4), j = o % (RP / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < r1) {
+#pragma unroll 8
+        for (int k = q; k < RP; k += subs) {
+            const float xv = x[i * S::LD + k];
+            const float4 yv = *reinterpret_cast<const float4 *>(y + k * S::LD + j);
+            v.x = fmaf(xv, yv.x, v.x); v.y = fmaf(xv, yv.y, v.y);
+            v.z = fmaf(xv, yv.z, v.z); v.w = fmaf(xv, yv.w, v.w);
+        }
+    }
+    for (int s = 1; s < subs; s <<= 1) v = add4(v, shfl_xor4(v, s));
+    if (i < r1 && q == 0) {
+        v.x *= alpha; v.y *= alpha; v.z *= alpha; v.w *= alpha;
+        if (w) {
+            const float4 u = *reinterpret_cast<const float4 *>(w + i * S::LD + j);
+            v.x = fmaf(beta, u.x, v.x); v.y = fmaf(beta, u.y, v.y);
+            v.z = fmaf(beta, u.z, v.z); v.w = fmaf(beta, u.w, v.w);
+        }
+        if (i == j) v.x += diag;
+        if (i == j + 1) v.y += diag;
+        if (i == j + 2) v.z += diag;
+        if (i == j + 3) v.w += diag;
+        *reinterpret_cast<float4 *>(z + i * S::LD + j) = v;
+    }
+    if constexpr (S::kSlabs) link.share<S::LD>(n, z, r0, r1, RP);
+    else __syncthreads();
+}
+
+// X <- P X for NC x CL columns (`left` of them, more than (NC - 1) x CL), in place.
+template <int RP, int NC>
+__device__ __forceinline__ void muon_apply_columns(float *s, const float *P, int left) {
+    using S = MuonShape<RP>;
+    const int cl = threadIdx.x % S::CL, i0 = threadIdx.x / S::CL * 8;
+    float acc[NC][8] = {};
+    const float *p0 = P + i0, *x0 = s + cl * S::LD;
+    // only the last of a thread's columns may lie past `left`: it then reads column 0
+    const int last = cl + (NC - 1) * S::CL < left ? (NC - 1) * S::CL * S::LD : -cl * S::LD;
+#pragma unroll 1
+    for (int k = 0; k < RP; k += 4, p0 += 4 * S::LD, x0 += 4) {
+        float4 x[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+            x[n] = *reinterpret_cast<const float4 *>(x0 + (n == NC - 1 ? last : n * S::CL * S::LD));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float4 p = *reinterpret_cast<const float4 *>(P + (k + e) * S::LD + i0);
-            pv[e][0] = p.x; pv[e][1] = p.y; pv[e][2] = p.z; pv[e][3] = p.w;
-        }
+            const float4 p = *reinterpret_cast<const float4 *>(p0 + e * S::LD);
+            const float4 q = *reinterpret_cast<const float4 *>(p0 + e * S::LD + 4);
 #pragma unroll
-        for (int n = 0; n < S::NC; ++n) {
-            if (n * S::CL >= cols) break;  // block-uniform; rows past cols within are never read back
-            const float4 x = *reinterpret_cast<const float4 *>(s + (cl + n * S::CL) * S::LD + k);
-            const float xv[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[n][i] = fmaf(xv[e], pv[e][i], acc[n][i]);
+            for (int n = 0; n < NC; ++n) {
+                const float v = e == 0 ? x[n].x : e == 1 ? x[n].y : e == 2 ? x[n].z : x[n].w;
+                acc[n][0] = fmaf(v, p.x, acc[n][0]); acc[n][1] = fmaf(v, p.y, acc[n][1]);
+                acc[n][2] = fmaf(v, p.z, acc[n][2]); acc[n][3] = fmaf(v, p.w, acc[n][3]);
+                acc[n][4] = fmaf(v, q.x, acc[n][4]); acc[n][5] = fmaf(v, q.y, acc[n][5]);
+                acc[n][6] = fmaf(v, q.z, acc[n][6]); acc[n][7] = fmaf(v, q.w, acc[n][7]);
+            }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < S::NC; ++n)
-        if (cl + n * S::CL < cols)
-            *reinterpret_cast<float4 *>(s + (cl + n * S::CL) * S::LD + i0) =
-                make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
-    __syncthreads();
+    for (int n = 0; n < NC; ++n)
+        if (cl + n * S::CL < left) {
+            float *to = s + (cl + n * S::CL) * S::LD + i0;
+            *reinterpret_cast<float4 *>(to) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+            *reinterpret_cast<float4 *>(to + 4) = make_float4(acc[n][4], acc[n][5], acc[n][6], acc[n][7]);
+        }
 }
 
 template <int RP>
+__device__ __noinline__ void muon_apply(int s_at, int p_at, int cols) {
+    using S = MuonShape<RP>;
+    float *s = muon_smem(s_at);
+    const float *P = muon_smem(p_at);
+    while (cols > 0) {  // even passes of at most 4 x CL columns
+        const int units = (cols + S::CL - 1) / S::CL, passes = (units + 3) / 4, nc = (units + passes - 1) / passes;
+        const int now = min(cols, nc * S::CL);
+        if (nc == 4) muon_apply_columns<RP, 4>(s, P, now);
+        else if (nc == 3) muon_apply_columns<RP, 3>(s, P, now);
+        else if (nc == 2) muon_apply_columns<RP, 2>(s, P, now);
+        else muon_apply_columns<RP, 1>(s, P, now);
+        s += now * S::LD;
+        cols -= now;
+    }
+    __syncthreads();
+}
+
+// STREAM: columns of a CTA may exceed what its shared memory holds.
+template <int RP, bool STREAM>
 __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_constant__ MuonArgs a) {
     using S = MuonShape<RP>;
-    extern __shared__ float4 s_raw[];
-    float *G = reinterpret_cast<float *>(s_raw), *B = G + S::kMat, *T = B + S::kMat, *part = G + S::kFirst;
-    float *tiles = G + S::kFixed;
+    constexpr int oG = 0, oB = S::kMat, oT = 2 * S::kMat, oX = S::kFixed;
+    float *const G = muon_smem(oG), *const B = muon_smem(oB), *const part = muon_smem(S::kFirst),
+          *const recv = part + RP * RP, *const X = muon_smem(oX);
     __shared__ float s_scale;
+    __shared__ __align__(8) uint64_t s_bars[2];
+    __shared__ int s_abort;
     const int rank = (int)cluster_ctarank();
     const MuonMat &t = a.mat[blockIdx.x / a.cluster];
     const int64_t c_begin = rank * t.per, c_end = min(t.n, c_begin + t.per);
-    const int ntiles = c_end > c_begin ? (int)((c_end - c_begin + kMuonCols - 1) / kMuonCols) : 0;
-    const int resident = ntiles <= a.slots ? ntiles : a.slots - 1;
-    auto place = [&](int q) { return tiles + (q < resident ? q : a.slots - 1) * S::kTile; };
-    auto first_col = [&](int q) { return c_begin + (int64_t)q * kMuonCols; };
-    auto columns = [&](int q) { return (int)min((int64_t)kMuonCols, c_end - first_col(q)); };
+    const int64_t cols = c_end > c_begin ? c_end - c_begin : 0;
+    // the first columns stay; the others pass through the last kMuonStage places
+    const int stay = (int)(!STREAM || cols <= a.room ? cols : a.room - kMuonStage);
+    const int o_stage = oX + (a.room - kMuonStage) * S::LD;
+    float *const stage = muon_smem(o_stage);
+    const MuonLink link{smem_u32(s_bars), a.cluster, rank, &s_abort, a.status};
+    uint32_t n = 0;  // exchanges so far
+    if (threadIdx.x == 0) {
+        mbar_init(link.bar0, 1);
+        mbar_init(link.bar0 + 8u, 1);
+        s_abort = 0;
+        fence_mbar_init();
+    }
+    muon_load<RP>(a, t, oX, c_begin, stay, true);
+    cluster_sync();  // X is there, and the barriers of all CTAs
 
     float acc[4][S::TJ] = {};
-    for (int q = 0; q < ntiles; ++q) {
-        if (q >= resident) __syncthreads();  // the place's last tile has been read
-        muon_load<RP>(a, t, place(q), first_col(q), columns(q), true);
-        if (q >= resident) {
+    muon_gram<RP>(X, stay, acc);
+    if constexpr (STREAM) {
+        for (int64_t c = stay; c < cols; c += kMuonStage) {
+            const int now = (int)min((int64_t)kMuonStage, cols - c);
+            muon_load<RP>(a, t, o_stage, c_begin + c, now, true);
             __syncthreads();
-            muon_gram<RP>(place(q), columns(q), acc);
+            muon_gram<RP>(stage, now, acc);
+            __syncthreads();
         }
     }
-    __syncthreads();
-    for (int q = 0; q < resident; ++q) muon_gram<RP>(place(q), columns(q), acc);
 
     const int groups = (a.steps + 1) / 2, single = a.steps % 2 ? groups / 2 : -1;  // pairs, the odd step amidst them
     for (int gi = 0; gi < groups; ++gi) {
-        muon_gram_sum<RP>(acc, G, part + gi % S::kParts * RP * RP, G, a.cluster, rank);
+        muon_gram_sum<RP>(acc, G, part, recv, G, link, n);
+        n += 2;
         float scale = 1.f;
         if (gi == 0) {
             if (threadIdx.x < 32) {
@@ -317,55 +554,51 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
             __syncthreads();
         }
         // B = a I + b G + c G^2, and for a pair of steps G <- B G B, P = (a I + b G + c G^2) B
-        const float *P = B;
-        muon_product<RP>(G, G, B, kNsC, G, kNsB, kNsA, a.cluster, rank);
+        int oP = oB;
+        muon_product<RP>(oG, oG, oB, kNsC, oG, kNsB, kNsA, link, n++);
         if (gi != single) {
-            muon_product<RP>(B, G, T, 1.f, nullptr, 0.f, 0.f, a.cluster, rank);
-            muon_product<RP>(T, B, G, 1.f, nullptr, 0.f, 0.f, a.cluster, rank);
-            muon_product<RP>(G, G, T, kNsC, G, kNsB, kNsA, a.cluster, rank);
-            muon_product<RP>(T, B, G, scale, nullptr, 0.f, 0.f, a.cluster, rank);
-            P = G;
+            muon_product<RP>(oB, oG, oT, 1.f, -1, 0.f, 0.f, link, n++);
+            muon_product<RP>(oT, oB, oG, 1.f, -1, 0.f, 0.f, link, n++);
+            muon_product<RP>(oG, oG, oT, kNsC, oG, kNsB, kNsA, link, n++);
+            muon_product<RP>(oT, oB, oG, scale, -1, 0.f, 0.f, link, n++);
+            oP = oG;
         } else if (gi == 0) {
             for (int e = threadIdx.x; e < RP * RP; e += kMuonThreads) B[e / RP * S::LD + e % RP] *= scale;
             __syncthreads();
         }
+        if constexpr (!S::kSlabs) n = 2 * (gi + 1);  // the products were no exchanges
+        const bool last = gi + 1 == groups;
+        muon_apply<RP>(oX, oP, stay);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < S::TJ; ++j) acc[i][j] = 0.f;
-        const bool last = gi + 1 == groups;
-        for (int q = 0; q < ntiles; ++q) {
-            float *s = place(q);
-            const int64_t c0 = first_col(q);
-            const int cols = columns(q);
-            if (q >= resident) {
-                __syncthreads();
+        if (last) muon_update<RP>(a, t, oX, c_begin, stay);
+        else muon_gram<RP>(X, stay, acc);
+        if constexpr (STREAM) {
+            for (int64_t c = stay; c < cols; c += kMuonStage) {
+                const int now = (int)min((int64_t)kMuonStage, cols - c);
+                float4 *x = reinterpret_cast<float4 *>(t.x + (c_begin + c) * RP);
                 if (gi == 0) {
-                    muon_load<RP>(a, t, s, c0, cols, false);
+                    muon_load<RP>(a, t, o_stage, c_begin + c, now, false);
                 } else {
-                    for (int e = threadIdx.x; e < cols * (RP / 4); e += kMuonThreads)
-                        *reinterpret_cast<float4 *>(s + e / (RP / 4) * S::LD + e % (RP / 4) * 4) =
-                            __ldcg(reinterpret_cast<const float4 *>(t.x + c0 * RP) + e);
+                    for (int e = threadIdx.x; e < now * (RP / 4); e += kMuonThreads)
+                        *reinterpret_cast<float4 *>(stage + e / (RP / 4) * S::LD + e % (RP / 4) * 4) = __ldcg(x + e);
+                }
+                __syncthreads();
+                muon_apply<RP>(o_stage, oP, now);
+                if (last) {
+                    muon_update<RP>(a, t, o_stage, c_begin + c, now);
+                } else {
+                    muon_gram<RP>(stage, now, acc);
+                    for (int e = threadIdx.x; e < now * (RP / 4); e += kMuonThreads)
+                        __stcg(x + e, *reinterpret_cast<const float4 *>(stage + e / (RP / 4) * S::LD + e % (RP / 4) * 4));
                 }
                 __syncthreads();
             }
-            muon_apply<RP>(s, P, cols);
-            if (last) {
-                muon_elements<RP>(t, a.r, c0, cols, [&](int64_t at, int c, int k) {
-                    const float p = fmaf(-t.step, s[c * S::LD + k], t.p[at] * a.keep);
-                    t.p[at] = p;
-                    if (t.p16) t.p16[at] = __float2bfloat16_rn(p);
-                });
-            } else {
-                muon_gram<RP>(s, cols, acc);
-                if (q >= resident)
-                    for (int e = threadIdx.x; e < cols * (RP / 4); e += kMuonThreads)
-                        __stcg(reinterpret_cast<float4 *>(t.x + c0 * RP) + e,
-                               *reinterpret_cast<const float4 *>(s + e / (RP / 4) * S::LD + e % (RP / 4) * 4));
-            }
         }
     }
-    cluster_sync();  // no CTA leaves while another reads its part
+    cluster_sync();  // no CTA leaves while it is sent to
 }
 
 static int muon_rp(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
@@ -380,7 +613,42 @@ static int64_t muon_columns(int nproj, const int64_t *din, const int64_t *dout) 
 static bool muon_sizes(int nproj, const int64_t *din, const int64_t *dout, int r) {
     if (nproj < 1 || nproj > kMuonMats / 2 || !din || !dout || r < 1 || r > 64) return false;
     for (int i = 0; i < nproj; ++i)
-        if (din[i] < 1 || dout[i] < 1 || din[i] > (1ll << 31) || dout[i] > (1ll << 31)) return false;
+        if (din[i] < 1 || dout[i] < 1 || din[i] > (1ll << 25) || dout[i] > (1ll << 25)) return false;
+    return true;
+}
+
+// Clusters of each size that the device runs at once (0: none), for one kernel (and a
+// second one of the same kind) with one amount of shared memory, asked once per device.
+static bool muon_clusters(const void *kern, const void *other, size_t smem, int dev,
+                          int (&most)[kMuonMaxCluster + 1]) {
+    static std::mutex mu;
+    static std::map<std::pair<const void *, int>, std::array<int, kMuonMaxCluster + 1>> known;
+    std::lock_guard<std::mutex> lock(mu);
+    const auto key = std::make_pair(kern, dev);
+    auto it = known.find(key);
+    if (it == known.end()) {
+        for (const void *k : {kern, other})
+            if (cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+        std::array<int, kMuonMaxCluster + 1> n{};
+        for (int c = 4; c <= kMuonMaxCluster; ++c) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(kMuonMats * c));
+            cfg.blockDim = dim3(kMuonThreads);
+            cfg.dynamicSmemBytes = smem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = (unsigned)c;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&n[c], kern, &cfg) != cudaSuccess) {
+                n[c] = 0;
+                (void)cudaGetLastError();
+            }
+        }
+        it = known.emplace(key, n).first;
+    }
+    std::copy(it->second.begin(), it->second.end(), most);
     return true;
 }
 
@@ -388,17 +656,30 @@ template <int RP>
 static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) {
     using S = MuonShape<RP>;
     constexpr size_t kMax = 232448 - 1024;  // 227 KB opt-in less the static part
-    const void *kern = reinterpret_cast<const void *>(muon_kernel<RP>);
-    const int most = (int)((kMax - sizeof(float) * S::kFixed) / (sizeof(float) * S::kTile));
-    a.cluster = 8;
-    int64_t per = 0;
-    for (int i = 0; i < nmat; ++i) {
-        a.mat[i].per = round_up(cdiv(a.mat[i].n, a.cluster), 8);
-        per = std::max(per, a.mat[i].per);
+    const void *kern = reinterpret_cast<const void *>(muon_kernel<RP, false>);
+    const void *stream_kern = reinterpret_cast<const void *>(muon_kernel<RP, true>);
+    a.room = (int)((kMax - sizeof(float) * S::kFixed) / (sizeof(float) * S::LD)) / 8 * 8;
+    const size_t smem = sizeof(float) * (S::kFixed + (size_t)a.room * S::LD);
+    int most[kMuonMaxCluster + 1];
+    if (!set_smem_limit(kern, smem, dev) || !set_smem_limit(stream_kern, smem, dev) ||
+        !muon_clusters(kern, stream_kern, smem, dev, most))
+        return ATTT_ERR_CUDA;
+    // The CTAs of a cluster: as many as leave the fewest columns for a CTA in all the
+    // rounds that the clusters take (a part with 15 clusters of 8, 8 of 12 and 7 of 16
+    // takes 12 for 8 matrices and 8 for 14).
+    int64_t n = 0;
+    for (int i = 0; i < nmat; ++i) n = std::max(n, a.mat[i].n);
+    int64_t best = INT64_MAX;
+    for (int c = 4; c <= kMuonMaxCluster; ++c) {
+        if (most[c] < 1) continue;
+        const int64_t cost = cdiv(nmat, most[c]) * round_up(cdiv(n, c), 8);
+        if (cost < best) {
+            best = cost;
+            a.cluster = c;
+        }
     }
-    a.slots = (int)std::min<int64_t>(most, cdiv(per, kMuonCols));
-    const size_t smem = sizeof(float) * (S::kFixed + (size_t)a.slots * S::kTile);
-    if (!set_smem_limit(kern, smem, dev)) return ATTT_ERR_CUDA;
+    if (best == INT64_MAX) return ATTT_ERR_CUDA;
+    for (int i = 0; i < nmat; ++i) a.mat[i].per = round_up(cdiv(a.mat[i].n, a.cluster), 8);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(nmat * a.cluster));
     cfg.blockDim = dim3(kMuonThreads);
@@ -411,7 +692,10 @@ static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) 
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, muon_kernel<RP>, a) != cudaSuccess) return ATTT_ERR_CUDA;
+    const bool all = round_up(cdiv(n, a.cluster), 8) <= a.room;
+    if ((all ? cudaLaunchKernelEx(&cfg, muon_kernel<RP, false>, a)
+             : cudaLaunchKernelEx(&cfg, muon_kernel<RP, true>, a)) != cudaSuccess)
+        return ATTT_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
 }
@@ -446,7 +730,10 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
     const attt_status st = current_device(&dev);
     if (st != ATTT_OK) return st;
     MuonArgs a{};
+    int *status = device_status_word(dev);
+    if (!status) return ATTT_ERR_CUDA;
     a.r = r; a.nesterov = nesterov ? 1 : 0; a.steps = ns_steps;
+    a.inv_r = r > 1 ? (uint32_t)(((1ull << 32) + r - 1) / r) : 0u; a.status = status;
     a.mu = momentum; a.keep = (float)(1.0 - (double)lr * weight_decay); a.eps = eps;
     float *x = static_cast<float *>(d_ws);
     for (int i = 0; i < 2 * nproj; ++i) {
@@ -459,6 +746,8 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
         attt_bf16 *const *h = t.tall ? d_A16 : d_B16;
         t.p16 = h ? reinterpret_cast<__nv_bfloat16 *>(h[p]) : nullptr;
         t.n = t.tall ? din[p] : dout[p];
+        t.vec = (t.tall ? r : t.n) % 4 == 0 && aligned16(t.p) && aligned16(t.g) && aligned16(t.m) &&
+                reinterpret_cast<uintptr_t>(t.p16) % 8 == 0;
         t.x = x;
         x += t.n * muon_rp(r);
         t.step = (float)((double)lr * rms * std::sqrt((double)std::max<int64_t>(t.n, r)));
