@@ -31,7 +31,7 @@ struct GemmProblem {
     bool pdl = false;
     bool operands_ready = false;
     bool second_waits = false;  // with operands_ready: A2 and B2 do come from it
-    // Tail split (EPI_F32_ACC): workspace for up to `split_regions` partials
+    // Tail split (EPI_F32_ACC, EPI_BF16): workspace for up to `split_regions` partials
     // of 128 x BN fp32 and as many arrival counters (zero on entry).
     float *split_ws = nullptr;
     unsigned int *split_tick = nullptr;
@@ -273,7 +273,7 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
         g.whole_tiles = 0;
         g.tail_s = p.pieces;
     }
-    if (EPI == EPI_F32_ACC && p.split_ws && p.split_tick && p.BN % 32 == 0) {
+    if ((EPI == EPI_F32_ACC || EPI == EPI_BF16) && p.split_ws && p.split_tick && p.BN % 32 == 0) {
         const int s = tail_pieces(tiles, units, g.kb_total, p.pair ? 2 : 1, p.split_regions);
         if (s > 1) {
             g.tail_s = s;

@@ -674,6 +674,7 @@ struct GradLayout {
     int regions;
     __nv_bfloat16 *G;
     float *split_ws;
+    unsigned int *split_tick;
     size_t bytes;
 };
 
@@ -686,6 +687,7 @@ static GradLayout grad_layout(void *ws, int64_t L, int64_t d, int64_t V) {
     Carve cv{static_cast<char *>(ws), 0};
     c.G = cv.take<__nv_bfloat16>((size_t)(c.rows * c.ld));
     c.split_ws = cv.take<float>((size_t)c.regions * 128 * 256);
+    c.split_tick = cv.take<unsigned int>((size_t)c.regions);
     c.bytes = (size_t)round_up((int64_t)cv.used, 256);
     return c;
 }
@@ -806,6 +808,11 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
     const int sets = lp_sets(d);
     for (int64_t r0 = 0; r0 < L; r0 += c.rows) {
         const int64_t R = L - r0 < c.rows ? L - r0 : c.rows;
+        const TilePlan td = plan_tiles(R, d, c.ld / 64, num_sms(dev), c.regions, true, true);
+        // whole tiles: the last wave's may be cut, with arrival counters that start at 0
+        if (td.pieces == 1 &&
+            cudaMemsetAsync(c.split_tick, 0, sizeof(unsigned int) * (size_t)c.regions, stream) != cudaSuccess)
+            return ATTT_ERR_CUDA;
         {   // G from the logits
             const TilePlan t = plan_tiles(R, V, cdiv(d, 64), num_sms(dev), 0, false, false);
             GemmProblem p{};
@@ -827,11 +834,10 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             p.b = d_W; p.b_rows_ld = d; p.b_rows = d; p.b_k = V;
             p.M = (int)R; p.N = (int)d; p.K = (int)c.ld;
             p.pdl = true;
-            p.split_ws = c.split_ws; p.split_regions = c.regions;
+            p.split_ws = c.split_ws; p.split_tick = c.split_tick; p.split_regions = c.regions;
             EpiParams ep{};
             ep.out16 = reinterpret_cast<__nv_bfloat16 *>(d_dh) + r0 * d; ep.out_ld = d; ep.alpha = 1.0f;
-            const TilePlan t = plan_tiles(R, d, c.ld / 64, num_sms(dev), c.regions, false, true);
-            st = launch_planned<true, false, true>(p, ep, t, dev, stream);
+            st = launch_planned<true, false, true>(p, ep, td, dev, stream);
             if (st != ATTT_OK) return st;
         }
     }

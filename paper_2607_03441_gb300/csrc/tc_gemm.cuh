@@ -19,7 +19,7 @@
 // loaded by TMA with the 128-byte swizzle that tcgen05 reads natively.
 // Tiles past M, N or K are zero-filled by TMA and masked in the epilogue.
 // When the tiles do not fill the last wave, the tiles of that wave may be
-// cut into K pieces spread over the idle SMs (EPI_F32_ACC): each piece
+// cut into K pieces spread over the idle SMs (EPI_F32_ACC, EPI_BF16): each piece
 // stores an fp32 partial and the last piece to arrive sums them in piece
 // order, so the result does not depend on which piece finishes last.  When
 // all tiles together leave most SMs idle, every tile is cut (EPI_F32_PART)
@@ -370,14 +370,16 @@ __device__ __forceinline__ void f32_part_store(const GemmArgs &g, const CUtensor
 
 // EPI_BF16 for this warp's 32 rows (from y; lane = row): out16 = bf16(alpha
 // acc) for the tile's columns [n_base, n_end), box by box through the warp's
-// staging buffers; the running box count `ec` picks the buffer.
+// staging buffers; the running box count `ec` picks the buffer.  src(c, v) gives the
+// lane's values of columns n_base + c .. + 31.
+template <class Src>
 __device__ __forceinline__ void bf16_tile_store(const GemmArgs &g, const CUtensorMap *tm, uint32_t sE, uint32_t &ec,
-                                                int lane, int y, int n_base, int n_end, uint32_t taddr) {
+                                                int lane, int y, int n_base, int n_end, Src &&src) {
     if (y >= g.M) return;  // every row of this warp lies past M (warp-uniform)
     for (int c = 0; c < g.BN; c += 32) {
         if (n_base + c >= n_end) break;
         float v[32];
-        tmem_ld_x32(taddr + (uint32_t)c, v);
+        src(c, v);
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
@@ -775,15 +777,14 @@ __device__ __forceinline__ void epilogue_kl(const GemmArgs &g, int gm_base, int 
     }
 }
 
-// EPI_F32_ACC for K piece k.piece of tail tile k.tail, on the 128 accumulator
-// rows this CTA holds (CTA `rank` of `nranks`).  The four epilogue warps store
-// the piece's partial (column-quad major: a warp writes 512 contiguous bytes
-// per store), then one thread takes a ticket; the piece that arrives last
-// forms the sum P_0 + P_1 + ... in piece order, its own term read back from
-// TMEM, and applies the epilogue to it.  BN is a multiple of 32.
-__device__ __forceinline__ void epilogue_piece_f32_acc(const GemmArgs &g, const Work &k, int gm_base, int rank,
-                                                      int nranks, int row, uint32_t taddr, const CUtensorMap *tm,
-                                                      F32Stage &st, volatile int *abort_flag) {
+// K piece k.piece of tail tile k.tail, on the 128 accumulator rows this CTA holds
+// (CTA `rank` of `nranks`).  The four epilogue warps store the piece's partial
+// (column-quad major: a warp writes 512 contiguous bytes per store), then one thread
+// takes a ticket; whether this piece is the one that arrived last, which forms the sum
+// P_0 + P_1 + ... in piece order (piece_sum) and applies the epilogue to it.  BN is a
+// multiple of 32.
+__device__ __forceinline__ bool piece_arrive(const GemmArgs &g, const Work &k, int rank, int nranks, int row,
+                                             uint32_t taddr) {
     const int BN = g.BN;
     const size_t region = (size_t)128 * (size_t)BN;
     const size_t slot0 = (size_t)k.tail * (size_t)g.tail_s;
@@ -804,31 +805,56 @@ __device__ __forceinline__ void epilogue_piece_f32_acc(const GemmArgs &g, const 
         if (last) atomicExch(tk, 0u);  // every piece has arrived: ready for the next launch
         __threadfence();
     }
-    if (!named_barrier_or(1, 128, last)) return;
+    return named_barrier_or(1, 128, last) != 0;
+}
 
+// The sum of a tail tile's pieces for this thread's row, columns c .. c + 31 of the tile; the
+// own piece is read back from TMEM.
+__device__ __forceinline__ void piece_sum(const GemmArgs &g, const Work &k, int rank, int nranks, int row,
+                                          uint32_t taddr, int c, float (&sm)[32]) {
+    const size_t region = (size_t)128 * (size_t)g.BN;
+    const size_t slot0 = (size_t)k.tail * (size_t)g.tail_s;
+    for (int j = 0; j < g.tail_s; ++j) {
+        float v[32];
+        if (j == k.piece) {
+            tmem_ld_x32(taddr + (uint32_t)c, v);
+        } else {
+            const float4 *src =
+                reinterpret_cast<const float4 *>(g.split_ws + ((slot0 + j) * nranks + rank) * region) + row;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float4 p = __ldcg(src + (size_t)(c / 4 + q) * 128);
+                v[4 * q] = p.x; v[4 * q + 1] = p.y; v[4 * q + 2] = p.z; v[4 * q + 3] = p.w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sm[i] = (j == 0) ? v[i] : sm[i] + v[i];
+    }
+}
+
+// EPI_F32_ACC for a K piece.
+__device__ __forceinline__ void epilogue_piece_f32_acc(const GemmArgs &g, const Work &k, int gm_base, int rank,
+                                                      int nranks, int row, uint32_t taddr, const CUtensorMap *tm,
+                                                      F32Stage &st, volatile int *abort_flag) {
+    if (!piece_arrive(g, k, rank, nranks, row, taddr)) return;
     const int gm = gm_base + row;
-    const int n_base = k.tn * BN;
+    const int n_base = k.tn * g.BN;
     const AccRow a = acc_row(g.ep, gm, gm < g.M);
-    f32_tile_store(g, tm, st, row & 31, gm - (row & 31), a, n_base, min(g.N, n_base + BN), abort_flag,
-                   [&](int c, float(&sm)[32]) {
-                       for (int j = 0; j < g.tail_s; ++j) {
-                           float v[32];
-                           if (j == k.piece) {
-                               tmem_ld_x32(taddr + (uint32_t)c, v);
-                           } else {
-                               const float4 *src = reinterpret_cast<const float4 *>(
-                                                       g.split_ws + ((slot0 + j) * nranks + rank) * region) +
-                                                   row;
-#pragma unroll
-                               for (int q = 0; q < 8; ++q) {
-                                   const float4 p = __ldcg(src + (size_t)(c / 4 + q) * 128);
-                                   v[4 * q] = p.x; v[4 * q + 1] = p.y; v[4 * q + 2] = p.z; v[4 * q + 3] = p.w;
-                               }
-                           }
-#pragma unroll
-                           for (int i = 0; i < 32; ++i) sm[i] = (j == 0) ? v[i] : sm[i] + v[i];
-                       }
-                   });
+    f32_tile_store(g, tm, st, row & 31, gm - (row & 31), a, n_base, min(g.N, n_base + g.BN), abort_flag,
+                   [&](int c, float(&sm)[32]) { piece_sum(g, k, rank, nranks, row, taddr, c, sm); });
+}
+
+// EPI_BF16 for this warp's 32 rows, a whole tile or a K piece.
+__device__ __forceinline__ void epilogue_bf16(const GemmArgs &g, const Work &k, int gm_base, int rank, int nranks,
+                                              int row, uint32_t taddr, const CUtensorMap *tm, uint32_t sE,
+                                              uint32_t &ec) {
+    const int lane = row & 31, y = gm_base + row - lane, n_base = k.tn * g.BN, n_end = min(g.N, n_base + g.BN);
+    if (k.piece < 0)
+        bf16_tile_store(g, tm, sE, ec, lane, y, n_base, n_end,
+                        [&](int c, float(&v)[32]) { tmem_ld_x32(taddr + (uint32_t)c, v); });
+    else if (piece_arrive(g, k, rank, nranks, row, taddr))
+        bf16_tile_store(g, tm, sE, ec, lane, y, n_base, n_end,
+                        [&](int c, float(&v)[32]) { piece_sum(g, k, rank, nranks, row, taddr, c, v); });
 }
 
 // ---------------------------------------------------------------------------
@@ -1037,9 +1063,7 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
                                    (int)part_row(wi.tm, wi.tn, g.tiles_m, wi.piece, g.tail_s, 128) + 32 * q,
                                    min(g.N - wi.tn * g.BN, g.BN), taddr);
             } else if constexpr (EPI == EPI_BF16) {
-                const int gm = wi.tm * 128 + row;
-                bf16_tile_store(g, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec, lane, gm - lane, wi.tn * g.BN,
-                                min(g.N, (wi.tn + 1) * g.BN), taddr);
+                epilogue_bf16(g, wi, wi.tm * 128, 0, 1, row, taddr, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else if constexpr (epi_logp(EPI)) {
                 epilogue_logp<epi_top(EPI), SETS>(g, wi.tm * 128 + row, wi.tn, set, taddr);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
@@ -1306,8 +1330,7 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
                                        32 * q,
                                    min(g.N - wi.tn * g.BN, g.BN), taddr);
             } else if constexpr (EPI == EPI_BF16) {
-                bf16_tile_store(g, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec, lane, gm_base + 32 * q,
-                                wi.tn * g.BN, min(g.N, (wi.tn + 1) * g.BN), taddr);
+                epilogue_bf16(g, wi, gm_base, (int)rank, 2, row, taddr, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else if constexpr (epi_logp(EPI)) {
                 epilogue_logp<epi_top(EPI), SETS>(g, gm_base + row, wi.tn, set, taddr);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
