@@ -35,37 +35,9 @@
 #include <mutex>
 #include <utility>
 
-#include "attt_common.cuh"
-#include "attt_host.h"
+#include "muon.cuh"
 
 namespace attt {
-
-constexpr int kMuonMats = 16;  // two per projection
-constexpr int kMuonThreads = 512;
-constexpr int kMuonStage = 128;  // columns of a tile that does not stay
-constexpr int kMuonMaxCluster = 16;
-constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
-
-struct MuonMat {
-    float *p, *m;
-    const float *g;
-    __nv_bfloat16 *p16;
-    float *x;    // [n][RP], columns that do not stay in shared memory
-    int64_t n;   // width beside r
-    int64_t per; // columns of a CTA, a multiple of 8
-    int tall;    // [n, r] (A), else [r, n] (B)
-    int vec;     // whether four neighbours in memory may move at once
-    float step;  // lr rms sqrt(max(rows, columns))
-};
-
-struct MuonArgs {
-    MuonMat mat[kMuonMats];
-    int r, nesterov, steps, cluster;
-    int room;        // columns that fit in shared memory
-    uint32_t inv_r;  // ceil(2^32 / r), r > 1: e / r is the high half of e inv_r for e < 2^26
-    float mu, keep, eps;  // keep = 1 - lr wd
-    int *status;
-};
 
 template <int RP>
 struct MuonShape {
@@ -84,7 +56,9 @@ struct MuonShape {
     static constexpr int kFirst = 3 * kMat > kScratch ? 3 * kMat : kScratch;
     // (cluster x rows of a slab, which are not even: up to RP + cluster rows)
     static constexpr int kRecv = (RP + kMuonMaxCluster) * RP;
-    static constexpr int kFixed = kFirst + RP * RP + kRecv;
+    // this CTA's slab of the sum, to be sent (G itself is written again at once)
+    static constexpr int kSlab = (RP / kMuonMinCluster) * LD;
+    static constexpr int kFixed = kFirst + RP * RP + kRecv + kSlab;
     // Row and column of a Gram tile's first element.
     __device__ static __forceinline__ void tile(int t, int &i0, int &j0) {
         if constexpr (RP > 32) {
@@ -98,54 +72,6 @@ struct MuonShape {
     }
 };
 
-// Rows [first, second) of an r x r matrix that CTA `rank` of `cluster` forms.
-__device__ __forceinline__ int muon_row(int RP, int rank, int cluster) { return rank * RP / cluster; }
-
-// Exchanges of the cluster: number `n` (0, 1, ..) is counted on barrier n & 1.  A CTA
-// sends for exchange n + 1 when it has all of exchange n, and so has nothing more to
-// read of what exchange n came from; what CTAs send for exchange n + 2 follows this
-// CTA's own data of n + 1.
-struct MuonLink {
-    uint32_t bar0;
-    int cluster, rank;
-    volatile int *abort_flag;
-    int *status;
-
-    // One thread: `bytes` will come in exchange n.
-    __device__ __forceinline__ void expect(uint32_t n, uint32_t bytes) const {
-        mbar_arrive_expect_tx(bar0 + 8u * (n & 1u), bytes);
-    }
-    // One thread per receiver: copies `bytes` of this CTA's shared memory to `dst` (an
-    // address of this CTA's own) in CTA `to`.
-    __device__ __forceinline__ void send(uint32_t n, uint32_t dst, uint32_t src, uint32_t bytes, int to) const {
-        asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                         mapa_shared(dst, to)),
-                     "r"(src), "r"(bytes), "r"(mapa_shared(bar0 + 8u * (n & 1u), to))
-                     : "memory");
-    }
-    // All threads: exchange n has arrived.  If it does not within the limit, the status word
-    // says so and the CTA goes on to its end on garbage, waiting for nothing.
-    __device__ __forceinline__ void receive(uint32_t n) const {
-        if (!mbar_wait(bar0 + 8u * (n & 1u), (n >> 1) & 1u, abort_flag)) {
-            *abort_flag = 1;
-            record_error(status, ATTT_ERR_TIMEOUT);
-        }
-    }
-    // All threads: this CTA's rows [r0, r1) of z (LD floats each) to all CTAs, and theirs
-    // of `total` from them.
-    template <int LD>
-    __device__ __forceinline__ void share(uint32_t n, const float *z, int r0, int r1, int total) const {
-        fence_proxy_async_smem();
-        __syncthreads();
-        if (threadIdx.x == 0) expect(n, (uint32_t)((total - (r1 - r0)) * LD * 4));
-        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank && r1 > r0) {
-            const uint32_t at = smem_u32(z + r0 * LD);
-            send(n, at, at, (uint32_t)((r1 - r0) * LD * 4), threadIdx.x);
-        }
-        receive(n);
-    }
-};
-
 __device__ __forceinline__ float4 shfl_xor4(float4 v, int o) {
     return make_float4(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o),
                        __shfl_xor_sync(0xffffffffu, v.z, o), __shfl_xor_sync(0xffffffffu, v.w, o));
@@ -154,54 +80,6 @@ __device__ __forceinline__ float4 shfl_xor4(float4 v, int o) {
 __device__ __forceinline__ float4 add4(float4 a, float4 b) {
     return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
 }
-
-// Shared memory is named by its place in s_muon: functions of their own know no other
-// way that an address is not global.
-extern __shared__ float4 s_muon[];
-__device__ __forceinline__ float *muon_smem(int at) { return reinterpret_cast<float *>(s_muon) + at; }
-
-// The elements of columns [0, cols) from column c0 on, U items of 1 (or, V4, 4
-// neighbours in memory) per thread at a time: first(u, at) for each of them, then
-// second(u, at, so), so that U loads are on their way together.  `at`: index from the
-// first column's first element in global memory; so: place in shared memory.
-// Neighbours are the rows k .. k + 3 of a column (tall), or the columns c .. c + 3.
-template <int RP, int U, bool V4, class F, class S>
-__device__ __forceinline__ void muon_items(const MuonMat &t, int r, uint32_t inv_r, int cols, F &&first, S &&second) {
-    constexpr int W = V4 ? 4 : 1, LD = MuonShape<RP>::LD;
-    // a warp of a wide matrix's items: 8 columns x 4 rows, or 4 x 4 columns x 8 rows
-    constexpr int KR = V4 ? 8 : 4, CW = V4 ? 16 : 8;
-    const int groups = (cols + CW - 1) / CW, width = (int)t.n;
-    const int items = t.tall ? cols * r / W : groups * (RP / KR) * 32;
-    for (int e0 = threadIdx.x; e0 < items; e0 += U * kMuonThreads) {
-        uint32_t at[U];
-        int so[U];
-        bool in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int e = e0 + u * kMuonThreads;
-            if (t.tall) {
-                const int c = r == 1 ? e : (int)__umulhi((uint32_t)(W * e), inv_r);
-                at[u] = (uint32_t)(W * e);
-                so[u] = c * LD + W * e - c * r;
-                in[u] = e < items;
-            } else {
-                const int b = e >> 5, lane = e & 31, kb = b / groups;
-                const int k = kb * KR + (V4 ? lane >> 2 : lane >> 3);
-                const int c = (b - kb * groups) * CW + (V4 ? (lane & 3) * 4 : lane & 7);
-                at[u] = (uint32_t)k * (uint32_t)width + (uint32_t)c;
-                so[u] = c * LD + k;
-                in[u] = e < items && k < r && c < cols;
-            }
-            if (in[u]) first(u, at[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (in[u]) second(u, at[u], so[u]);
-    }
-}
-
-// The first column's first element.
-__device__ __forceinline__ int64_t muon_origin(const MuonMat &t, int r, int64_t c0) { return t.tall ? c0 * r : c0; }
 
 // u of the columns into s (rows of r..RP stay 0), m updated when `first`.  (The passes over
 // columns are functions of their own: inlined, what lives across them spills inside
@@ -214,7 +92,7 @@ __device__ __forceinline__ void muon_load_as(const MuonArgs &a, const MuonMat &t
     const float *pg = t.g + o;
     float *pm = t.m + o;
     float g[U][W], m[U][W];
-    muon_items<RP, U, V4>(
+    muon_items<RP, LD, U, V4>(
         t, a.r, a.inv_r, cols,
         [&](int u, uint32_t at) {
             if constexpr (V4) {
@@ -258,56 +136,6 @@ __device__ __noinline__ void muon_load(const MuonArgs &a, const MuonMat &t, int 
             s[e / (RP - a.r) * LD + a.r + e % (RP - a.r)] = 0.f;
     if (t.vec) muon_load_as<RP, true>(a, t, s, c0, cols, first);
     else muon_load_as<RP, false>(a, t, s, c0, cols, first);
-}
-
-// p <- keep p - step X for the columns, and the bf16 copy.
-template <int RP, bool V4>
-__device__ __forceinline__ void muon_update_as(const MuonArgs &a, const MuonMat &t, const float *s, int64_t c0,
-                                               int cols) {
-    constexpr int LD = MuonShape<RP>::LD, W = V4 ? 4 : 1, U = V4 ? 5 : 6;
-    const int64_t o = muon_origin(t, a.r, c0);
-    float *pp = t.p + o;
-    __nv_bfloat16 *ph = t.p16 ? t.p16 + o : nullptr;
-    float p[U][W];
-    muon_items<RP, U, V4>(
-        t, a.r, a.inv_r, cols,
-        [&](int u, uint32_t at) {
-            if constexpr (V4) {
-                const float4 x = *reinterpret_cast<const float4 *>(pp + at);
-                p[u][0] = x.x; p[u][1] = x.y; p[u][2] = x.z; p[u][3] = x.w;
-            } else {
-                p[u][0] = pp[at];
-            }
-        },
-        [&](int u, uint32_t at, int so) {
-            float x[W];
-            if (V4 && t.tall) {
-                const float4 q = *reinterpret_cast<const float4 *>(s + so);
-                x[0] = q.x; x[W / 4] = q.y; x[W / 2] = q.z; x[W - 1] = q.w;
-            } else {
-#pragma unroll
-                for (int w = 0; w < W; ++w) x[w] = s[so + w * LD];
-            }
-#pragma unroll
-            for (int w = 0; w < W; ++w) p[u][w] = fmaf(-t.step, x[w], p[u][w] * a.keep);
-            if constexpr (V4) {
-                *reinterpret_cast<float4 *>(pp + at) = make_float4(p[u][0], p[u][1], p[u][2], p[u][3]);
-                if (ph) {
-                    __nv_bfloat162 h[2] = {__floats2bfloat162_rn(p[u][0], p[u][1]),
-                                           __floats2bfloat162_rn(p[u][2], p[u][3])};
-                    *reinterpret_cast<uint2 *>(ph + at) = *reinterpret_cast<uint2 *>(h);
-                }
-            } else {
-                pp[at] = p[u][0];
-                if (ph) ph[at] = __float2bfloat16_rn(p[u][0]);
-            }
-        });
-}
-
-template <int RP>
-__device__ __noinline__ void muon_update(const MuonArgs &a, const MuonMat &t, int s_at, int64_t c0, int cols) {
-    if (t.vec) muon_update_as<RP, true>(a, t, muon_smem(s_at), c0, cols);
-    else muon_update_as<RP, false>(a, t, muon_smem(s_at), c0, cols);
 }
 
 // acc += the columns' part of X X^T, this thread's 4 x TJ elements and its share of the
@@ -370,27 +198,14 @@ __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP
             part[(j + 3) * RP + i] = v.w;
         }
     }
-    fence_proxy_async_smem();
-    __syncthreads();
-    const int cluster = link.cluster, rank = link.rank;
-    const int r0 = muon_row(RP, rank, cluster), r1 = muon_row(RP, rank + 1, cluster), rows = r1 - r0;
-    // every CTA's rows of this one's Gram matrix to it: place `rank` of its recv
-    if (threadIdx.x == 0) link.expect(n, (uint32_t)((cluster - 1) * rows * RP * 4));
-    if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank) {
-        const int o0 = muon_row(RP, threadIdx.x, cluster), o = muon_row(RP, threadIdx.x + 1, cluster) - o0;
-        if (o > 0)
-            link.send(n, smem_u32(recv + rank * o * RP), smem_u32(part + o0 * RP), (uint32_t)(o * RP * 4), threadIdx.x);
-    }
-    link.receive(n);
-    for (int e = threadIdx.x; e < rows * RP / 4; e += kMuonThreads) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = 0; c < cluster; ++c)
-            v = add4(v, *reinterpret_cast<const float4 *>(c == rank ? part + r0 * RP + 4 * e
-                                                                   : recv + c * rows * RP + 4 * e));
-        *reinterpret_cast<float4 *>(G + (r0 + e / (RP / 4)) * S::LD + e % (RP / 4) * 4) = v;
-    }
-    link.share<S::LD>(n + 1, G, r0, r1, RP);
+    const int r0 = muon_row(RP, link.rank, link.cluster), r1 = muon_row(RP, link.rank + 1, link.cluster);
+    float *const slab = recv + S::kRecv;
+    link.gather<RP>(n, part, recv, r0, r1, [&](int e, float4 v) {
+        const int at = e / (RP / 4) * S::LD + e % (RP / 4) * 4;
+        *reinterpret_cast<float4 *>(G + r0 * S::LD + at) = v;
+        *reinterpret_cast<float4 *>(slab + at) = v;
+    });
+    link.share<S::LD>(n + 1, slab, G, r0, r1, RP);
 }
 
 // z = alpha x y (+ beta w, w_at >= 0) + diag I in every CTA, x and y symmetric and
@@ -431,7 +246,7 @@ __device__ __noinline__ void muon_product(int x_at, int y_at, int z_at, float al
         if (i == j + 3) v.w += diag;
         *reinterpret_cast<float4 *>(z + i * S::LD + j) = v;
     }
-    if constexpr (S::kSlabs) link.share<S::LD>(n, z, r0, r1, RP);
+    if constexpr (S::kSlabs) link.share<S::LD>(n, z + r0 * S::LD, z, r0, r1, RP);
     else __syncthreads();
 }
 
@@ -535,6 +350,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
 
     const int groups = (a.steps + 1) / 2, single = a.steps % 2 ? groups / 2 : -1;  // pairs, the odd step amidst them
     for (int gi = 0; gi < groups; ++gi) {
+        if (gi > 0) cluster_sync();  // every CTA has what this one's matrices were sent for
         muon_gram_sum<RP>(acc, G, part, recv, G, link, n);
         n += 2;
         float scale = 1.f;
@@ -554,17 +370,16 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
             __syncthreads();
         }
         // B = a I + b G + c G^2, and for a pair of steps G <- B G B, P = (a I + b G + c G^2) B
+        // (a single first step takes the scale into B, as X_0 has it in u)
         int oP = oB;
-        muon_product<RP>(oG, oG, oB, kNsC, oG, kNsB, kNsA, link, n++);
+        const float s0 = gi == single ? scale : 1.f;
+        muon_product<RP>(oG, oG, oB, kNsC * s0, oG, kNsB * s0, kNsA * s0, link, n++);
         if (gi != single) {
             muon_product<RP>(oB, oG, oT, 1.f, -1, 0.f, 0.f, link, n++);
             muon_product<RP>(oT, oB, oG, 1.f, -1, 0.f, 0.f, link, n++);
             muon_product<RP>(oG, oG, oT, kNsC, oG, kNsB, kNsA, link, n++);
             muon_product<RP>(oT, oB, oG, scale, -1, 0.f, 0.f, link, n++);
             oP = oG;
-        } else if (gi == 0) {
-            for (int e = threadIdx.x; e < RP * RP; e += kMuonThreads) B[e / RP * S::LD + e % RP] *= scale;
-            __syncthreads();
         }
         if constexpr (!S::kSlabs) n = 2 * (gi + 1);  // the products were no exchanges
         const bool last = gi + 1 == groups;
@@ -617,20 +432,16 @@ static bool muon_sizes(int nproj, const int64_t *din, const int64_t *dout, int r
     return true;
 }
 
-// Clusters of each size that the device runs at once (0: none), for one kernel (and a
-// second one of the same kind) with one amount of shared memory, asked once per device.
-static bool muon_clusters(const void *kern, const void *other, size_t smem, int dev,
-                          int (&most)[kMuonMaxCluster + 1]) {
+bool muon_clusters(const void *kern, size_t smem, int dev, int (&most)[kMuonMaxCluster + 1]) {
     static std::mutex mu;
     static std::map<std::pair<const void *, int>, std::array<int, kMuonMaxCluster + 1>> known;
     std::lock_guard<std::mutex> lock(mu);
     const auto key = std::make_pair(kern, dev);
     auto it = known.find(key);
     if (it == known.end()) {
-        for (const void *k : {kern, other})
-            if (cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
         std::array<int, kMuonMaxCluster + 1> n{};
-        for (int c = 4; c <= kMuonMaxCluster; ++c) {
+        for (int c = kMuonMinCluster; c <= kMuonMaxCluster; ++c) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3((unsigned)(kMuonMats * c));
             cfg.blockDim = dim3(kMuonThreads);
@@ -652,33 +463,21 @@ static bool muon_clusters(const void *kern, const void *other, size_t smem, int 
     return true;
 }
 
-template <int RP>
-static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) {
-    using S = MuonShape<RP>;
-    constexpr size_t kMax = 232448 - 1024;  // 227 KB opt-in less the static part
-    const void *kern = reinterpret_cast<const void *>(muon_kernel<RP, false>);
-    const void *stream_kern = reinterpret_cast<const void *>(muon_kernel<RP, true>);
-    a.room = (int)((kMax - sizeof(float) * S::kFixed) / (sizeof(float) * S::LD)) / 8 * 8;
-    const size_t smem = sizeof(float) * (S::kFixed + (size_t)a.room * S::LD);
-    int most[kMuonMaxCluster + 1];
-    if (!set_smem_limit(kern, smem, dev) || !set_smem_limit(stream_kern, smem, dev) ||
-        !muon_clusters(kern, stream_kern, smem, dev, most))
-        return ATTT_ERR_CUDA;
-    // The CTAs of a cluster: as many as leave the fewest columns for a CTA in all the
-    // rounds that the clusters take (a part with 15 clusters of 8, 8 of 12 and 7 of 16
-    // takes 12 for 8 matrices and 8 for 14).
-    int64_t n = 0;
-    for (int i = 0; i < nmat; ++i) n = std::max(n, a.mat[i].n);
-    int64_t best = INT64_MAX;
-    for (int c = 4; c <= kMuonMaxCluster; ++c) {
-        if (most[c] < 1) continue;
-        const int64_t cost = cdiv(nmat, most[c]) * round_up(cdiv(n, c), 8);
-        if (cost < best) {
-            best = cost;
-            a.cluster = c;
+int muon_cluster(const int (&most)[kMuonMaxCluster + 1], int nmat, int64_t n, int64_t room, int64_t *cost) {
+    int best = 0;
+    for (int c = kMuonMinCluster; c <= kMuonMaxCluster; ++c) {
+        const int64_t per = round_up(cdiv(n, c), 8);
+        if (most[c] < 1 || (room > 0 && per > room)) continue;
+        const int64_t now = cdiv(nmat, most[c]) * per;
+        if (best == 0 || now < *cost) {
+            *cost = now;
+            best = c;
         }
     }
-    if (best == INT64_MAX) return ATTT_ERR_CUDA;
+    return best;
+}
+
+attt_status muon_launch(const void *kern, MuonArgs &a, int nmat, size_t smem, cudaStream_t stream) {
     for (int i = 0; i < nmat; ++i) a.mat[i].per = round_up(cdiv(a.mat[i].n, a.cluster), 8);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(nmat * a.cluster));
@@ -692,12 +491,28 @@ static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) 
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const bool all = round_up(cdiv(n, a.cluster), 8) <= a.room;
-    if ((all ? cudaLaunchKernelEx(&cfg, muon_kernel<RP, false>, a)
-             : cudaLaunchKernelEx(&cfg, muon_kernel<RP, true>, a)) != cudaSuccess)
-        return ATTT_ERR_CUDA;
+    void *args[] = {&a};
+    if (cudaLaunchKernelExC(&cfg, kern, args) != cudaSuccess) return ATTT_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
+}
+
+template <int RP>
+static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) {
+    using S = MuonShape<RP>;
+    constexpr size_t kMax = 232448 - 1024;  // 227 KB opt-in less the static part
+    const void *kerns[2] = {reinterpret_cast<const void *>(muon_kernel<RP, false>),
+                            reinterpret_cast<const void *>(muon_kernel<RP, true>)};
+    a.room = (int)((kMax - sizeof(float) * S::kFixed) / (sizeof(float) * S::LD)) / 8 * 8;
+    const size_t smem = sizeof(float) * (S::kFixed + (size_t)a.room * S::LD);
+    int most[2][kMuonMaxCluster + 1];
+    for (int k = 0; k < 2; ++k)
+        if (!set_smem_limit(kerns[k], smem, dev) || !muon_clusters(kerns[k], smem, dev, most[k])) return ATTT_ERR_CUDA;
+    int64_t n = 0, cost = 0;
+    for (int i = 0; i < nmat; ++i) n = std::max(n, a.mat[i].n);
+    a.cluster = muon_cluster(most[0], nmat, n, 0, &cost);
+    if (a.cluster == 0) return ATTT_ERR_CUDA;
+    return muon_launch(kerns[round_up(cdiv(n, a.cluster), 8) <= a.room ? 0 : 1], a, nmat, smem, stream);
 }
 
 }  // namespace attt
@@ -751,6 +566,11 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
         t.x = x;
         x += t.n * muon_rp(r);
         t.step = (float)((double)lr * rms * std::sqrt((double)std::max<int64_t>(t.n, r)));
+    }
+    if (r > 32) {
+        bool done = false;
+        const attt_status tc = muon_tc_run(a, 2 * nproj, dev, stream, &done);
+        if (done || tc != ATTT_OK) return tc;
     }
     return r <= 16 ? muon_run<16>(a, 2 * nproj, dev, stream)
          : r <= 32 ? muon_run<32>(a, 2 * nproj, dev, stream)
