@@ -55,10 +55,10 @@ struct MuonShape {
     // Gram matrix; what the others send of its slab of theirs
     static constexpr int kFirst = 3 * kMat > kScratch ? 3 * kMat : kScratch;
     // (cluster x rows of a slab, which are not even: up to RP + cluster rows)
-    static constexpr int kRecv = (RP + kMuonMaxCluster) * RP;
+    static constexpr int kRecv = (RP + kMuonMaxCluster) * LD;
     // this CTA's slab of the sum, to be sent (G itself is written again at once)
     static constexpr int kSlab = (RP / kMuonMinCluster) * LD;
-    static constexpr int kFixed = kFirst + RP * RP + kRecv + kSlab;
+    static constexpr int kFixed = kFirst + kMat + kRecv + kSlab;
     // Row and column of a Gram tile's first element.
     __device__ static __forceinline__ void tile(int t, int &i0, int &j0) {
         if constexpr (RP > 32) {
@@ -164,7 +164,7 @@ __device__ __forceinline__ void muon_gram(const float *s, int cols, float (&acc)
 }
 
 // The cluster's Gram matrix into G of every CTA, from the threads' shares (exchanges n and
-// n + 1).  `part`: RP x RP floats, `recv`: kRecv.
+// n + 1).  `part`: kMat floats, `recv`: kRecv.
 template <int RP>
 __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP>::TJ], float *scratch, float *part,
                                               float *recv, float *G, const MuonLink &link, uint32_t n) {
@@ -190,18 +190,17 @@ __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP
         const int at = e / S::kTiles;
         i += at / (S::TJ / 4);
         j += at % (S::TJ / 4) * 4;
-        *reinterpret_cast<float4 *>(part + i * RP + j) = v;
+        *reinterpret_cast<float4 *>(part + i * S::LD + j) = v;
         if (RP > 32 && i < 32 && j >= 32) {
-            part[j * RP + i] = v.x;
-            part[(j + 1) * RP + i] = v.y;
-            part[(j + 2) * RP + i] = v.z;
-            part[(j + 3) * RP + i] = v.w;
+            part[j * S::LD + i] = v.x;
+            part[(j + 1) * S::LD + i] = v.y;
+            part[(j + 2) * S::LD + i] = v.z;
+            part[(j + 3) * S::LD + i] = v.w;
         }
     }
     const int r0 = muon_row(RP, link.rank, link.cluster), r1 = muon_row(RP, link.rank + 1, link.cluster);
     float *const slab = recv + S::kRecv;
-    link.gather<RP>(n, part, recv, r0, r1, [&](int e, float4 v) {
-        const int at = e / (RP / 4) * S::LD + e % (RP / 4) * 4;
+    link.gather<RP, S::LD>(n, part, recv, r0, r1, [&](int at, float4 v) {
         *reinterpret_cast<float4 *>(G + r0 * S::LD + at) = v;
         *reinterpret_cast<float4 *>(slab + at) = v;
     });
@@ -313,7 +312,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
     using S = MuonShape<RP>;
     constexpr int oG = 0, oB = S::kMat, oT = 2 * S::kMat, oX = S::kFixed;
     float *const G = muon_smem(oG), *const B = muon_smem(oB), *const part = muon_smem(S::kFirst),
-          *const recv = part + RP * RP, *const X = muon_smem(oX);
+          *const recv = part + S::kMat, *const X = muon_smem(oX);
     __shared__ float s_scale;
     __shared__ __align__(8) uint64_t s_bars[2];
     __shared__ int s_abort;

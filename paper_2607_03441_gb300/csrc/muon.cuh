@@ -68,31 +68,32 @@ struct MuonLink {
             record_error(status, ATTT_ERR_TIMEOUT);
         }
     }
-    // Every CTA's rows of this one's RP x RP matrix `part` to it, place `rank` of its recv;
-    // then rows [r0, r1) of the sum over the CTAs, in their order: add(e, v) for vector e
-    // of 4 of them.  Exchange n.
-    template <int RP, class Add>
+    // Every CTA's rows of this one's RP x RP matrix `part` (rows of LD floats) to it, place
+    // `rank` of its recv; then rows [r0, r1) of the sum over the CTAs, in their order:
+    // add(at, v) for 4 of them at `at` from the first row.  Exchange n.
+    template <int RP, int LD, class Add>
     __device__ __forceinline__ void gather(uint32_t n, const float *part, const float *recv, int r0, int r1,
                                            Add &&add) const {
         const int rows = r1 - r0;
         fence_proxy_async_smem();
         __syncthreads();
-        if (threadIdx.x == 0) expect(n, (uint32_t)((cluster - 1) * rows * RP * 4));
+        if (threadIdx.x == 0) expect(n, (uint32_t)((cluster - 1) * rows * LD * 4));
         if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank) {
             const int o0 = muon_row(RP, threadIdx.x, cluster), o = muon_row(RP, threadIdx.x + 1, cluster) - o0;
             if (o > 0)
-                send(n, smem_u32(recv + rank * o * RP), smem_u32(part + o0 * RP), (uint32_t)(o * RP * 4), threadIdx.x);
+                send(n, smem_u32(recv + rank * o * LD), smem_u32(part + o0 * LD), (uint32_t)(o * LD * 4), threadIdx.x);
         }
         receive(n);
         for (int e = threadIdx.x; e < rows * RP / 4; e += kMuonThreads) {
+            const int at = e / (RP / 4) * LD + e % (RP / 4) * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
             for (int c = 0; c < cluster; ++c) {
                 const float4 q =
-                    *reinterpret_cast<const float4 *>(c == rank ? part + r0 * RP + 4 * e : recv + c * rows * RP + 4 * e);
+                    *reinterpret_cast<const float4 *>(c == rank ? part + r0 * LD + at : recv + c * rows * LD + at);
                 v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
             }
-            add(e, v);
+            add(at, v);
         }
     }
     // All threads: rows [r0, r1) of z (LD floats each) to all CTAs from `src`, and theirs of
@@ -162,7 +163,7 @@ __device__ __forceinline__ int64_t muon_origin(const MuonMat &t, int r, int64_t 
 template <int RP, bool V4>
 __device__ __forceinline__ void muon_update_as(const MuonArgs &a, const MuonMat &t, const float *s, int64_t c0,
                                                int cols) {
-    constexpr int LD = RP + 4, W = V4 ? 4 : 1, U = V4 ? 5 : 6;
+    constexpr int LD = RP + 4, W = V4 ? 4 : 1, U = V4 ? 7 : 8;
     const int64_t o = muon_origin(t, a.r, c0);
     float *pp = t.p + o;
     __nv_bfloat16 *ph = t.p16 ? t.p16 + o : nullptr;

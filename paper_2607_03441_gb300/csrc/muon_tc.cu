@@ -23,18 +23,21 @@
 
 namespace attt {
 
-constexpr int kTcCols = 448;                          // columns of a CTA at most
+constexpr int kTcCols = 440;                          // columns of a CTA at most
 constexpr uint32_t kTcSplit = kTcCols * 128u;         // bytes of one of X's tiles
 constexpr uint32_t kTcMat = 64 * 128u;                // of one of an r x r matrix's
 constexpr uint32_t kTcTmem = 512;
-constexpr uint32_t kTcPoly = 256, kTcGram = 320;      // TMEM columns of the r x r products, of the Gram matrix
-constexpr int kTcPart = 0, kTcRecv = 4096, kTcG = kTcRecv + (64 + kMuonMaxCluster) * 64;  // floats
-constexpr int kTcSlab = kTcG + 4096;                  // beside them: outgoing copies may still read it
-constexpr uint32_t kTcRest = (kTcSlab + 64 / kMuonMinCluster * 64) * 4u;
+constexpr uint32_t kTcPoly = 256, kTcGram = 320;      // TMEM columns of the r x r products (64), the Gram matrix (192)
+// fp32 matrices for the exchanges, in floats, over two r x r matrices' tiles; rows of 68:
+// vectors of 8 neighbouring rows then lie in different banks
+constexpr int kTcLD = 68;
+constexpr int kTcPart = 0, kTcRecv = 64 * kTcLD, kTcG = kTcRecv + (64 + kMuonMaxCluster) * kTcLD;
+constexpr int kTcSlab = kTcG + 64 * kTcLD;            // beside the tiles: outgoing copies may still read it
+constexpr uint32_t kTcRest = (kTcSlab + 64 / kMuonMinCluster * kTcLD) * 4u;
 static_assert(kTcSlab * 4u >= 6 * kTcMat && kTcRest >= 7 * kTcMat, "two matrices of three tiles, and a seventh to overrun");
 static_assert(kTcSplit % 1024 == 0 && kTcCols * 68 * 4 <= 3 * kTcSplit, "");
 constexpr size_t kTcSmem = 1024 + 3 * kTcSplit + kTcRest;
-static_assert(kTcCols / 128 * 128 + 128 <= 512 && 64 * 128 <= kTcRest, "the last tile of 128 columns stays in bounds");
+static_assert(kTcCols / 128 * 128 + 128 <= 512 && (512 - kTcCols) * 128 <= (int)kTcRest, "the last tile of 128 columns stays in bounds");
 
 // Three bf16 whose sum is x, two values at a time, packed.
 struct Split2 {
@@ -99,16 +102,16 @@ __device__ __forceinline__ void tc_load_as(const MuonArgs &a, const MuonMat &t, 
     float *pm = t.m + o;
     if constexpr (V4) {
         if (!t.tall) {
-            // a warp: 8 rows (lane & 7) x 4 groups of 4 columns; four lanes then exchange, so
+            // a warp: 4 rows (lane & 3) x 8 groups of 4 columns; four lanes then exchange, so
             // that each has four rows of one column
-            constexpr int U = 3;
-            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (cols + 15) / 16, items = groups * 8;
+            constexpr int U = 5;
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (cols + 31) / 32, items = groups * 16;
             for (int b0 = warp; b0 < items; b0 += U * (kMuonThreads / 32)) {
                 float4 g[U], m[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int b = b0 + u * (kMuonThreads / 32), kb = b / groups, k = kb * 8 + (lane & 7),
-                              c = (b - kb * groups) * 16 + (lane >> 3) * 4;
+                    const int b = b0 + u * (kMuonThreads / 32), kb = b / groups, k = kb * 4 + (lane & 3),
+                              c = (b - kb * groups) * 32 + (lane >> 2) * 4;
                     g[u] = m[u] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (b < items && k < a.r && c < cols) {
                         const uint32_t at = (uint32_t)k * (uint32_t)t.n + (uint32_t)c;
@@ -118,8 +121,8 @@ __device__ __forceinline__ void tc_load_as(const MuonArgs &a, const MuonMat &t, 
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int b = b0 + u * (kMuonThreads / 32), kb = b / groups, k = kb * 8 + (lane & 7),
-                              c = (b - kb * groups) * 16 + (lane >> 3) * 4;
+                    const int b = b0 + u * (kMuonThreads / 32), kb = b / groups, k = kb * 4 + (lane & 3),
+                              c = (b - kb * groups) * 32 + (lane >> 2) * 4;
                     if (b >= items) break;  // warp-uniform
                     float4 v = m[u];
                     v.x = fmaf(a.mu, v.x, g[u].x); v.y = fmaf(a.mu, v.y, g[u].y);
@@ -147,7 +150,7 @@ __device__ __forceinline__ void tc_load_as(const MuonArgs &a, const MuonMat &t, 
             return;
         }
     }
-    constexpr int W = V4 ? 4 : 1, U = V4 ? 4 : 6;
+    constexpr int W = V4 ? 4 : 1, U = V4 ? 5 : 6;
     float g[U][W], m[U][W];
     muon_items<64, 64, U, V4>(
         t, a.r, a.inv_r, cols,
@@ -215,17 +218,15 @@ __device__ __forceinline__ void tc_mma_k64(uint32_t d, uint32_t a0, uint32_t a_s
     }
 }
 
-// One thread: D[128 x 64] = X X^T over `steps` x 16 columns: X's tiles at x0 are both
-// operands, the rank on M and N (the upper half of M, 1,024 bytes on, is not read).
+// One thread: D[128 x 192] = [h m]^T [h m l] over `steps` x 16 columns of X, the rank on M
+// and N (six products of 64 x 64, of which m l is not used; one MMA reads 10 KB of
+// shared memory, which is what it takes, where six of N 64 would read 36).
 __device__ __forceinline__ void tc_mma_gram(uint32_t d, uint32_t x0, int steps) {
-    const uint32_t idesc = idesc_bf16_f32(64, true, true);
-#pragma unroll 1
-    for (int p = 0; p < 6; ++p) {
-        const uint32_t a = x0 + tc_a(p) * kTcSplit, b = x0 + tc_b(p) * kTcSplit;
+    const uint32_t idesc = idesc_bf16_f32(192, true, true);
 #pragma unroll 4
-        for (int s = 0; s < steps; ++s)
-            umma_bf16(d, smem_desc_sw128(a + s * 2048, 1024, 1024), smem_desc_sw128(b + s * 2048, 1024, 1024), idesc,
-                      p > 0 || s > 0 ? 1u : 0u);
+    for (int s = 0; s < steps; ++s) {
+        const uint64_t x = smem_desc_sw128(x0 + s * 2048, kTcSplit, 1024);
+        umma_bf16(d, x, x, idesc, s > 0 ? 1u : 0u);
     }
 }
 
@@ -296,26 +297,35 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
         fence_proxy_async_smem();
         __syncthreads();
     };
+    // The same for r x r products, among the warps that have their results: the others wait
+    // for the last one's.
+    auto settle_few = [&]() {
+        tc_fence_before();
+        fence_proxy_async_smem();
+        named_barrier_sync(1, kMuonThreads / 2);
+    };
     // An r x r matrix is in the first two quarters' lanes: row 32 q + lane, columns 16 part4 ..
     const bool mine = q < 2;
-    const int row = 32 * q + lane, col = 16 * part4;
+    const int row = 32 * q + lane, col = 16 * part4;  // (rows 64 .. 127: the upper lanes)
     float keep[16];  // this thread's elements of G, fp32
     // z = alpha x y (+ beta keep) + diag I from the split x at xa and y at ya to za
     auto product = [&](uint32_t xa, uint32_t ya, uint32_t za, float alpha, float beta, float diag, bool hold) {
+        if (!mine) {
+            ++mmas;
+            return;
+        }
         run([&] { tc_mma_k64(tmem + kTcPoly, xa, kTcMat, ya, kTcMat); });
         await();
-        if (mine) {
-            float v[16];
-            tc_read(tmem, q, kTcPoly + col, v);
+        float v[16];
+        tc_read(tmem, q, kTcPoly + col, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] = fmaf(beta, keep[i], alpha * v[i]);
-                if (col + i == row) v[i] += diag;
-                if (hold) keep[i] = v[i];
-            }
-            tc_put16(za, kTcMat, row, col, v);
+        for (int i = 0; i < 16; ++i) {
+            v[i] = fmaf(beta, keep[i], alpha * v[i]);
+            if (col + i == row) v[i] += diag;
+            if (hold) keep[i] = v[i];
         }
-        settle();
+        tc_put16(za, kTcMat, row, col, v);
+        settle_few();
     };
 
     const int groups = (a.steps + 1) / 2, single = a.steps % 2 ? groups / 2 : -1;  // pairs, the odd step amidst them
@@ -323,29 +333,49 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
         // the cluster's Gram matrix: exchanges over the matrices' tiles, which no CTA reads any more
         run([&] { tc_mma_gram(tmem + kTcGram, x0, steps); });
         await();
-        if (gi > 0) cluster_sync();
-        if (mine) {
-            float v[16];
+        {   // h h + h m + h l (lower lanes) + m h + m m (upper lanes) + (h l)^T
+            float v[16], w[16], hl[16];
             tc_read(tmem, q, kTcGram + col, v);
-            if (steps == 0)
+            tc_read(tmem, q, kTcGram + 64 + col, w);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.f;  // no columns, no MMAs
+            for (int i = 0; i < 16; ++i) v[i] = steps > 0 ? v[i] + w[i] : 0.f;  // no columns: no MMAs
+            const int i0 = row & 63;
+            if (mine) {
+                tc_read(tmem, q, kTcGram + 128 + col, hl);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4 *>(part + row * 64 + col + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                for (int i = 0; i < 16; ++i) G[i0 * 65 + col + i] = steps > 0 ? hl[i] : 0.f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<float4 *>(part + i0 * kTcLD + col + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            }
+            __syncthreads();
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    float4 *to = reinterpret_cast<float4 *>(part + i0 * kTcLD + col + i);
+                    const float4 u = *to;
+                    const float o[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[i + e] += o[e] + (G[i0 * 65 + col + i + e] + G[(col + i + e) * 65 + i0]);
+                    *to = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            }
         }
         tc_fence_before();
+        if (gi > 0) cluster_sync();  // every CTA has done with the matrices' tiles that exchanges come over
         const int r0 = muon_row(64, rank, a.cluster), r1 = muon_row(64, rank + 1, a.cluster);
-        link.gather<64>(n, part, recv, r0, r1, [&](int e, float4 v) {
-            *reinterpret_cast<float4 *>(G + r0 * 64 + 4 * e) = v;
-            *reinterpret_cast<float4 *>(slab + 4 * e) = v;
+        link.gather<64, kTcLD>(n, part, recv, r0, r1, [&](int at, float4 v) {
+            *reinterpret_cast<float4 *>(G + r0 * kTcLD + at) = v;
+            *reinterpret_cast<float4 *>(slab + at) = v;
         });
-        link.share<64>(n + 1, slab, G, r0, r1, 64);
+        link.share<kTcLD>(n + 1, slab, G, r0, r1, 64);
         n += 2;
         float scale = 1.f;
         if (gi == 0) {
             if (warp == 0) {
-                float v = G[lane * 65] + G[(lane + 32) * 65];
+                float v = G[lane * (kTcLD + 1)] + G[(lane + 32) * (kTcLD + 1)];
                 for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
                 if (lane == 0) s_scale = 1.f / (sqrtf(v) + a.eps);
             }
@@ -355,7 +385,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
         if (mine) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(G + row * 64 + col + i);
+                const float4 v = *reinterpret_cast<const float4 *>(G + row * kTcLD + col + i);
                 keep[i] = v.x * scale * scale; keep[i + 1] = v.y * scale * scale;
                 keep[i + 2] = v.z * scale * scale; keep[i + 3] = v.w * scale * scale;
             }
@@ -376,6 +406,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
             product(b1, b1, b2, kNsC * scale, kNsB * scale, kNsA * scale, false);
             P = b2;
         }
+        __syncthreads();
         // X <- P X: warp (q, part4) has columns 128 part4 + 32 q + lane
         const bool last = gi + 1 == groups;
         run([&] {
