@@ -6,16 +6,16 @@
 // With z = h W^T, T the temperature, p = softmax(z / T):
 //   logp_j = z_{j,t_j} / T - lse_j,   lse_j = log sum_v exp(z_jv / T),
 //   H_j = -sum_v p_jv log p_jv.
-// Forward: one contraction over the whole vocabulary (2 L V d FLOPs).  Its epilogue
-// reduces each row of a column set (a tile, or half of one) to its max, the sum
-// of exponentials, that sum's first moment, and its few largest logits
-// (tc_gemm.cuh, EPI_LOGP*); a second kernel merges a row's sets.
+// Forward: one contraction over the whole vocabulary (2 L V d FLOPs).  Every SM, or pair
+// of SMs, takes a run of tiles along rows; its epilogue keeps each row's max, the sum of
+// exponentials, that sum's first moment, and its few largest logits in registers from
+// tile to tile (tc_gemm.cuh, EPI_LOGP*); a second kernel merges a row's runs.
 // Gradient: with given da_j = dL/dlogp_j and db_j = dL/dH_j,
 //   dL/dz_jv = (da_j [v = t_j] - p_jv (da_j + db_j (log p_jv + H_j))) / T,
 // formed from the logits in the epilogue of the same contraction (the
 // softmax needs no second sweep: lse and H are the forward call's) as a bf16 block
 // G, then dh = G W (4 L V d FLOPs: the logits are formed again).
-// Rows are taken in blocks so that the workspace stays bounded.
+// The gradient takes rows in blocks so that G stays bounded.
 // Bound: the tensor core from a few hundred rows on, the head's bytes below.
 #include <algorithm>
 
@@ -24,22 +24,16 @@
 namespace attt {
 
 constexpr int kLpTopMax = 20;
-constexpr int kLpWarps = 16;
-constexpr int kLpRows = 8;  // rows per reduction block: lane & 7
-constexpr int kLpStreams = kLpWarps * 32 / kLpRows;
-// Bounds of the forward workspace (largest logits of every column set and row) and
-// of the gradient block, in bytes per row block.
-constexpr int64_t kLpTopBytes = 512ll << 20;
-constexpr int64_t kLpNarrowBytes = 64ll << 20;  // what narrower sets than a 256-column tile's may take
-constexpr int64_t kLpGBytes = 2048ll << 20;
-constexpr int kFewRows = 32;   // rows of a call that reads the head as the M operand, at most
-constexpr int kFewSets = 160;  // and its CTAs
+constexpr int kLpUnits = 160;  // SMs, or pairs of SMs, that take runs, at most
+constexpr int kLpWarps = 16;   // of a reduction block
+constexpr int64_t kLpGBytes = 2048ll << 20;  // the gradient block of a row block, at most
+constexpr int64_t kLpHiddenBytes = 48ll << 20;  // the hidden states of a row block of the forward call, at most
+constexpr int64_t kLpHeadBytes = 48ll << 20;    // a head that L2 holds beside them (tc_gemm.cuh: Span)
+constexpr int64_t kLpRunRows = 16384;           // and its rows
+constexpr int kFewRows = 32;  // rows of a call that reads the head as the M operand, at most
 constexpr int kLpSplitRegions = 320;  // K pieces of the second contraction: 128 KB each
 
 inline int lp_sets(int64_t d) { return cdiv(d, 64) <= kTwoSetBlocks ? 2 : 1; }
-inline int64_t lp_top_ld(int topk) { return round_up(topk, 4); }
-inline int64_t lp_set_bytes(int topk) { return 12 + 8 * lp_top_ld(topk); }  // of one row
-
 // Rows of a block of `total` rows at `row_bytes` of workspace each: equal blocks, a
 // multiple of 256.
 inline int64_t lp_block_rows(int64_t total, int64_t row_bytes, int64_t bound) {
@@ -50,39 +44,35 @@ inline int64_t lp_block_rows(int64_t total, int64_t row_bytes, int64_t bound) {
 }
 
 struct LpLayout {
-    int64_t rows, plane, ld;  // rows per block; elements of a plane [sets, rows]
-    bool few;
+    int64_t plane, ld;  // elements of a plane [slots, L]; places for a row's largest logits
     float *part, *ztgt, *top_v;
     int32_t *top_i;
     size_t bytes;
 };
 
+// Rows of a block, all of whose tiles share the head's from L2: their hidden states stay
+// there too, and a run is at most a row of tiles long.
+inline int64_t lp_forward_rows(int64_t L, int64_t d) {
+    return lp_block_rows(L, 2 * d, std::min<int64_t>(kLpHiddenBytes, 2 * d * kLpRunRows));
+}
+
+// Slots: U units of runs over m rows of tiles leave at most U / m + 2 runs in each (a
+// run and its neighbours' ends), and no more than U, of up to two slots each if m > 1
+// (tc_gemm.cuh: logp_flush).
 static LpLayout lp_layout(void *ws, int64_t L, int64_t d, int64_t V, int topk) {
     LpLayout c{};
-    if (L <= kFewRows) {  // one set per CTA, 32 alternatives
-        c.few = true;
-        c.rows = L;
-        c.ld = 32;
-        c.plane = kFewSets * L;
-        Carve cv{static_cast<char *>(ws), 0};
-        c.part = cv.take<float>((size_t)(3 * c.plane));
-        c.ztgt = cv.take<float>((size_t)L);
-        c.top_v = cv.take<float>((size_t)(topk > 0 ? c.plane * c.ld : 0));
-        c.top_i = cv.take<int32_t>((size_t)(topk > 0 ? c.plane * c.ld : 0));
-        c.bytes = (size_t)round_up((int64_t)cv.used, 256);
-        return c;
-    }
-    const int64_t wide = cdiv(V, 256) * lp_sets(d), per = lp_set_bytes(topk);
-    c.rows = lp_block_rows(L, wide * per, kLpTopBytes);
-    c.ld = lp_top_ld(topk);
-    const int64_t narrow = cdiv(V, 64) * lp_sets(d) * c.rows, most = kLpNarrowBytes / per;
-    c.plane = narrow < most ? narrow : most;
-    if (c.plane < wide * c.rows) c.plane = wide * c.rows;
+    const int64_t rows = L <= kFewRows ? L : lp_forward_rows(L, d), least = L % rows ? L % rows : rows;
+    auto slots = [](int64_t r) {
+        return r <= 128 ? kLpUnits : 2 * std::min<int64_t>(kLpUnits, kLpUnits / cdiv(r, 256) + 2);
+    };
+    c.plane = std::max(slots(rows) * rows, slots(least) * least) * (L <= kFewRows ? 1 : lp_sets(d));
+    c.ld = L <= kFewRows ? 32 : round_up(topk, 4);
+    const int64_t tops = topk > 0 ? c.plane * c.ld : 0;
     Carve cv{static_cast<char *>(ws), 0};
     c.part = cv.take<float>((size_t)(3 * c.plane));
-    c.ztgt = cv.take<float>((size_t)c.rows);
-    c.top_v = cv.take<float>((size_t)(c.plane * c.ld));
-    c.top_i = cv.take<int32_t>((size_t)(c.plane * c.ld));
+    c.ztgt = cv.take<float>((size_t)L);
+    c.top_v = cv.take<float>((size_t)tops);
+    c.top_i = cv.take<int32_t>((size_t)tops);
     c.bytes = (size_t)round_up((int64_t)cv.used, 256);
     return c;
 }
@@ -113,9 +103,11 @@ struct LpReduceArgs {
     const float *part, *ztgt, *top_v;
     const int32_t *top_i;
     int64_t plane;
-    int nsets, rows, V, topk, top_ld;
+    // sets of a row: `nsets`, or (tile_rows > 0) those of its row tile's runs (tc_gemm.cuh: logp_flush)
+    int nsets, tile_rows, tiles_n, nwork, units, sets, split;
+    int rows, V, topk, top_ld;
     float inv_temp;
-    const int32_t *tgt;  // outputs and tgt from the block's first row
+    const int32_t *tgt;
     float *logp, *entropy, *lse, *top_logp;
     int32_t *top_id;
     int *status;
@@ -136,119 +128,6 @@ __device__ __forceinline__ void lp_row(const LpReduceArgs &a, int j, const LpPar
             lp = __int_as_float(0x7fc00000);
         }
         a.logp[j] = lp;
-    }
-}
-
-// Merges the sets of 8 rows (lane & 7): 64 streams read every 64th set, four sets'
-// loads in flight, then shuffles and shared memory, in a fixed order.  K > 0: every
-// stream also keeps its K largest logits; their lists meet in shared memory, where
-// one warp per row takes the best head of its 64 lists `topk` times, the lowest id
-// among equal ones.
-template <int K>
-__global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpReduceArgs a) {
-    extern __shared__ float s_dyn[];
-    __shared__ LpPart s_part[kLpWarps][kLpRows];
-    __shared__ float s_max[kLpRows], s_ln[kLpRows];
-    griddep_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rl = lane & (kLpRows - 1), sub = lane / kLpRows;
-    const int j = blockIdx.x * kLpRows + rl;
-    const int stream = warp * (32 / kLpRows) + sub;
-    const float c2 = a.inv_temp * kLog2e;
-    LpPart acc{-INFINITY, 0.f, 0.f};
-    if (j < a.rows) {
-        for (int t0 = stream; t0 < a.nsets; t0 += 4 * kLpStreams) {
-            LpPart v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = t0 + k * kLpStreams;
-                const int64_t o = (int64_t)t * a.rows + j;
-                v[k] = t < a.nsets ? LpPart{__ldcg(a.part + o), __ldcg(a.part + a.plane + o),
-                                            __ldcg(a.part + 2 * a.plane + o)}
-                                   : LpPart{-INFINITY, 0.f, 0.f};
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc.merge(v[k], c2);
-        }
-    }
-    for (int o = kLpRows; o < 32; o <<= 1) acc.merge(acc.shfl_xor(o), c2);
-    if (sub == 0) s_part[warp][rl] = acc;
-    if constexpr (K > 0) {
-        TopList<K> top;
-        top.clear();
-        if (j < a.rows) {
-            for (int t = stream; t < a.nsets; t += kLpStreams) {
-                const int64_t o = ((int64_t)t * a.rows + j) * a.top_ld;
-                float v[K];
-#pragma unroll
-                for (int q = 0; q < K; q += 4) {
-                    const float4 f = q < a.top_ld ? __ldcg(reinterpret_cast<const float4 *>(a.top_v + o + q))
-                                                  : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                    v[q] = f.x; v[q + 1] = f.y; v[q + 2] = f.z; v[q + 3] = f.w;
-                }
-                if (v[0] > top.least()) {  // a stream's sets and a set's list come in order: ties keep the lower id
-#pragma unroll
-                    for (int q = 0; q < K; ++q)
-                        if (v[q] > top.least()) top.insert(v[q], __ldcg(a.top_i + o + q));
-                }
-            }
-        }
-        float *sv = s_dyn;
-        int *si = reinterpret_cast<int *>(s_dyn + kLpRows * kLpStreams * K);
-#pragma unroll
-        for (int q = 0; q < K; ++q) {
-            sv[(rl * kLpStreams + stream) * K + q] = top.v[q];
-            si[(rl * kLpStreams + stream) * K + q] = top.id[q];
-        }
-    }
-    __syncthreads();
-    if (warp == 0) {
-        acc = LpPart{-INFINITY, 0.f, 0.f};
-        for (int w = sub; w < kLpWarps; w += 32 / kLpRows) acc.merge(s_part[w][rl], c2);
-        for (int o = kLpRows; o < 32; o <<= 1) acc.merge(acc.shfl_xor(o), c2);
-        if (j < a.rows && sub == 0) {
-            const float ln = logf(acc.s);
-            s_max[rl] = acc.m;
-            s_ln[rl] = ln;
-            lp_row(a, j, acc, ln);
-        }
-    }
-    if constexpr (K > 0) {
-        __syncthreads();
-        const int jr = blockIdx.x * kLpRows + warp;
-        if (warp >= kLpRows || jr >= a.rows) return;
-        const float *sv = s_dyn + warp * kLpStreams * K;
-        const int *si = reinterpret_cast<const int *>(s_dyn + kLpRows * kLpStreams * K) + warp * kLpStreams * K;
-        int h0 = 0, h1 = 0;  // heads of this lane's lists, lane and lane + 32
-        for (int q = 0; q < a.topk; ++q) {
-            float v = h0 < K ? sv[lane * K + h0] : -INFINITY;
-            int id = h0 < K ? si[lane * K + h0] : -1;
-            const float v1 = h1 < K ? sv[(lane + 32) * K + h1] : -INFINITY;
-            const int id1 = h1 < K ? si[(lane + 32) * K + h1] : -1;
-            const bool second = v1 > v || (v1 == v && (unsigned)id1 < (unsigned)id);  // -1: after every id
-            if (second) {
-                v = v1;
-                id = id1;
-            }
-            float bv = v;
-            unsigned bi = (unsigned)id;
-            for (int o = 16; o > 0; o >>= 1) {
-                const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-                const unsigned oi = __shfl_xor_sync(0xffffffffu, bi, o);
-                if (ov > bv || (ov == bv && oi < bi)) {
-                    bv = ov;
-                    bi = oi;
-                }
-            }
-            if (bi == (unsigned)id && id >= 0) {
-                if (second) ++h1;
-                else ++h0;
-            }
-            if (lane == 0) {
-                a.top_logp[(int64_t)jr * a.topk + q] = (bv - s_max[warp]) * a.inv_temp - s_ln[warp];
-                a.top_id[(int64_t)jr * a.topk + q] = (int)bi;
-            }
-        }
     }
 }
 
@@ -339,7 +218,7 @@ struct FewArgs {
     float c2;  // log2 e / T
     const int32_t *tgt;
     float *ztgt;
-    float *part;   // [CTAs][L] max, then sum, then moment, kFewSets * L apart
+    float *part;   // [CTAs][L] max, then sum, then moment, kLpUnits * L apart
     float *top_v;  // [CTAs][L][32]
     int32_t *top_i;
     int *status;
@@ -528,7 +407,7 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
             }
         }
         named_barrier_sync(1u + set, 128);
-        const int64_t plane = (int64_t)kFewSets * a.L;
+        const int64_t plane = (int64_t)kLpUnits * a.L;
         for (int t = q; t < rows; t += 4) {
             const int64_t o = (int64_t)blockIdx.x * a.L + row0 + t;
             if (lane == 0) {
@@ -556,54 +435,85 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
     if (warp == 1) tmem_dealloc(tmem_base, kCols);
 }
 
-// The CTAs' results of row blockIdx.x: warps take every kLpWarps-th, all of a warp's loads
-// on their way at once, then warp 0 takes the warps'.
-template <bool TOP>
-__global__ void __launch_bounds__(kLpWarps * 32)
-    logprob_few_reduce_kernel(const LpReduceArgs a) {
+// Merges a row's sets: WARPS warps per row, each every WARPS-th set, some at a time on
+// their way, then the first one the others' (ties of alternatives go to the lowest id,
+// sums are in a fixed order).  FEW: the sets of a call of few rows, one per CTA and each
+// with 32 alternatives, all on their way at once (13 rows through 33,364 x 3,368: 63 us the
+// call, 66 with the loops that other calls take).
+template <bool TOP, int WARPS, bool FEW>
+__global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpReduceArgs a) {
     __shared__ LpPart s_part[kLpWarps];
     __shared__ float s_v[kLpWarps][32];
     __shared__ int s_i[kLpWarps][32];
-    constexpr int kEach = kFewSets / kLpWarps;
     griddep_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
+    const int j = blockIdx.x * (kLpWarps / WARPS) + warp / WARPS;
+    if (WARPS == 1 && j >= a.rows) return;  // (a block of one row always has it)
     const float c2 = a.inv_temp * kLog2e;
     LpPart p{-INFINITY, 0.f, 0.f};
-    {
-        const int t = warp + lane * kLpWarps;  // one set per lane
+    float v = -INFINITY;
+    int id = -1;
+    if constexpr (FEW) {
+        constexpr int kEach = kLpUnits / WARPS;
+        const int t = w + lane * WARPS;
         const int64_t o = (int64_t)t * a.rows + j;
         if (lane < kEach && t < a.nsets)
             p = LpPart{__ldcg(a.part + o), __ldcg(a.part + a.plane + o), __ldcg(a.part + 2 * a.plane + o)};
-    }
-    float v = -INFINITY;
-    int id = -1;
-    if constexpr (TOP) {
-        float nv[kEach];
-        int ni[kEach];
+        if constexpr (TOP) {
+            float nv[kEach];
+            int ni[kEach];
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const int t = warp + k * kLpWarps;
-            const int64_t o = ((int64_t)t * a.rows + j) * 32 + lane;
-            nv[k] = t < a.nsets ? __ldcg(a.top_v + o) : -INFINITY;
-            ni[k] = t < a.nsets ? __ldcg(a.top_i + o) : -1;
+            for (int k = 0; k < kEach; ++k) {
+                const int t = w + k * WARPS;
+                const int64_t o = ((int64_t)t * a.rows + j) * 32 + lane;
+                nv[k] = t < a.nsets ? __ldcg(a.top_v + o) : -INFINITY;
+                ni[k] = t < a.nsets ? __ldcg(a.top_i + o) : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) lp_merge(v, id, nv[k], ni[k], lane);
         }
+    } else {
+        const int first = j / a.tile_rows * a.tiles_n;
+        const int units = run_unit(a.nwork, first + a.tiles_n - 1, a.units) - run_unit(a.nwork, first, a.units) + 1;
+        const int nsets = a.sets * units * (a.split ? 2 : 1);
+        for (int t = w + lane * WARPS; t < nsets; t += 32 * WARPS) {
+            const int64_t o = (int64_t)t * a.rows + j;
+            p.merge(LpPart{__ldcg(a.part + o), __ldcg(a.part + a.plane + o), __ldcg(a.part + 2 * a.plane + o)}, c2);
+        }
+        if constexpr (TOP) {
+            for (int t0 = w; t0 < nsets; t0 += 4 * WARPS) {
+                float nv[4];
+                int ni[4];
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) lp_merge(v, id, nv[k], ni[k], lane);
+                for (int k = 0; k < 4; ++k) {
+                    const int t = t0 + k * WARPS;
+                    const int64_t o = ((int64_t)t * a.rows + j) * a.top_ld + lane;
+                    nv[k] = lane < a.topk && t < nsets ? __ldcg(a.top_v + o) : -INFINITY;
+                    ni[k] = lane < a.topk && t < nsets ? __ldcg(a.top_i + o) : -1;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (t0 + k * WARPS < nsets) lp_merge(v, id, nv[k], ni[k], lane);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
+    if constexpr (WARPS > 1) {
+        if (lane == 0) s_part[warp] = p;
         s_v[warp][lane] = v;
         s_i[warp][lane] = id;
+        __syncthreads();
+        if (w > 0) return;
+        p = lane < WARPS ? s_part[warp + lane] : LpPart{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
+        if constexpr (TOP)
+            for (int k = 1; k < WARPS; ++k) lp_merge(v, id, s_v[warp + k][lane], s_i[warp + k][lane], lane);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
-    if (lane == 0) s_part[warp] = p;
-    __syncthreads();
-    if (warp > 0) return;
-    p = lane < kLpWarps ? s_part[lane] : LpPart{-INFINITY, 0.f, 0.f};
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
     const float ln = logf(p.s);
     if (lane == 0) lp_row(a, j, p, ln);
     if constexpr (TOP) {
-        for (int k = 1; k < kLpWarps; ++k) lp_merge(v, id, s_v[k][lane], s_i[k][lane], lane);
         if (lane < a.topk) {
             a.top_logp[(int64_t)j * a.topk + lane] = (v - p.m) * a.inv_temp - ln;
             a.top_id[(int64_t)j * a.topk + lane] = id;
@@ -611,24 +521,27 @@ __global__ void __launch_bounds__(kLpWarps * 32)
     }
 }
 
-template <int K>
-static attt_status launch_reduce(const LpReduceArgs &a, int dev, cudaStream_t stream) {
-    auto kern = logprob_reduce_kernel<K>;
-    const size_t smem = (size_t)8 * kLpRows * kLpStreams * K;
-    if (smem > 0 && !set_smem_limit(reinterpret_cast<const void *>(kern), smem, dev)) return ATTT_ERR_CUDA;
+template <bool TOP, int WARPS, bool FEW>
+static attt_status launch_reduce_as(const LpReduceArgs &a, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)cdiv(a.rows, kLpRows));
+    cfg.gridDim = dim3((unsigned)cdiv(a.rows, kLpWarps / WARPS));
     cfg.blockDim = dim3(kLpWarps * 32);
-    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kern, a) != cudaSuccess) return ATTT_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, logprob_reduce_kernel<TOP, WARPS, FEW>, a) != cudaSuccess) return ATTT_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
+}
+
+// A block per row while there are many sets and few rows, a warp per row else.
+template <bool TOP>
+static attt_status launch_reduce(const LpReduceArgs &a, cudaStream_t stream) {
+    if (a.tile_rows == 0) return launch_reduce_as<TOP, kLpWarps, true>(a, stream);
+    return a.rows <= 1024 ? launch_reduce_as<TOP, kLpWarps, false>(a, stream) : launch_reduce_as<TOP, 1, false>(a, stream);
 }
 
 template <bool TOP, int SETS>
@@ -644,23 +557,12 @@ static attt_status launch_few(const attt_bf16 *d_h, int64_t h_ld, const attt_bf1
     f.stages = kFewMaxStages;
     const size_t smem = 1024 + (size_t)f.stages * few_stage_bytes(SETS) + 8 * (2 * f.stages + 5) + 16;
     if (!set_smem_limit(reinterpret_cast<const void *>(kern), smem, dev)) return ATTT_ERR_CUDA;
-    const int ctas = std::min({f.tiles, num_sms(dev), kFewSets});
+    const int ctas = std::min({f.tiles, num_sms(dev), kLpUnits});
     kern<<<ctas, few_threads(SETS), smem, stream>>>(tw, th, f);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) return ATTT_ERR_CUDA;
     a.nsets = ctas;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)f.L);
-    cfg.blockDim = dim3(kLpWarps * 32);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, logprob_few_reduce_kernel<TOP>, a) != cudaSuccess) return ATTT_ERR_CUDA;
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
+    return launch_reduce<TOP>(a, stream);
 }
 
 template <int EPI>
@@ -731,26 +633,26 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
     int *status = device_status_word(dev);
     if (!status) return ATTT_ERR_CUDA;
     const LpLayout c = lp_layout(d_ws, L, d, V, topk);
-    if (c.few) {
+    LpReduceArgs a{};
+    a.part = c.part; a.ztgt = c.ztgt; a.top_v = c.top_v; a.top_i = c.top_i; a.plane = c.plane;
+    a.rows = (int)L; a.V = (int)V; a.topk = topk; a.top_ld = (int)c.ld; a.inv_temp = inv_temp;
+    a.tgt = d_tgt; a.logp = d_logp; a.entropy = d_entropy; a.lse = d_lse; a.top_logp = d_top_logp;
+    a.top_id = d_top_id; a.status = status;
+    if (L <= kFewRows) {
         FewArgs f{};
         f.L = (int)L; f.V = (int)V; f.topk = topk; f.c2 = inv_temp * kLog2e;
         f.tgt = d_tgt; f.ztgt = c.ztgt; f.part = c.part; f.top_v = c.top_v; f.top_i = c.top_i; f.status = status;
-        LpReduceArgs a{};
-        a.part = c.part; a.ztgt = c.ztgt; a.top_v = c.top_v; a.top_i = c.top_i; a.plane = c.plane;
-        a.rows = (int)L; a.V = (int)V; a.topk = topk; a.top_ld = (int)c.ld; a.inv_temp = inv_temp;
-        a.tgt = d_tgt; a.logp = d_logp; a.entropy = d_entropy; a.lse = d_lse; a.top_logp = d_top_logp;
-        a.top_id = d_top_id; a.status = status;
         if (topk > 0)
             return L <= 16 ? launch_few<true, 1>(d_h, h_ld, d_W, d, f, a, dev, stream)
                            : launch_few<true, 2>(d_h, h_ld, d_W, d, f, a, dev, stream);
         return L <= 16 ? launch_few<false, 1>(d_h, h_ld, d_W, d, f, a, dev, stream)
                        : launch_few<false, 2>(d_h, h_ld, d_W, d, f, a, dev, stream);
     }
-    const int sets = lp_sets(d);
-    for (int64_t r0 = 0; r0 < L; r0 += c.rows) {
-        const int64_t R = L - r0 < c.rows ? L - r0 : c.rows;
-        TilePlan t = plan_tiles(R, V, cdiv(d, 64), num_sms(dev), 0, false, false);
-        while (t.BN < 256 && cdiv(V, t.BN) * sets * R > c.plane) t.BN += 64;
+    const int sms = num_sms(dev);
+    const int64_t rows = lp_forward_rows(L, d);
+    for (int64_t r0 = 0; r0 < L; r0 += rows) {
+        const int64_t R = std::min(rows, L - r0);
+        const TilePlan t = plan_tiles(R, V, cdiv(d, 64), sms, 0, false, false);
         GemmProblem p{};
         p.a = d_h + r0 * h_ld; p.a_rows_ld = h_ld; p.a_rows = R; p.a_k = d;
         p.b = d_W; p.b_rows_ld = d; p.b_rows = V; p.b_k = d;
@@ -760,14 +662,14 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
         ep.lp_part = c.part; ep.lp_plane = c.plane;
         ep.top_v = c.top_v; ep.top_i = c.top_i; ep.top_ld = (int)c.ld;
         ep.inv_temp = inv_temp;
-        st = topk == 0  ? launch_logits<EPI_LOGP>(p, ep, sets, dev, stream)
-             : topk <= 8 ? launch_logits<EPI_LOGP_TOP8>(p, ep, sets, dev, stream)
-                         : launch_logits<EPI_LOGP_TOP20>(p, ep, sets, dev, stream);
-        if (st != ATTT_OK) return st;
-        LpReduceArgs a{};
-        a.part = c.part; a.ztgt = c.ztgt; a.top_v = c.top_v; a.top_i = c.top_i; a.plane = c.plane;
-        a.nsets = (int)cdiv(V, t.BN / sets); a.rows = (int)R; a.V = (int)V; a.topk = topk; a.top_ld = (int)c.ld;
-        a.inv_temp = inv_temp;
+        ep.lp_split = a.split = R > (t.pair ? 256 : 128) && 2 * d * V > kLpHeadBytes;
+        a.rows = (int)R;
+        a.sets = lp_sets(d);
+        a.tile_rows = t.pair ? 256 : 128;
+        a.tiles_n = (int)cdiv(V, t.BN);
+        a.nwork = (int)cdiv(R, a.tile_rows) * a.tiles_n;
+        a.units = std::min(a.nwork, t.pair ? sms / 2 : sms);  // as launch_gemm has it
+        if (a.nwork > a.units * a.tiles_n) return ATTT_ERR_UNSUPPORTED;  // runs longer than a row (fewer SMs than 128)
         a.tgt = ep.tgt;
         a.logp = d_logp ? d_logp + r0 : nullptr;
         a.entropy = d_entropy ? d_entropy + r0 : nullptr;
@@ -776,10 +678,11 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
             a.top_logp = d_top_logp + r0 * topk;
             a.top_id = d_top_id + r0 * topk;
         }
-        a.status = status;
-        st = topk == 0  ? launch_reduce<0>(a, dev, stream)
-             : topk <= 8 ? launch_reduce<8>(a, dev, stream)
-                         : launch_reduce<20>(a, dev, stream);
+        st = topk == 0   ? launch_logits<EPI_LOGP>(p, ep, a.sets, dev, stream)
+             : topk == 1 ? launch_logits<EPI_LOGP_TOP1>(p, ep, a.sets, dev, stream)
+             : topk <= 8 ? launch_logits<EPI_LOGP_TOP8>(p, ep, a.sets, dev, stream)
+                         : launch_logits<EPI_LOGP_TOP20>(p, ep, a.sets, dev, stream);
+        if (st == ATTT_OK) st = topk > 0 ? launch_reduce<true>(a, stream) : launch_reduce<false>(a, stream);
         if (st != ATTT_OK) return st;
     }
     return ATTT_OK;

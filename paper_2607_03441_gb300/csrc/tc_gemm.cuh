@@ -36,14 +36,19 @@ enum EpiKind : int {
     EPI_BF16 = 5,      // out16[m, n] = bf16(alpha * acc)  (row-major, through TMA boxes)
     EPI_F32_PART = 3,  // K piece of every tile: its fp32 accumulator to the piece's region of `out` (split_reduce.cu)
     EPI_KL = 6,        // A tile = 64 rows of A over the same 64 rows of A2: per (row, tile) max, sum of exp, cross term
-    EPI_LOGP = 7,      // per (row, column set): max, sum of exp, its first moment, target logit
-    EPI_LOGP_TOP8 = 8,    // the same with the set's 8 largest logits
-    EPI_LOGP_TOP20 = 9,   // the same with the set's 20 largest logits
-    EPI_LOGP_GRAD = 10,   // gradient block of log probabilities and entropies, bf16
+    EPI_LOGP = 7,      // per row and run of tiles: max, sum of exp, its first moment, target logit
+    EPI_LOGP_TOP1 = 8,    // the same with the run's largest logit
+    EPI_LOGP_TOP8 = 9,    // its 8 largest
+    EPI_LOGP_TOP20 = 10,  // its 20 largest
+    EPI_LOGP_GRAD = 11,   // gradient block of log probabilities and entropies, bf16
 };
 
-// Largest logits that a log-probability epilogue keeps per row and column set.
-__host__ __device__ constexpr int epi_top(int epi) { return epi == EPI_LOGP_TOP8 ? 8 : epi == EPI_LOGP_TOP20 ? 20 : 0; }
+// Largest logits that a log-probability epilogue keeps per row.
+__host__ __device__ constexpr int epi_top(int epi) {
+    return epi == EPI_LOGP_TOP1 ? 1 : epi == EPI_LOGP_TOP8 ? 8 : epi == EPI_LOGP_TOP20 ? 20 : 0;
+}
+// Epilogues that keep a row's state in registers from tile to tile: their units take runs
+// of tiles along the rows' columns (work_run).
 __host__ __device__ constexpr bool epi_logp(int epi) { return epi >= EPI_LOGP && epi <= EPI_LOGP_TOP20; }
 // Epilogues that write a bf16 block G through staged TMA stores.
 __host__ __device__ constexpr bool epi_block(int epi) { return epi == EPI_CE_EXP || epi == EPI_LOGP_GRAD; }
@@ -76,10 +81,11 @@ struct EpiParams {
     // EPI_KL: five planes of [tiles, M] fp32 (m_p, s_p, m_q, s_q, x), kl_plane apart
     float *kl_part;
     int64_t kl_plane;
-    // EPI_LOGP*: three planes of [column sets, M] fp32 (max, sum, moment), lp_plane
-    // apart, and [column sets, M, top_ld] values and ids (tgt, ztgt as for CE)
+    // EPI_LOGP*: three planes of [run slots x sets, M] fp32 (max, sum, moment), lp_plane
+    // apart, and [run slots x sets, M, top_ld] values and ids (tgt, ztgt as for CE)
     float *lp_part;
     int64_t lp_plane;
+    int lp_split;  // runs go to their row's boundaries first (Span)
     float *top_v;
     int32_t *top_i;
     int top_ld;  // a multiple of 4
@@ -202,6 +208,58 @@ __host__ __device__ __forceinline__ Work work_item(const GemmArgs &g, int w, int
 
 __host__ __device__ __forceinline__ int work_count(const GemmArgs &g, int tiles_m) {
     return g.whole_tiles + (tiles_m * g.tiles_n - g.whole_tiles) * g.tail_s;
+}
+
+// EPI_LOGP*: unit `unit` of `units` takes the tiles [work_run(unit), work_run(unit + 1)) of
+// `nwork` in the order of rows of tiles, so that a row's state stays in the unit's
+// registers along its columns.  Row tile tm's runs belong to consecutive units from
+// run_unit(first tile of tm) on.
+__host__ __device__ __forceinline__ int work_run(int nwork, int unit, int units) {
+    return (int)((int64_t)nwork * unit / units);
+}
+__host__ __device__ __forceinline__ int run_unit(int nwork, int w, int units) {
+    return (int)((((int64_t)w + 1) * units - 1) / nwork);
+}
+
+// The work of one unit, i = begin, begin + step, .. < end.  For EPI_LOGP*, whose runs are
+// at most a row of tiles long, i counts up to three stretches of the run: the `next` tiles
+// that lie in the following row, then the tiles from column `split` on, then those before
+// it.  `split` is where the first row's runs have a boundary, so that the runs of all rows
+// are at the same columns at about the same time, and a B that L2 does not hold is read
+// once (2,282 rows x 4,480 through 22,402, 8 largest: 339 us with every run from its start
+// on, 270 so).  A small B is in L2 anyhow, and a second stretch begins its lists anew
+// (2,940 x 752 through 13,323: 139 us with the 20 largest, 170 so): no split then.
+struct Span {
+    int begin, end, step;
+    int next, high, w_next, w_high, w_low;
+};
+template <int EPI>
+__device__ __forceinline__ Span work_span(const GemmArgs &g, int nwork, int unit, int units) {
+    Span s{unit, nwork, units, 0, 0, 0, 0, 0};
+    if constexpr (epi_logp(EPI)) {
+        const int b = work_run(nwork, unit, units), e = work_run(nwork, unit + 1, units);
+        const int row = b / g.tiles_n * g.tiles_n, mid = min(e, row + g.tiles_n);
+        const int k = run_unit(nwork, b - row, units);
+        int split = work_run(nwork, k, units) == b - row ? b : row + work_run(nwork, k + 1, units);
+        if (split >= mid || !g.ep.lp_split) split = b;
+        s = Span{0, e - b, 1, e - mid, mid - split, mid, split, b};
+    }
+    return s;
+}
+template <int EPI>
+__device__ __forceinline__ Work work_tile(const GemmArgs &g, const Span &s, int i, int tiles_m) {
+    if constexpr (epi_logp(EPI)) {
+        const int j = i - s.next;
+        const int w = j < 0 ? s.w_next + i : j < s.high ? s.w_high + j : s.w_low + j - s.high;
+        Work k;
+        k.tm = w / g.tiles_n;
+        k.tn = w - k.tm * g.tiles_n;
+        k.kb0 = 0;
+        k.kb1 = g.kb_total;
+        k.piece = k.tail = -1;
+        return k;
+    }
+    return work_item(g, i, tiles_m);
 }
 
 // EPI_F32_PART: first row of a piece's region in the matrix of partials, for
@@ -537,16 +595,30 @@ struct TopList {
     }
 };
 
-// EPI_LOGP*: one pass over the set's columns, 32 at a time, with a running max.
-// With z the accumulator, c = log2 e / T, m the max: s = sum 2^((z - m) c) and
-// t = sum 2^((z - m) c) (z - m) c, so that lse = m / T + ln s and the entropy is
-// ln s - ln 2 t / s, both without a difference of large numbers.  A block's terms
-// are formed as 2^(z c - m2) with m2 = fl(m c), one FMA each, and what m2 was
-// rounded by is taken out of the sums.  -inf (also of columns past N) adds 0 to both
-// sums; NaN reaches s.  K > 0: a block's largest value joins the row's list as long
-// as it beats the list's least one; what it costs is instructions, not loads.
+// What a run keeps of a row.  With z the accumulator, c = log2 e / T, m the max so far:
+// s = sum 2^((z - m) c) and t = sum 2^((z - m) c) (z - m) c, so that lse = m / T + ln s and
+// the entropy is ln s - ln 2 t / s, both without a difference of large numbers.
+template <int K>
+struct LogpState {
+    float m, s, t;
+    TopList<K> top;
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        s = t = 0.f;
+        top.clear();
+    }
+};
+
+// EPI_LOGP*: one pass over the set's columns of a tile, 32 at a time, into the row's
+// state.  A block's terms are formed as 2^(z c - m2) with m2 = fl(m c), one FMA each, and
+// what m2 was rounded by is taken out of the sums.  -inf (also of columns past N) adds 0
+// to both sums; NaN reaches s.  K > 0: a block's largest value joins the row's list as long
+// as it beats the list's least one; a run goes along the row, so after its first tile
+// few do (2,940 rows x 752 through 13,323: 134 us the call with the largest one and lists
+// kept per tile, 64 kept per run; 313 and 144 with the 20 largest, 48 and 47 without).
 template <int K, int SETS>
-__device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn, int set, uint32_t taddr) {
+__device__ __forceinline__ void epilogue_logp(const GemmArgs &g, LogpState<K> &st, int gm, int tn, int set,
+                                              uint32_t taddr) {
     const EpiParams &ep = g.ep;
     const bool rv = gm < g.M;
     const int n_base = tn * g.BN;
@@ -554,10 +626,6 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn,
     const int n_end = min(g.N, n_base + c1);
     const float c2 = ep.inv_temp * kLog2e;
     const int t = ep.tgt && rv ? __ldg(ep.tgt + gm) : -1;
-    TopList<K> top;
-    top.clear();
-    float m = -INFINITY, s = 0.f, mom = 0.f, zt = 0.f;
-    bool hit = false;
     for (int c = c0; c < c1 && n_base + c < n_end; c += 32) {
         float v[32];
         tmem_ld_x32(taddr + (uint32_t)c, v);
@@ -568,11 +636,12 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn,
                 if (col0 + i >= n_end) v[i] = -INFINITY;
         }
         const int tc = t - col0;
-        if (tc >= 0 && tc < 32 && t < n_end) {
-            hit = true;
+        if (tc >= 0 && tc < 32 && t < n_end && ep.ztgt) {
+            float zt = 0.f;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (tc == i) zt = v[i];
+            ep.ztgt[gm] = zt;
         }
         float b4[4];
 #pragma unroll
@@ -580,7 +649,7 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn,
 #pragma unroll
         for (int i = 4; i < 32; ++i) b4[i & 3] = fmaxf(b4[i & 3], v[i]);
         float bm = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]));
-        const float mn = fmaxf(m, bm);
+        const float mn = fmaxf(st.m, bm);
         const float ref = mn == -INFINITY ? 0.f : mn, m2 = ref * c2;
         float s4[4] = {0.f, 0.f, 0.f, 0.f}, t4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -595,23 +664,24 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn,
         float bs = (s4[0] + s4[1]) + (s4[2] + s4[3]), bt = (t4[0] + t4[1]) + (t4[2] + t4[3]);
         bt = rs * fmaf(-r, bs, bt);
         bs *= rs;
-        if (m == mn || m == -INFINITY) {
-            s += bs;
-            mom += bt;
+        if (st.m == mn || st.m == -INFINITY) {
+            st.s += bs;
+            st.t += bt;
         } else {
-            const float dm = (m - mn) * c2, f = ex2(dm);
-            mom = fmaf(f, fmaf(s, fmaxf(dm, -1e4f), mom), bt);
-            s = fmaf(s, f, bs);
+            const float dm = (st.m - mn) * c2, f = ex2(dm);
+            st.t = fmaf(f, fmaf(st.s, fmaxf(dm, -1e4f), st.t), bt);
+            st.s = fmaf(st.s, f, bs);
         }
-        m = mn;
+        st.m = mn;
         if constexpr (K > 0) {
             if (!rv) bm = -INFINITY;
-            while (bm > top.least()) {
+            while (bm > st.top.least()) {
                 int at = 31;
 #pragma unroll
                 for (int i = 30; i >= 0; --i)
                     if (v[i] == bm) at = i;
-                top.insert(bm, col0 + at);
+                st.top.insert(bm, col0 + at);
+                if constexpr (K == 1) break;  // none of the block beats it
                 float nx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
@@ -623,23 +693,50 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, int gm, int tn,
             __syncwarp();
         }
     }
-    if (!rv || n_base + c0 >= g.N) return;
-    const int64_t o = (int64_t)(SETS * tn + set) * g.M + gm;
-    if (!ATTT_GUARD(o < ep.lp_plane, g.status)) return;
-    ep.lp_part[o] = m;
-    ep.lp_part[ep.lp_plane + o] = s;
-    ep.lp_part[2 * ep.lp_plane + o] = mom;
-    if (hit && ep.ztgt) ep.ztgt[gm] = zt;
-    if constexpr (K > 0) {
+}
+
+// The row's state into its slot.
+template <int K, int SETS>
+__device__ __forceinline__ void logp_store(const GemmArgs &g, LogpState<K> &st, int gm, int slot, int set) {
+    const EpiParams &ep = g.ep;
+    const int64_t o = (int64_t)(SETS * slot + set) * g.M + gm;
+    if (gm < g.M && ATTT_GUARD(o < ep.lp_plane, g.status)) {
+        ep.lp_part[o] = st.m;
+        ep.lp_part[ep.lp_plane + o] = st.s;
+        ep.lp_part[2 * ep.lp_plane + o] = st.t;
+        if constexpr (K == 1) {
+            ep.top_v[o * ep.top_ld] = st.top.v[0];
+            ep.top_i[o * ep.top_ld] = st.top.id[0];
+        } else if constexpr (K > 0) {
 #pragma unroll
-        for (int j = 0; j < K; j += 4)
-            if (j < ep.top_ld) {
-                *reinterpret_cast<float4 *>(ep.top_v + o * ep.top_ld + j) =
-                    make_float4(top.v[j], top.v[j + 1], top.v[j + 2], top.v[j + 3]);
-                *reinterpret_cast<int4 *>(ep.top_i + o * ep.top_ld + j) =
-                    make_int4(top.id[j], top.id[j + 1], top.id[j + 2], top.id[j + 3]);
-            }
+            for (int j = 0; j < K; j += 4)
+                if (j < ep.top_ld) {
+                    *reinterpret_cast<float4 *>(ep.top_v + o * ep.top_ld + j) =
+                        make_float4(st.top.v[j], st.top.v[j + 1], st.top.v[j + 2], st.top.v[j + 3]);
+                    *reinterpret_cast<int4 *>(ep.top_i + o * ep.top_ld + j) =
+                        make_int4(st.top.id[j], st.top.id[j + 1], st.top.id[j + 2], st.top.id[j + 3]);
+                }
+        }
     }
+    st.clear();
+}
+
+// After tile i of a run: at the end of a stretch the row's state goes to its slot, which
+// is the unit's place among the row tile's units; with lp_split each has two places, the
+// second for the tiles before `split`, empty where there are none.
+template <int K, int SETS>
+__device__ __forceinline__ void logp_flush(const GemmArgs &g, const Span &s, LogpState<K> &st, int i, int nwork,
+                                           int unit, int units, int tm, int gm, int set) {
+    const bool last = i + 1 == s.end, next = i + 1 == s.next, high = i + 1 == s.next + s.high;
+    if (!last && !next && !high) return;
+    const int place = unit - run_unit(nwork, tm * g.tiles_n, units);
+    if (!g.ep.lp_split) {
+        logp_store<K, SETS>(g, st, gm, place, set);
+        return;
+    }
+    const bool low = last && !high && !next;
+    logp_store<K, SETS>(g, st, gm, 2 * place + (low ? 1 : 0), set);
+    if (next || (last && high)) logp_store<K, SETS>(g, st, gm, 2 * place + 1, set);
 }
 
 // EPI_LOGP_GRAD: with p = exp(z / T - lse), the gradient of sum_j a_j logp_j + b_j
@@ -916,6 +1013,7 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
     const uint32_t tmem_base = *tmem_slot;
 
     const int nwork = work_count(g, g.tiles_m);
+    const Span span = work_span<EPI>(g, nwork, blockIdx.x, gridDim.x);
 
     if (warp == 0) {
         if (elect_one()) {
@@ -926,8 +1024,8 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
             uint32_t phase = 0;
             uint32_t issued_mask = 0, issued_parity = 0;  // per stage: last issue pending?
             bool ok = true;
-            for (int w = blockIdx.x; w < nwork && ok; w += gridDim.x) {
-                const Work wi = work_item(g, w, g.tiles_m);
+            for (int w = span.begin; w < span.end && ok; w += span.step) {
+                const Work wi = work_tile<EPI>(g, span, w, g.tiles_m);
                 const int tm = wi.tm, tn = wi.tn;
                 for (int kb = wi.kb0; kb < wi.kb1; ++kb) {
                     if (!mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
@@ -982,8 +1080,8 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
             uint32_t phase = 0;
             int it = 0;
             bool ok = true, ready = false;
-            for (int w = blockIdx.x; w < nwork && ok; w += gridDim.x, ++it) {
-                const Work wi = work_item(g, w, g.tiles_m);
+            for (int w = span.begin; w < span.end && ok; w += span.step, ++it) {
+                const Work wi = work_tile<EPI>(g, span, w, g.tiles_m);
                 const int kb0 = wi.kb0, kb1 = wi.kb1;
                 const int acc = it & 1;
                 if (!mbar_wait(tempty0 + 8 * acc, (((uint32_t)it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -1031,9 +1129,11 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
         const int row = q * 32 + lane;
         F32Stage fst{smem_u32(sE) + (uint32_t)q * 8192u, smem_u32(sE) + 32768u + (uint32_t)q * 16u, 0u};
         uint32_t bec = 0;  // bf16 blocks stored by this warp (picks its staging buffer)
+        [[maybe_unused]] LogpState<epi_top(EPI)> logp;
+        logp.clear();
         int it = 0;
-        for (int w = blockIdx.x; w < nwork; w += gridDim.x, ++it) {
-            const Work wi = work_item(g, w, g.tiles_m);
+        for (int w = span.begin; w < span.end; w += span.step, ++it) {
+            const Work wi = work_tile<EPI>(g, span, w, g.tiles_m);
             const int acc = it & 1;
             const uint32_t par = ((uint32_t)it >> 1) & 1u;
             int ok = 1;
@@ -1065,7 +1165,9 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
             } else if constexpr (EPI == EPI_BF16) {
                 epilogue_bf16(g, wi, wi.tm * 128, 0, 1, row, taddr, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else if constexpr (epi_logp(EPI)) {
-                epilogue_logp<epi_top(EPI), SETS>(g, wi.tm * 128 + row, wi.tn, set, taddr);
+                epilogue_logp<epi_top(EPI), SETS>(g, logp, wi.tm * 128 + row, wi.tn, set, taddr);
+                logp_flush<epi_top(EPI), SETS>(g, span, logp, w, nwork, blockIdx.x, gridDim.x, wi.tm,
+                                               wi.tm * 128 + row, set);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
                 epilogue_logp_grad<SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);
@@ -1163,6 +1265,7 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
     const int tiles_m2 = (g.tiles_m + 1) / 2;
     const int nwork = work_count(g, tiles_m2);
     const int cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+    const Span span = work_span<EPI>(g, nwork, cid, ncl);
     const uint32_t lead_full0 = mapa_shared(full0, 0);
     const uint32_t lead_tempty0 = mapa_shared(tempty0, 0);
 
@@ -1177,8 +1280,8 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
             uint32_t phase = 0;
             uint32_t issued_mask = 0, issued_parity = 0;  // leader: stages whose bytes it expects
             bool ok = true;
-            for (int w = cid; w < nwork && ok; w += ncl) {
-                const Work wi = work_item(g, w, tiles_m2);
+            for (int w = span.begin; w < span.end && ok; w += span.step) {
+                const Work wi = work_tile<EPI>(g, span, w, tiles_m2);
                 // EPI_KL: 64 rows of A and the same 64 rows of A2 per CTA
                 const int arow0 = EPI == EPI_KL ? wi.tm * 128 + 64 * (int)rank : wi.tm * 256 + 128 * (int)rank;
                 const int brow0 = wi.tn * g.BN + BNh * (int)rank;
@@ -1245,8 +1348,8 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
             uint32_t phase = 0;
             int it = 0;
             bool ok = true, ready = false;
-            for (int w = cid; w < nwork && ok; w += ncl, ++it) {
-                const Work wi = work_item(g, w, tiles_m2);
+            for (int w = span.begin; w < span.end && ok; w += span.step, ++it) {
+                const Work wi = work_tile<EPI>(g, span, w, tiles_m2);
                 const int kb0 = wi.kb0, kb1 = wi.kb1;
                 const int acc = it & 1;
                 if (!mbar_wait(tempty0 + 8 * acc, (((uint32_t)it >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -1292,10 +1395,12 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
         const int row = q * 32 + lane;
         F32Stage fst{smem_u32(sE) + (uint32_t)q * 8192u, smem_u32(sE) + 32768u + (uint32_t)q * 16u, 0u};
         uint32_t bec = 0;  // bf16 blocks stored by this warp (picks its staging buffer)
+        [[maybe_unused]] LogpState<epi_top(EPI)> logp;
+        logp.clear();
         uint32_t kl_ck = 0;  // EPI_KL chunks handed over by this warp pair
         int it = 0;
-        for (int w = cid; w < nwork; w += ncl, ++it) {
-            const Work wi = work_item(g, w, tiles_m2);
+        for (int w = span.begin; w < span.end; w += span.step, ++it) {
+            const Work wi = work_tile<EPI>(g, span, w, tiles_m2);
             const int acc = it & 1;
             const uint32_t par = ((uint32_t)it >> 1) & 1u;
             int ok = 1;
@@ -1332,7 +1437,8 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
             } else if constexpr (EPI == EPI_BF16) {
                 epilogue_bf16(g, wi, gm_base, (int)rank, 2, row, taddr, &tmC, smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else if constexpr (epi_logp(EPI)) {
-                epilogue_logp<epi_top(EPI), SETS>(g, gm_base + row, wi.tn, set, taddr);
+                epilogue_logp<epi_top(EPI), SETS>(g, logp, gm_base + row, wi.tn, set, taddr);
+                logp_flush<epi_top(EPI), SETS>(g, span, logp, w, nwork, cid, ncl, wi.tm, gm_base + row, set);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
                 epilogue_logp_grad<SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);

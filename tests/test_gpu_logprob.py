@@ -54,6 +54,8 @@ CASES = [  # L, d, V, topk, inv_temp
     (1, 8, 1, 1, 1.0), (1, 64, 7, 7, 1.0), (2, 72, 63, 0, 0.5), (3, 64, 64, 5, 1.0), (31, 136, 65, 20, 2.0),
     (1, 512, 8192, 5, 1.0), (16, 512, 8191, 20, 1 / 0.7), (129, 128, 1000, 8, 1.0), (127, 1600, 257, 9, 1.0),
     (257, 64, 255, 1, 1.0), (300, 520, 5001, 12, 0.25), (513, 128, 2049, 20, 1.0), (1000, 64, 300, 3, 1.25),
+    # runs of tiles that end inside a row of tiles, begin inside one, or go over to the next
+    (700, 72, 15000, 5, 1.0), (2400, 264, 2100, 20, 0.5), (5000, 64, 700, 1, 1.0), (1111, 1608, 6000, 0, 1.0),
 ]
 
 
@@ -88,6 +90,24 @@ def test_alternatives_in_any_order_of_the_vocabulary(order):
         _close(g, w, what)
 
 
+@pytest.mark.parametrize("L,topk", [(1300, 20), (2100, 8), (1700, 1)])
+def test_equal_logits_over_many_rows(L, topk):
+    """Every logit of a row occurs 40 times: the lowest ids come first, wherever the runs
+    of tiles begin and end."""
+    V, d = 12000, 64
+    W = np.zeros((V, d))
+    W[:, 0], W[:, 1] = np.floor(-(np.arange(V) % 300) / 64), -(np.arange(V) % 300) % 64
+    h = np.zeros((L, d))
+    h[:, 0], h[:, 1] = 1, 1 / 64
+    h[::2] *= -1  # the least ones become the largest
+    tgt = np.full(L, 5, dtype=np.int32)
+    got = _run(h, W, tgt, topk, 1.0)
+    want = op.logprobs(h[:2], W, tgt[:2], topk)
+    assert np.array_equal(got[4], want[4][np.arange(L) % 2])
+    for g, w, what in zip(got[:4], want, ("logp", "entropy", "lse", "top_logp")):
+        _close(g, w[np.arange(L) % 2], what)
+
+
 def test_rows_of_wider_tensors_and_given_outputs():
     h, W, tgt = _inputs(5, 37, 96, 700)
     wide = torch.full((37, 200), float("nan"), dtype=torch.bfloat16, device=DEV)
@@ -102,8 +122,7 @@ def test_rows_of_wider_tensors_and_given_outputs():
 
 
 def test_row_blocks():
-    """A call whose rows exceed one block of the workspace (20 alternatives of
-    72 column sets: 12,384 bytes a row) equals the calls on its parts."""
+    """A call of more rows than one block takes equals the calls on its parts."""
     L, d, V = 90000, 8, 9000
     g = torch.Generator(device=DEV).manual_seed(3)
     h = (torch.randn(L, d, generator=g, device=DEV) * 8).round().clamp(-32, 32).div(8).to(torch.bfloat16)
