@@ -575,6 +575,7 @@ struct GradLayout {
     int64_t rows, ld;
     int regions;
     __nv_bfloat16 *G;
+    float *loss;
     float *split_ws;
     unsigned int *split_tick;
     size_t bytes;
@@ -588,6 +589,7 @@ static GradLayout grad_layout(void *ws, int64_t L, int64_t d, int64_t V) {
     c.regions = (int)(t2 < kLpSplitRegions ? t2 : kLpSplitRegions);
     Carve cv{static_cast<char *>(ws), 0};
     c.G = cv.take<__nv_bfloat16>((size_t)(c.rows * c.ld));
+    c.loss = cv.take<float>((size_t)c.rows);
     c.split_ws = cv.take<float>((size_t)c.regions * 128 * 256);
     c.split_tick = cv.take<unsigned int>((size_t)c.regions);
     c.bytes = (size_t)round_up((int64_t)cv.used, 256);
@@ -727,7 +729,7 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             ep.entropy = d_gent ? d_entropy + r0 : nullptr;
             ep.gent = d_gent ? d_gent + r0 : nullptr;
             ep.inv_temp = inv_temp; ep.V = (int)V;
-            ep.G = c.G; ep.G_ld = c.ld;
+            ep.G = c.G; ep.G_ld = c.ld; ep.lp_loss = c.loss;
             st = launch_logits<EPI_LOGP_GRAD>(p, ep, sets, dev, stream);
             if (st != ATTT_OK) return st;
         }
@@ -740,6 +742,8 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             p.split_ws = c.split_ws; p.split_tick = c.split_tick; p.split_regions = c.regions;
             EpiParams ep{};
             ep.out16 = reinterpret_cast<__nv_bfloat16 *>(d_dh) + r0 * d; ep.out_ld = d; ep.alpha = 1.0f;
+            ep.row_gamma = c.loss; ep.fix_tgt = d_tgt + r0; ep.fix_W = reinterpret_cast<const __nv_bfloat16 *>(d_W);
+            ep.fix_ld = d; ep.fix_V = (int)V;
             st = launch_planned<true, false, true>(p, ep, td, dev, stream);
             if (st != ATTT_OK) return st;
         }

@@ -32,10 +32,22 @@ __global__ void __launch_bounds__(kReduceThreads) split_reduce_kernel(const Spli
         const float4 v = __ldcg(src + p * step);
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
+    auto fix = [&](float4 &o) {
+        if (!a.row_gamma) return;
+        const float gam = __ldcg(a.row_gamma + row);
+        int t = __ldg(a.fix_tgt + row);
+        if (t < 0 || t >= a.fix_V) t = 0;
+        const uint2 u = __ldg(reinterpret_cast<const uint2 *>(a.fix_W + (int64_t)t * a.fix_ld + col));
+        const float2 w0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x));
+        const float2 w1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y));
+        o.x = fmaf(-gam, w0.x, o.x); o.y = fmaf(-gam, w0.y, o.y);
+        o.z = fmaf(-gam, w1.x, o.z); o.w = fmaf(-gam, w1.y, o.w);
+    };
     if constexpr (OUT16) {
-        __nv_bfloat162 o[2] = {__floats2bfloat162_rn(a.alpha * s.x, a.alpha * s.y),
-                               __floats2bfloat162_rn(a.alpha * s.z, a.alpha * s.w)};
-        *reinterpret_cast<uint2 *>(a.out16 + (int64_t)row * a.ld + col) = *reinterpret_cast<uint2 *>(o);
+        float4 o = make_float4(a.alpha * s.x, a.alpha * s.y, a.alpha * s.z, a.alpha * s.w);
+        fix(o);
+        __nv_bfloat162 b[2] = {__floats2bfloat162_rn(o.x, o.y), __floats2bfloat162_rn(o.z, o.w)};
+        *reinterpret_cast<uint2 *>(a.out16 + (int64_t)row * a.ld + col) = *reinterpret_cast<uint2 *>(b);
         return;
     }
     const float rb = a.row_beta ? __ldcg(a.row_beta + row) : 1.f;
@@ -47,16 +59,7 @@ __global__ void __launch_bounds__(kReduceThreads) split_reduce_kernel(const Spli
         o.x = fmaf(ra, p.x, o.x); o.y = fmaf(ra, p.y, o.y);
         o.z = fmaf(ra, p.z, o.z); o.w = fmaf(ra, p.w, o.w);
     }
-    if (a.row_gamma) {
-        const float gam = __ldcg(a.row_gamma + row);
-        int t = __ldg(a.fix_tgt + row);
-        if (t < 0 || t >= a.fix_V) t = 0;
-        const uint2 u = __ldg(reinterpret_cast<const uint2 *>(a.fix_W + (int64_t)t * a.fix_ld + col));
-        const float2 w0 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x));
-        const float2 w1 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y));
-        o.x = fmaf(-gam, w0.x, o.x); o.y = fmaf(-gam, w0.y, o.y);
-        o.z = fmaf(-gam, w1.x, o.z); o.w = fmaf(-gam, w1.y, o.w);
-    }
+    fix(o);
     *dst = o;
 }
 

@@ -33,7 +33,7 @@ namespace attt {
 enum EpiKind : int {
     EPI_CE_EXP = 0,    // per (row, vocab tile): max m, E = exp(z - m) as bf16, sum of E, target logit
     EPI_F32_ACC = 2,   // out[m, n] = (acc ? alpha_m out[m, n] : 0) + beta_m acc [- gamma_m W[t_m, n]]  (fp32)
-    EPI_BF16 = 5,      // out16[m, n] = bf16(alpha * acc)  (row-major, through TMA boxes)
+    EPI_BF16 = 5,      // out16[m, n] = bf16(alpha * acc - gamma_m W[t_m, n])  (row-major, through TMA boxes)
     EPI_F32_PART = 3,  // K piece of every tile: its fp32 accumulator to the piece's region of `out` (split_reduce.cu)
     EPI_KL = 6,        // A tile = 64 rows of A over the same 64 rows of A2: per (row, tile) max, sum of exp, cross term
     EPI_LOGP = 7,      // per row and run of tiles: max, sum of exp, its first moment, target logit
@@ -92,6 +92,7 @@ struct EpiParams {
     float inv_temp;
     // EPI_LOGP_GRAD: [M] each; gent nullptr: no entropy term
     const float *lse, *entropy, *glogp, *gent;
+    float *lp_loss;  // [M] bf16(x) - x of the given token's entry x; 0 without one
     int V;  // valid targets are below V (tgt, v0, G, G_ld, inv_temp as above)
 };
 
@@ -279,8 +280,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kCeRefJump = 64.f;
 constexpr int kCeMaxChunk = 1 << 18;
 
-// Per-row terms of EPI_F32_ACC for output row gm: ra, rb and, when the
-// epilogue subtracts gamma_m W[t_m, :], gamma and that row of W.
+// Per-row terms of EPI_F32_ACC and EPI_BF16 for output row gm: ra, rb (not EPI_BF16's)
+// and, when the epilogue subtracts gamma_m W[t_m, :], gamma and that row of W.
 struct AccRow {
     float ra, rb, gam;
     const __nv_bfloat16 *wrow;
@@ -434,14 +435,33 @@ template <class Src>
 __device__ __forceinline__ void bf16_tile_store(const GemmArgs &g, const CUtensorMap *tm, uint32_t sE, uint32_t &ec,
                                                 int lane, int y, int n_base, int n_end, Src &&src) {
     if (y >= g.M) return;  // every row of this warp lies past M (warp-uniform)
+    const AccRow a = acc_row(g.ep, y + lane, y + lane < g.M);
+    const __nv_bfloat16 *wrow = a.wrow;
+    const float gam = a.gam;
     for (int c = 0; c < g.BN; c += 32) {
         if (n_base + c >= n_end) break;
         float v[32];
         src(c, v);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= g.ep.alpha;
+        if (wrow) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (n_base + c + 8 * q >= n_end) break;
+                const uint4 u = __ldg(reinterpret_cast<const uint4 *>(wrow + n_base + c + 8 * q));
+                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x[i]));
+                    v[8 * q + 2 * i] = fmaf(-gam, f.x, v[8 * q + 2 * i]);
+                    v[8 * q + 2 * i + 1] = fmaf(-gam, f.y, v[8 * q + 2 * i + 1]);
+                }
+            }
+        }
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            __nv_bfloat162 b = __floats2bfloat162_rn(g.ep.alpha * v[i], g.ep.alpha * v[i + 1]);
+            __nv_bfloat162 b = __floats2bfloat162_rn(v[i], v[i + 1]);
             pk[i / 2] = *reinterpret_cast<uint32_t *>(&b);
         }
         e_block_store(tm, sE, (int)(ec++), lane, pk, n_base + c, y);
@@ -744,7 +764,10 @@ __device__ __forceinline__ void logp_flush(const GemmArgs &g, const Span &s, Log
 //   g = (a [v = t] - p (a + b (log p + H))) / T,
 // formed in fp32, rounded once to bf16 and stored as the block G that the second
 // contraction reads (relative errors of 2^-8 at most, independent over the
-// vocabulary: dh is off by 6e-4 of its norm, its own rounding to bf16 by 1.7e-3).
+// vocabulary).  What the given token's entry, a row's largest as a rule, loses
+// there goes to lp_loss, negative, and comes back in fp32 with the second contraction
+// (EPI_BF16's gamma): without it dh is off by 2.4e-3 of its norm, with it by 1.8e-3, of
+// which its own rounding to bf16 is 1.7e-3.
 // Columns past N within the tile are stored as zeros.  A row without a given token
 // (t < 0) has a = 0; an invalid target makes its row NaN.
 template <int SETS>
@@ -778,7 +801,7 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
             A = fmaf(b * ep.inv_temp, __ldg(ep.entropy + gm), at);
             B = b * ep.inv_temp;
         }
-        t -= ep.v0;
+        if ((t < 0 || t >= ep.V) && tn == 0 && set == 0) ep.lp_loss[gm] = 0.f;
     }
     for (int c = c0; c < c1; c += 32) {
         float v[32];
@@ -793,7 +816,10 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
         if (tc >= 0 && tc < 32) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                if (tc == i) v[i] += at;
+                if (tc == i) {
+                    v[i] += at;
+                    if (col0 + i < n_end) ep.lp_loss[gm] = __bfloat162float(__float2bfloat16_rn(v[i])) - v[i];
+                }
         }
         if (col0 + 32 > n_end) {
 #pragma unroll

@@ -227,6 +227,25 @@ def test_gradient(L, d, V, inv_temp, ent):
     assert abs((got * u).sum() - slope) <= bound
 
 
+@pytest.mark.parametrize("L,d,V", [(1, 64, 4000), (40, 1032, 4100), (300, 520, 12000)])
+def test_gradient_of_the_given_token_is_not_rounded(L, d, V):
+    """Weights halfway between two bf16 values: the given token's own term counts in
+    full, and dh is off by its own rounding (2^-8 of it) and by that of the other terms
+    (2^-8 of |a| / V |W|, and 1e-5 of their values) alone."""
+    h, W, tgt = _inputs(8, L, d, V, peaked=False)
+    h[:] = 0
+    tgt[:] = np.arange(L) * 7 % V
+    a = np.where(np.arange(L) % 2 == 0, 1 + 2.0 ** -8, -1 - 3 * 2.0 ** -8).astype(np.float32)
+    f = attt.attt_logprob_forward(_bf16(h), _bf16(W), torch.from_numpy(tgt).to(DEV))
+    dh = attt.attt_logprob_input_grad(_bf16(h), _bf16(W), torch.from_numpy(tgt).to(DEV), f[2],
+                                      torch.from_numpy(a).to(DEV))
+    want, _ = op.logprobs_grad(h, W, tgt, a, None, 1.0)
+    rest = np.abs(a)[:, None] / V * np.abs(W).sum(0)[None] * (2.0 ** -8 + 1e-5)
+    err = np.abs(dh.float().cpu().numpy() - want)
+    # 2^-17: the loss of the given token's term is itself an fp32 difference
+    assert (err <= 2.0 ** -8 * (np.abs(want) + rest) + rest + 2.0 ** -17 * np.abs(a[:, None] * W[tgt])).all()
+
+
 def test_gradient_rows_without_a_token_or_weight():
     h, W, tgt = _inputs(11, 40, 64, 900)
     a, b = _grads(2, 40)
