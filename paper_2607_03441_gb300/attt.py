@@ -208,10 +208,31 @@ def _rows_ptr(t: torch.Tensor, name: str) -> Tuple[int, int]:
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
     rows, cols = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), max(cols, 1)
     ld = t.stride(0) if rows > 1 else max(cols, 1)
     if (cols > 1 and t.stride(1) != 1) or ld < cols:
         raise ValueError(f"{name}: expected rows that are contiguous and do not overlap")
     return t.data_ptr(), ld
+
+
+def _rows_of(t: torch.Tensor, shape, dtype, name: str) -> Tuple[int, int]:
+    """_expect and _rows_ptr in one (each call of Python costs a tenth of a launch)."""
+    if t.shape != shape or t.dtype != dtype:
+        _expect(t, shape, dtype, name)
+    return _rows_ptr(t, name)
+
+
+_F32 = torch.float32
+
+
+def _f32_of(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
+    """_expect (float32) and _ptr in one."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != _F32:
+        _expect(t, shape, _F32, name)
+    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
 
 
 def _out_f32(t: Optional[torch.Tensor], shape, name: str, dev) -> torch.Tensor:
@@ -771,15 +792,15 @@ def attt_kl_drift(hp: torch.Tensor, hq: torch.Tensor, W: torch.Tensor, kl: Optio
 _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
 
 
-def _norm_check(x: torch.Tensor, gamma: torch.Tensor):
-    if x.dim() != 2:
-        raise ValueError(f"x: expected a 2-D [L, d] tensor, got shape {tuple(x.shape)}")
-    L, d = x.shape
-    dtype = _DTYPES.get(x.dtype)
-    if dtype is None:
-        raise ValueError(f"x: expected bfloat16 or float32, got {x.dtype}")
-    _expect(gamma, (d,), torch.float32, "gamma")
-    return L, d, dtype
+def _norm_check(x: torch.Tensor):
+    """(shape, type, the C ABI's name of it) of the rows of a layer norm."""
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2:
+        raise ValueError(f"x: expected a 2-D [L, d] tensor, got shape {tuple(shape)}")
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"x: expected bfloat16 or float32, got {dtype}")
+    return shape, dtype, code
 
 
 def attt_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None,
@@ -788,18 +809,19 @@ def attt_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: Optional
     """Layer norm of the rows of x (bf16 or fp32 [L, d], rows may lie inside wider
     ones), gamma and beta fp32 [d].  Returns (y, mean, rstd): y of x's type, fp32 [L]
     twice."""
-    L, d, dtype = _norm_check(x, gamma)
-    _expect(beta, (d,), torch.float32, "beta")
-    _expect(y, (L, d), x.dtype, "y")
+    shape, dtype, code = _norm_check(x)
+    L, d = shape
     if y is None:
-        y = torch.empty(L, d, dtype=x.dtype, device=x.device)
-    mean = _out_f32(mean, (L,), "mean", x.device)
-    rstd = _out_f32(rstd, (L,), "rstd", x.device)
+        y = torch.empty(L, d, dtype=dtype, device=x.device)
+    if mean is None:
+        mean = torch.empty(L, dtype=_F32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(L, dtype=_F32, device=x.device)
     px, x_ld = _rows_ptr(x, "x")
-    py, y_ld = _rows_ptr(y, "y")
+    py, y_ld = _rows_of(y, shape, dtype, "y")
     _check((_lib or load_library()).attt_layer_norm_forward(
-        px, x_ld, _ptr(gamma), _ptr(beta), L, d, eps, dtype, py, y_ld, _ptr(mean), _ptr(rstd), _stream(stream)),
-        "attt_layer_norm_forward")
+        px, x_ld, _f32_of(gamma, (d,), "gamma"), _f32_of(beta, (d,), "beta"), L, d, eps, code, py, y_ld,
+        _f32_of(mean, (L,), "mean"), _f32_of(rstd, (L,), "rstd"), _stream(stream)), "attt_layer_norm_forward")
     return y, mean, rstd
 
 
@@ -814,24 +836,24 @@ def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Ten
     """Gradients of the layer norm's x, gamma and beta from dy (bf16 or fp32 [L, d]),
     with the forward call's mean and rstd.  Returns (dx, dgamma, dbeta): dx of x's
     type, fp32 [d] twice."""
-    L, d, dtype = _norm_check(x, gamma)
-    dev = x.device
-    _expect(dy, (L, d), x.dtype, "dy")
-    _expect(mean, (L,), torch.float32, "mean")
-    _expect(rstd, (L,), torch.float32, "rstd")
-    _expect(dx, (L, d), x.dtype, "dx")
+    shape, dtype, code = _norm_check(x)
+    L, d = shape
     if dx is None:
-        dx = torch.empty(L, d, dtype=x.dtype, device=dev)
-    dgamma = _out_f32(dgamma, (d,), "dgamma", dev)
-    dbeta = _out_f32(dbeta, (d,), "dbeta", dev)
+        dx = torch.empty(L, d, dtype=dtype, device=x.device)
+    if dgamma is None:
+        dgamma = torch.empty(d, dtype=_F32, device=x.device)
+    if dbeta is None:
+        dbeta = torch.empty(d, dtype=_F32, device=x.device)
     if workspace is None:
-        workspace = torch.empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=dev)
-    pg, g_ld = _rows_ptr(dy, "dy")
+        workspace = torch.empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=x.device)
+    pg, g_ld = _rows_of(dy, shape, dtype, "dy")
     px, x_ld = _rows_ptr(x, "x")
-    po, o_ld = _rows_ptr(dx, "dx")
+    po, o_ld = _rows_of(dx, shape, dtype, "dx")
+    vec, col = (d,), (L,)
     _check((_lib or load_library()).attt_layer_norm_backward(
-        pg, g_ld, px, x_ld, _ptr(gamma), _ptr(mean), _ptr(rstd), L, d, dtype, po, o_ld, _ptr(dgamma), _ptr(dbeta),
-        _ptr(workspace), workspace.numel(), _stream(stream)), "attt_layer_norm_backward")
+        pg, g_ld, px, x_ld, _f32_of(gamma, vec, "gamma"), _f32_of(mean, col, "mean"), _f32_of(rstd, col, "rstd"), L, d,
+        code, po, o_ld, _f32_of(dgamma, vec, "dgamma"), _f32_of(dbeta, vec, "dbeta"), _ptr(workspace),
+        workspace.numel(), _stream(stream)), "attt_layer_norm_backward")
     return dx, dgamma, dbeta
 
 
