@@ -140,76 +140,86 @@ __device__ __forceinline__ void lp_row(const LpReduceArgs &a, int j, const LpPar
 // lane in order, and merges a tile's 32 new ones into them (sorted by 15 exchanges,
 // merged by 5) or, where at most two beat the least that counts, inserts those.  At the
 // end of the kernel a CTA's four warps merge, and one block per row merges the CTAs.
-// Through 152,064 x 3,584 with 5 alternatives one row takes 167 us (96% of the copy
+// Through 152,064 x 3,584 with 5 alternatives one row takes 165 us (98% of the copy
 // bandwidth; 228 with the row padded to 128 and the alternatives kept by its one lane),
-// 16 rows through 152,064 x 5,120 with 20 take 255 (90%; 307).
+// 16 rows through 152,064 x 5,120 with 20 take 236 (97%; 307).  A small head is bound by
+// the exchanges, each of which waits for the one before: those of four rows go side by
+// side, and so do the merges of a level (24 rows x 648 through 16,971 with 5: 22.5 us, 41
+// row by row and list by list).
 // ---------------------------------------------------------------------------
 
 constexpr int kFewMaxStages = 10;
 
-// Whether logit a of id i comes before b of j: larger, or equal and of a lower id (ids
-// as unsigned: -1, an empty place, comes last).
-__device__ __forceinline__ bool lp_before(float a, int i, float b, int j) {
-    return a > b || (a == b && (unsigned)i < (unsigned)j);
+// A place of a list: larger keys are larger logits, of equal ones the lower id.  Empty: -inf
+// and id -1, after every id.
+using LpKey = unsigned long long;
+constexpr LpKey kLpNone = 0x007fffffull << 32;
+__device__ __forceinline__ LpKey lp_key(float v, int id) {  // v not NaN
+    const uint32_t u = __float_as_uint(v + 0.f);  // -0 is equal to 0
+    return (LpKey)((int)u < 0 ? ~u : u | 0x80000000u) << 32 | ~(uint32_t)id;
+}
+__device__ __forceinline__ float lp_value(LpKey k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float((int)u < 0 ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int lp_id(LpKey k) { return (int)~(uint32_t)k; }
+
+// One compare-exchange of a warp-wide sort: the lane keeps the larger of its own and its
+// partner's (lane ^ o) where `first`, else the smaller.
+__device__ __forceinline__ void lp_exchange(LpKey &k, int o, bool first) {
+    const LpKey other = __shfl_xor_sync(0xffffffffu, k, o);
+    if ((other > k) == first) k = other;
 }
 
-// One compare-exchange of a warp-wide sort: the lane keeps the earlier of its own and
-// its partner's (lane ^ o) where `first`, else the later.
-__device__ __forceinline__ void lp_exchange(float &v, int &id, int o, bool first) {
-    const float ov = __shfl_xor_sync(0xffffffffu, v, o);
-    const int oi = __shfl_xor_sync(0xffffffffu, id, o);
-    if (lp_before(ov, oi, v, id) == first) {
-        v = ov;
-        id = oi;
-    }
-}
-
-// Sorts the warp's 32 values, lane 0 the first.
-__device__ __forceinline__ void lp_sort(float &v, int &id, int lane) {
+// Sorts the warp's 32 places, lane 0 the first.
+__device__ __forceinline__ void lp_sort(LpKey &v, int lane) {
 #pragma unroll
     for (int k = 2; k <= 32; k <<= 1)
 #pragma unroll
-        for (int o = k >> 1; o > 0; o >>= 1) lp_exchange(v, id, o, ((lane & o) == 0) == ((lane & k) == 0));
+        for (int o = k >> 1; o > 0; o >>= 1) lp_exchange(v, o, ((lane & o) == 0) == ((lane & k) == 0));
 }
 
-// (v, id): the first 32 of two sorted lists.
-__device__ __forceinline__ void lp_merge(float &v, int &id, float ov, int oi, int lane) {
-    ov = __shfl_xor_sync(0xffffffffu, ov, 31);
-    oi = __shfl_xor_sync(0xffffffffu, oi, 31);
-    if (lp_before(ov, oi, v, id)) {
-        v = ov;
-        id = oi;
+// v: the first 32 of two sorted lists.
+__device__ __forceinline__ void lp_merge(LpKey &v, LpKey o, int lane) {
+    o = __shfl_xor_sync(0xffffffffu, o, 31);
+    if (o > v) v = o;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) lp_exchange(v, s, (lane & s) == 0);
+}
+
+// Four lists and a tile's 32 logits for each, sorted and merged into them: exchanges of
+// one list wait for each other, those of four fill the time.  A call, not one copy per four
+// rows: a call of few tiles would spend its time on fetching them.
+struct LpKeys {
+    LpKey k[4];
+};
+__device__ __noinline__ LpKeys lp_sort_in(LpKeys l, LpKeys n, int lane) {
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int o = k >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) lp_exchange(n.k[r], o, ((lane & o) == 0) == ((lane & k) == 0));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const LpKey o = __shfl_xor_sync(0xffffffffu, n.k[r], 31);
+        if (o > l.k[r]) l.k[r] = o;
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) lp_exchange(v, id, o, (lane & o) == 0);
+    for (int s = 16; s > 0; s >>= 1)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lp_exchange(l.k[r], s, (lane & s) == 0);
+    return l;
 }
 
-// A tile's 32 logits (-inf or NaN: none) into the list, of which the first k count.
-__device__ __forceinline__ void lp_offer(float &lv, int &li, float v, int id, int k, int lane) {
-    unsigned mask = __ballot_sync(0xffffffffu, v > __shfl_sync(0xffffffffu, lv, k - 1));
-    if (__popc(mask) > 2) {
-        float nv = v > -INFINITY ? v : -INFINITY;  // NaN: none
-        int ni = v > -INFINITY ? id : -1;
-        lp_sort(nv, ni, lane);
-        lp_merge(lv, li, nv, ni, lane);
-        return;
-    }
-    while (mask) {  // ids come in order, so that equal ones already there stay before
-        const int from = __ffs(mask) - 1;
+// The places of `mask` of one tile's 32 into a list, one by one.
+__device__ __forceinline__ void lp_insert(LpKey &l, LpKey n, unsigned mask, int lane) {
+    while (mask) {
+        const LpKey k = __shfl_sync(0xffffffffu, n, __ffs(mask) - 1);
         mask &= mask - 1;
-        const float nv = __shfl_sync(0xffffffffu, v, from);
-        const int ni = __shfl_sync(0xffffffffu, id, from);
-        const int at = __popc(__ballot_sync(0xffffffffu, lv >= nv));
-        const float uv = __shfl_up_sync(0xffffffffu, lv, 1);
-        const int ui = __shfl_up_sync(0xffffffffu, li, 1);
-        if (lane > at) {
-            lv = uv;
-            li = ui;
-        }
-        if (lane == at) {
-            lv = nv;
-            li = ni;
-        }
+        const int at = __popc(__ballot_sync(0xffffffffu, l >= k));
+        const LpKey up = __shfl_up_sync(0xffffffffu, l, 1);
+        if (lane >= at) l = lane > at ? up : k;
     }
 }
 
@@ -330,15 +340,11 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
     } else {
         const int q = warp & 3, set = (warp - 2) >> 2, row0 = 16 * set, rows = min(16, a.L - row0);
         LpPart st[16];
-        float lv[TOP ? 16 : 1];
-        int li[TOP ? 16 : 1];
+        LpKeys top[TOP ? 4 : 1];
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
             st[t] = LpPart{-INFINITY, 0.f, 0.f};
-            if constexpr (TOP) {
-                lv[t] = -INFINITY;
-                li[t] = -1;
-            }
+            if constexpr (TOP) top[t / 4].k[t % 4] = kLpNone;
         }
         // the given token of row row0 + (lane & 15) in this lane
         const int given = a.tgt && (lane & 15) < rows ? __ldg(a.tgt + row0 + (lane & 15)) : -1;
@@ -365,67 +371,91 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
             if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
             const int id = w * 128 + q * 32 + lane;
 #pragma unroll
-            for (int t = 0; t < 16; ++t) {
-                if (t >= rows) break;  // warp-uniform
-                const float z = id < a.V ? v[t] : -INFINITY;
-                if (__shfl_sync(0xffffffffu, given, t) == id && id < a.V) a.ztgt[row0 + t] = z;
-                // the lane's running max moves to z, or z counts against it; -inf adds nothing, NaN
-                // reaches the sum
-                if (z != -INFINITY) {
-                    const bool above = z > st[t].m;
-                    const float d = (above ? st[t].m - z : z - st[t].m) * a.c2, e = ex2(d), dm = fmaxf(d, -1e4f);
-                    if (above) {
-                        st[t].t = e * fmaf(st[t].s, dm, st[t].t);
-                        st[t].s = fmaf(st[t].s, e, 1.f);
-                        st[t].m = z;
-                    } else {
-                        st[t].t = fmaf(e, dm, st[t].t);
-                        st[t].s += e;
+            for (int g = 0; g < 4; ++g) {
+                if (4 * g >= rows) break;  // warp-uniform
+                LpKeys n;
+                unsigned mask[4];
+                bool many = false;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = 4 * g + r;
+                    const float z = id < a.V && t < rows ? v[t] : -INFINITY;
+                    if (__shfl_sync(0xffffffffu, given, t) == id && id < a.V) a.ztgt[row0 + t] = z;
+                    // the lane's running max moves to z, or z counts against it; -inf adds nothing,
+                    // NaN reaches the sum
+                    if (z != -INFINITY) {
+                        const bool above = z > st[t].m;
+                        const float d = (above ? st[t].m - z : z - st[t].m) * a.c2, e = ex2(d), dm = fmaxf(d, -1e4f);
+                        if (above) {
+                            st[t].t = e * fmaf(st[t].s, dm, st[t].t);
+                            st[t].s = fmaf(st[t].s, e, 1.f);
+                            st[t].m = z;
+                        } else {
+                            st[t].t = fmaf(e, dm, st[t].t);
+                            st[t].s += e;
+                        }
+                    }
+                    __syncwarp();
+                    if constexpr (TOP) {  // those above the least that counts
+                        n.k[r] = z > -INFINITY ? lp_key(z, id) : kLpNone;
+                        mask[r] = __ballot_sync(0xffffffffu,
+                                                n.k[r] > __shfl_sync(0xffffffffu, top[g].k[r], a.topk - 1));
+                        many |= __popc(mask[r]) > 2;
                     }
                 }
-                __syncwarp();
-                if constexpr (TOP) lp_offer(lv[t], li[t], z, id, a.topk, lane);
+                if constexpr (TOP) {
+                    if (many) {
+                        top[g] = lp_sort_in(top[g], n, lane);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) lp_insert(top[g].k[r], n.k[r], mask[r], lane);
+                    }
+                }
             }
         }
         // the four warps of a set through shared memory: every MMA has completed, and with it
         // every load into the ring
-        float *sp = reinterpret_cast<float *>(smem) + set * 16 * 4 * 3;
-        float *sv = reinterpret_cast<float *>(smem) + SETS * 16 * 4 * 3 + set * 16 * 4 * 64;
+        LpPart *sp = reinterpret_cast<LpPart *>(smem) + set * 16 * 4;
+        LpKey *sk = reinterpret_cast<LpKey *>(smem + 2048) + set * 16 * 4 * 32;
+        // a lane's 16 sums over the warp: with every exchange half as many rows and twice as many
+        // lanes in each sum, until lanes 2 t and 2 t + 1 hold row t's
 #pragma unroll
-        for (int t = 0; t < 16; ++t) {
-            if (t >= rows) break;
+        for (int o = 16, n = 8; n > 0; o >>= 1, n >>= 1) {
+            const bool up = lane & o;
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) st[t].merge(st[t].shfl_xor(o), a.c2);
-            if (lane == 0) {
-                sp[(t * 4 + q) * 3] = st[t].m;
-                sp[(t * 4 + q) * 3 + 1] = st[t].s;
-                sp[(t * 4 + q) * 3 + 2] = st[t].t;
+            for (int t = 0; t < n; ++t) {
+                const LpPart mine = up ? st[t + n] : st[t];
+                st[t] = (up ? st[t] : st[t + n]).shfl_xor(o);
+                st[t].merge(mine, a.c2);
             }
-            if constexpr (TOP) {
-                sv[(t * 4 + q) * 64 + lane] = lv[t];
-                reinterpret_cast<int *>(sv)[(t * 4 + q) * 64 + 32 + lane] = li[t];
-            }
+        }
+        st[0].merge(st[0].shfl_xor(1), a.c2);
+        if ((lane & 1) == 0) sp[(lane >> 1) * 4 + q] = st[0];
+        if constexpr (TOP) {
+#pragma unroll
+            for (int t = 0; t < 16; ++t)
+                if (t < rows) sk[(t * 4 + q) * 32 + lane] = top[t / 4].k[t % 4];
         }
         named_barrier_sync(1u + set, 128);
         const int64_t plane = (int64_t)kLpUnits * a.L;
-        for (int t = q; t < rows; t += 4) {
-            const int64_t o = (int64_t)blockIdx.x * a.L + row0 + t;
-            if (lane == 0) {
-                LpPart p{-INFINITY, 0.f, 0.f};
-                for (int k = 0; k < 4; ++k)
-                    p.merge(LpPart{sp[(t * 4 + k) * 3], sp[(t * 4 + k) * 3 + 1], sp[(t * 4 + k) * 3 + 2]}, a.c2);
-                a.part[o] = p.m;
-                a.part[plane + o] = p.s;
-                a.part[2 * plane + o] = p.t;
-            }
-            if constexpr (TOP) {
-                float x = sv[t * 4 * 64 + lane];
-                int i = reinterpret_cast<int *>(sv)[t * 4 * 64 + 32 + lane];
-                for (int k = 1; k < 4; ++k)
-                    lp_merge(x, i, sv[(t * 4 + k) * 64 + lane], reinterpret_cast<int *>(sv)[(t * 4 + k) * 64 + 32 + lane],
-                             lane);
-                a.top_v[o * 32 + lane] = x;
-                a.top_i[o * 32 + lane] = i;
+        if (q == 0 && lane < rows) {
+            LpPart p = sp[lane * 4];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) p.merge(sp[lane * 4 + k], a.c2);
+            const int64_t o = (int64_t)blockIdx.x * a.L + row0 + lane;
+            a.part[o] = p.m;
+            a.part[plane + o] = p.s;
+            a.part[2 * plane + o] = p.t;
+        }
+        if constexpr (TOP) {
+            for (int t = q; t < rows; t += 4) {
+                const int64_t o = (int64_t)blockIdx.x * a.L + row0 + t;
+                LpKey x = sk[t * 4 * 32 + lane], y = sk[(t * 4 + 2) * 32 + lane];
+                lp_merge(x, sk[(t * 4 + 1) * 32 + lane], lane);
+                lp_merge(y, sk[(t * 4 + 3) * 32 + lane], lane);
+                lp_merge(x, y, lane);
+                a.top_v[o * 32 + lane] = lp_value(x);
+                a.top_i[o * 32 + lane] = lp_id(x);
             }
         }
     }
@@ -436,23 +466,21 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
 }
 
 // Merges a row's sets: WARPS warps per row, each every WARPS-th set, some at a time on
-// their way, then the first one the others' (ties of alternatives go to the lowest id,
-// sums are in a fixed order).  FEW: the sets of a call of few rows, one per CTA and each
-// with 32 alternatives, all on their way at once (13 rows through 33,364 x 3,368: 63 us the
-// call, 66 with the loops that other calls take).
+// their way, then the warps' in pairs (ties of alternatives go to the lowest id, sums are
+// in a fixed order).  FEW: the sets of a call of few rows, one per CTA and each with 32
+// alternatives, all on their way at once (13 rows through 33,364 x 3,368: 3 us of the call
+// against the loops that other calls take).
 template <bool TOP, int WARPS, bool FEW>
 __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpReduceArgs a) {
     __shared__ LpPart s_part[kLpWarps];
-    __shared__ float s_v[kLpWarps][32];
-    __shared__ int s_i[kLpWarps][32];
+    __shared__ LpKey s_top[TOP && WARPS > 1 ? kLpWarps : 1][32];
     griddep_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
     const int j = blockIdx.x * (kLpWarps / WARPS) + warp / WARPS;
     if (WARPS == 1 && j >= a.rows) return;  // (a block of one row always has it)
     const float c2 = a.inv_temp * kLog2e;
     LpPart p{-INFINITY, 0.f, 0.f};
-    float v = -INFINITY;
-    int id = -1;
+    LpKey top = kLpNone;
     if constexpr (FEW) {
         constexpr int kEach = kLpUnits / WARPS;
         const int t = w + lane * WARPS;
@@ -460,17 +488,19 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
         if (lane < kEach && t < a.nsets)
             p = LpPart{__ldcg(a.part + o), __ldcg(a.part + a.plane + o), __ldcg(a.part + 2 * a.plane + o)};
         if constexpr (TOP) {
-            float nv[kEach];
-            int ni[kEach];
+            LpKey n[kEach];
 #pragma unroll
             for (int k = 0; k < kEach; ++k) {
                 const int t = w + k * WARPS;
                 const int64_t o = ((int64_t)t * a.rows + j) * 32 + lane;
-                nv[k] = t < a.nsets ? __ldcg(a.top_v + o) : -INFINITY;
-                ni[k] = t < a.nsets ? __ldcg(a.top_i + o) : -1;
+                const float v = t < a.nsets ? __ldcg(a.top_v + o) : -INFINITY;
+                n[k] = lp_key(v, t < a.nsets ? __ldcg(a.top_i + o) : -1);
             }
 #pragma unroll
-            for (int k = 0; k < kEach; ++k) lp_merge(v, id, nv[k], ni[k], lane);
+            for (int h = 1; h < kEach; h *= 2)  // pairs of pairs: a level's merges do not wait for each other
+#pragma unroll
+                for (int k = 0; k + h < kEach; k += 2 * h) lp_merge(n[k], n[k + h], lane);
+            top = n[0];
         }
     } else {
         const int first = j / a.tile_rows * a.tiles_n;
@@ -482,18 +512,19 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
         }
         if constexpr (TOP) {
             for (int t0 = w; t0 < nsets; t0 += 4 * WARPS) {
-                float nv[4];
-                int ni[4];
+                LpKey n[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int t = t0 + k * WARPS;
                     const int64_t o = ((int64_t)t * a.rows + j) * a.top_ld + lane;
-                    nv[k] = lane < a.topk && t < nsets ? __ldcg(a.top_v + o) : -INFINITY;
-                    ni[k] = lane < a.topk && t < nsets ? __ldcg(a.top_i + o) : -1;
+                    const bool in = lane < a.topk && t < nsets;
+                    const float v = in ? __ldcg(a.top_v + o) : -INFINITY;
+                    n[k] = lp_key(v, in ? __ldcg(a.top_i + o) : -1);
                 }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (t0 + k * WARPS < nsets) lp_merge(v, id, nv[k], ni[k], lane);
+                lp_merge(n[0], n[1], lane);
+                lp_merge(n[2], n[3], lane);
+                lp_merge(n[0], n[2], lane);
+                lp_merge(top, n[0], lane);
             }
         }
     }
@@ -501,22 +532,28 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
     for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
     if constexpr (WARPS > 1) {
         if (lane == 0) s_part[warp] = p;
-        s_v[warp][lane] = v;
-        s_i[warp][lane] = id;
-        __syncthreads();
+        if constexpr (TOP) {
+            // half of the warps that hold a list take the other half's
+            for (int n = WARPS / 2; n > 0; n /= 2) {
+                s_top[warp][lane] = top;
+                __syncthreads();
+                if (warp < n) lp_merge(top, s_top[warp + n][lane], lane);
+                __syncthreads();
+            }
+        } else {
+            __syncthreads();
+        }
         if (w > 0) return;
-        p = lane < WARPS ? s_part[warp + lane] : LpPart{-INFINITY, 0.f, 0.f};
+        p = lane < WARPS ? s_part[lane] : LpPart{-INFINITY, 0.f, 0.f};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
-        if constexpr (TOP)
-            for (int k = 1; k < WARPS; ++k) lp_merge(v, id, s_v[warp + k][lane], s_i[warp + k][lane], lane);
     }
     const float ln = logf(p.s);
     if (lane == 0) lp_row(a, j, p, ln);
     if constexpr (TOP) {
         if (lane < a.topk) {
-            a.top_logp[(int64_t)j * a.topk + lane] = (v - p.m) * a.inv_temp - ln;
-            a.top_id[(int64_t)j * a.topk + lane] = id;
+            a.top_logp[(int64_t)j * a.topk + lane] = (lp_value(top) - p.m) * a.inv_temp - ln;
+            a.top_id[(int64_t)j * a.topk + lane] = lp_id(top);
         }
     }
 }
