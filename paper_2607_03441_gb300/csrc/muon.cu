@@ -415,6 +415,221 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
     cluster_sync();  // no CTA leaves while it is sent to
 }
 
+// ---------------------------------------------------------------------------
+// Ranks up to 5: matrices of no more elements than a warp has lanes.  With the Gram matrix
+// in twice 24 bits (pairs of fp32: T. J. Dekker, "A floating-point technique for extending
+// the available precision", 1971) nothing of the small singular values is lost, and every
+// step is taken on that one matrix: X_K = P X_0 with P formed in 64 bits by one warp, lane
+// i r + j its element i, j, and applied in pairs, since P has up to 3.44^K where X comes to
+// 1.  One exchange (128 bytes from each CTA to each) instead of six.  Over 138 matrices of
+// rank 4 the step is off the 64-bit one by 1.2e-7 as a rule and 3.7e-7 at most (the other
+// ranks' kernel: 3.3e-7 and 1e-6; element by element in fp32: up to 7e-7).  Two projections
+// of 3,584 at rank 5 take 16.5 us, 24.6 with the other ranks' kernel; seven of up to 5,120
+// at rank 4 18.5, 28.9.  Bound: launch, load and update, and 64-bit FMA issue (a warp's
+// takes some 60 cycles, which is why r 8 would gain nothing).
+// ---------------------------------------------------------------------------
+
+constexpr int kMuonLaneRank = 5, kMuonLaneSums = 16;  // 15 elements of a symmetric matrix, and one of 0
+
+// The value h + l.
+struct MuonPair {
+    float h, l;
+    __device__ __forceinline__ void add(float p, float e) {
+        const float s = __fadd_rn(h, p), v = __fadd_rn(s, -h);
+        l += __fadd_rn(__fadd_rn(h, -__fadd_rn(s, -v)), __fadd_rn(p, -v)) + e;
+        h = s;
+    }
+    // + (ah + al) x
+    __device__ __forceinline__ void add_product(float ah, float al, float x) {
+        const float p = __fmul_rn(ah, x);
+        add(p, __fmaf_rn(al, x, __fmaf_rn(ah, x, -p)));
+    }
+    __device__ __forceinline__ MuonPair shfl_xor(int o) const {
+        return MuonPair{__shfl_xor_sync(0xffffffffu, h, o), __shfl_xor_sync(0xffffffffu, l, o)};
+    }
+};
+
+// Place of element i <= j among the sums.
+__host__ __device__ constexpr int muon_lane_sum(int i, int j) { return i * kMuonLaneRank - i * (i - 1) / 2 + j - i; }
+
+struct MuonLaneShape {
+    static constexpr int RP = 8, LD = RP + 4;
+    static constexpr int oP = 0;                                   // 25 pairs
+    static constexpr int oWarps = 64;                              // [warps][sums] pairs
+    static constexpr int oOwn = oWarps + kMuonThreads / 32 * 2 * kMuonLaneSums;  // the CTA's sums
+    static constexpr int oRecv = oOwn + 2 * kMuonLaneSums;         // the others'
+    static constexpr int kFixed = oRecv + kMuonMaxCluster * 2 * kMuonLaneSums;
+};
+template <>
+struct MuonShape<8> : MuonLaneShape {};
+
+// Matrices in a warp's lanes.
+__device__ __forceinline__ double muon_lane_product(double x, double y, int r, int i, int j) {
+    double z = 0.;
+#pragma unroll
+    for (int k = 0; k < kMuonLaneRank; ++k) {
+        const double a = __shfl_sync(0xffffffffu, x, (i * r + k) & 31), b = __shfl_sync(0xffffffffu, y, (k * r + j) & 31);
+        if (k < r) z = fma(a, b, z);
+    }
+    return z;
+}
+
+__device__ __forceinline__ void muon_lane_gram(const float *s, int cols, MuonPair (&acc)[kMuonLaneSums]) {
+    for (int c = threadIdx.x; c < cols; c += kMuonThreads) {
+        const float4 a = *reinterpret_cast<const float4 *>(s + c * MuonLaneShape::LD);
+        const float x[kMuonLaneRank] = {a.x, a.y, a.z, a.w, s[c * MuonLaneShape::LD + 4]};
+#pragma unroll
+        for (int i = 0; i < kMuonLaneRank; ++i)
+#pragma unroll
+            for (int j = i; j < kMuonLaneRank; ++j) acc[muon_lane_sum(i, j)].add_product(x[i], 0.f, x[j]);
+    }
+}
+
+__device__ __forceinline__ void muon_lane_apply(float *s, int cols) {
+    const float2 *p = reinterpret_cast<const float2 *>(muon_smem(MuonLaneShape::oP));
+    for (int c = threadIdx.x; c < cols; c += kMuonThreads) {
+        float4 *at = reinterpret_cast<float4 *>(s + c * MuonLaneShape::LD);
+        const float4 a = *at;
+        const float x[kMuonLaneRank] = {a.x, a.y, a.z, a.w, s[c * MuonLaneShape::LD + 4]};
+        float y[kMuonLaneRank];
+#pragma unroll
+        for (int i = 0; i < kMuonLaneRank; ++i) {
+            MuonPair v{0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kMuonLaneRank; ++k) {
+                const float2 q = p[i * kMuonLaneRank + k];
+                v.add_product(q.x, q.y, x[k]);
+            }
+            y[i] = v.h + v.l;
+        }
+        *at = make_float4(y[0], y[1], y[2], y[3]);
+        s[c * MuonLaneShape::LD + 4] = y[4];
+    }
+}
+
+// One warp: the cluster's Gram matrix from the CTAs' sums, in rank order, and P (0 past r).
+__device__ __noinline__ void muon_lane_matrix(const MuonArgs &a, int rank) {
+    using S = MuonLaneShape;
+    const int lane = threadIdx.x & 31, r = a.r, e = min(lane, r * r - 1), i = e / r, j = e - i * r;
+    const float2 *own = reinterpret_cast<const float2 *>(muon_smem(S::oOwn)),
+                 *recv = reinterpret_cast<const float2 *>(muon_smem(S::oRecv));
+    MuonPair sum{0.f, 0.f};
+    for (int c = 0; c < a.cluster; ++c) {
+        const float2 q = c == rank ? own[lane & 15] : recv[c * kMuonLaneSums + (lane & 15)];
+        sum.add(q.x, q.y);
+    }
+    double g = __shfl_sync(0xffffffffu, (double)sum.h + (double)sum.l, muon_lane_sum(min(i, j), max(i, j)));
+    double v = 0.;
+    for (int k = 0; k < r; ++k) v += __shfl_sync(0xffffffffu, g, k * (r + 1));
+    const double scale = 1. / (sqrt(v) + (double)a.eps), diag = i == j ? kNsA64 : 0.;
+    g *= scale * scale;
+    double p = i == j ? scale : 0.;
+    for (int k = 0; k < a.steps; ++k) {
+        const double b = fma(kNsC64, muon_lane_product(g, g, r, i, j), fma(kNsB64, g, diag));
+        p = k == 0 ? b * scale : muon_lane_product(b, p, r, i, j);
+        if (k + 1 < a.steps) g = muon_lane_product(muon_lane_product(b, g, r, i, j), b, r, i, j);
+    }
+    float2 *out = reinterpret_cast<float2 *>(muon_smem(S::oP));
+    if (lane < kMuonLaneRank * kMuonLaneRank) out[lane] = make_float2(0.f, 0.f);
+    __syncwarp();
+    const float h = (float)p;
+    if (lane < r * r) out[i * kMuonLaneRank + j] = make_float2(h, (float)(p - (double)h));
+}
+
+template <bool STREAM>
+__global__ void __launch_bounds__(kMuonThreads, 1) muon_lane_kernel(const __grid_constant__ MuonArgs a) {
+    using S = MuonLaneShape;
+    constexpr int RP = S::RP, oX = S::kFixed;
+    __shared__ __align__(8) uint64_t s_bars[2];
+    __shared__ int s_abort;
+    float *const X = muon_smem(oX);
+    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const MuonMat &t = a.mat[blockIdx.x / a.cluster];
+    const int64_t c_begin = rank * t.per, c_end = min(t.n, c_begin + t.per);
+    const int64_t cols = c_end > c_begin ? c_end - c_begin : 0;
+    // the first columns stay; the others pass through the last kMuonStage places, twice
+    const int stay = (int)(!STREAM || cols <= a.room ? cols : a.room - kMuonStage);
+    const int o_stage = oX + (a.room - kMuonStage) * S::LD;
+    float *const stage = muon_smem(o_stage);
+    const MuonLink link{smem_u32(s_bars), a.cluster, rank, &s_abort, a.status};
+    if (threadIdx.x == 0) {
+        mbar_init(link.bar0, 1);
+        mbar_init(link.bar0 + 8u, 1);
+        s_abort = 0;
+        fence_mbar_init();
+    }
+    muon_load<RP>(a, t, oX, c_begin, stay, true);
+    cluster_sync();  // X is there, and the barriers of all CTAs
+    MuonPair acc[kMuonLaneSums];
+#pragma unroll
+    for (int i = 0; i < kMuonLaneSums; ++i) acc[i] = MuonPair{0.f, 0.f};
+    muon_lane_gram(X, stay, acc);
+    if constexpr (STREAM) {
+        for (int64_t c = stay; c < cols; c += kMuonStage) {
+            const int now = (int)min((int64_t)kMuonStage, cols - c);
+            muon_load<RP>(a, t, o_stage, c_begin + c, now, true);
+            __syncthreads();
+            muon_lane_gram(stage, now, acc);
+            __syncthreads();
+        }
+    }
+    // the warp's sums: with every exchange half as many in a lane, each of twice as many lanes,
+    // until lanes 2 e and 2 e + 1 hold sum e
+#pragma unroll
+    for (int o = 16, n = 8; n > 0; o >>= 1, n >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+            const MuonPair mine = up ? acc[k + n] : acc[k], other = (up ? acc[k] : acc[k + n]).shfl_xor(o);
+            acc[k] = mine;
+            acc[k].add(other.h, other.l);
+        }
+    }
+    const MuonPair other = acc[0].shfl_xor(1);
+    float2 *const warps = reinterpret_cast<float2 *>(muon_smem(S::oWarps));
+    // both lanes in the same order
+    MuonPair sum = lane & 1 ? other : acc[0];
+    const MuonPair second = lane & 1 ? acc[0] : other;
+    sum.add(second.h, second.l);
+    if ((lane & 1) == 0) warps[warp * kMuonLaneSums + (lane >> 1)] = make_float2(sum.h, sum.l);
+    __syncthreads();
+    if (warp == 0) {
+        sum = MuonPair{0.f, 0.f};
+#pragma unroll 4
+        for (int w = 0; w < kMuonThreads / 32; ++w) {
+            const float2 q = warps[w * kMuonLaneSums + (lane & 15)];
+            sum.add(q.x, q.y);
+        }
+        constexpr uint32_t kBytes = 8 * kMuonLaneSums;
+        float *const own = muon_smem(S::oOwn);
+        if (lane < kMuonLaneSums) reinterpret_cast<float2 *>(own)[lane] = make_float2(sum.h, sum.l);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) link.expect(0, (uint32_t)(a.cluster - 1) * kBytes);
+        if (lane < a.cluster && lane != rank)
+            link.send(0, smem_u32(muon_smem(S::oRecv) + rank * 2 * kMuonLaneSums), smem_u32(own), kBytes, lane);
+        __syncwarp();
+        link.receive(0);
+        muon_lane_matrix(a, rank);
+    }
+    __syncthreads();
+    muon_lane_apply(X, stay);
+    __syncthreads();
+    muon_update<RP>(a, t, oX, c_begin, stay);
+    if constexpr (STREAM) {
+        for (int64_t c = stay; c < cols; c += kMuonStage) {
+            const int now = (int)min((int64_t)kMuonStage, cols - c);
+            muon_load<RP>(a, t, o_stage, c_begin + c, now, false);
+            __syncthreads();
+            muon_lane_apply(stage, now);
+            __syncthreads();
+            muon_update<RP>(a, t, o_stage, c_begin + c, now);
+            __syncthreads();
+        }
+    }
+    cluster_sync();  // no CTA leaves while it is sent to
+}
+
 static int muon_rp(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
 
 // Floats of the workspace: a row of RP per column, whether it is used or not.
@@ -500,8 +715,14 @@ template <int RP>
 static attt_status muon_run(MuonArgs a, int nmat, int dev, cudaStream_t stream) {
     using S = MuonShape<RP>;
     constexpr size_t kMax = 232448 - 1024;  // 227 KB opt-in less the static part
-    const void *kerns[2] = {reinterpret_cast<const void *>(muon_kernel<RP, false>),
-                            reinterpret_cast<const void *>(muon_kernel<RP, true>)};
+    const void *kerns[2];
+    if constexpr (RP == 8) {
+        kerns[0] = reinterpret_cast<const void *>(muon_lane_kernel<false>);
+        kerns[1] = reinterpret_cast<const void *>(muon_lane_kernel<true>);
+    } else {
+        kerns[0] = reinterpret_cast<const void *>(muon_kernel<RP, false>);
+        kerns[1] = reinterpret_cast<const void *>(muon_kernel<RP, true>);
+    }
     a.room = (int)((kMax - sizeof(float) * S::kFixed) / (sizeof(float) * S::LD)) / 8 * 8;
     const size_t smem = sizeof(float) * (S::kFixed + (size_t)a.room * S::LD);
     int most[2][kMuonMaxCluster + 1];
@@ -571,6 +792,7 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
         const attt_status tc = muon_tc_run(a, 2 * nproj, dev, stream, &done);
         if (done || tc != ATTT_OK) return tc;
     }
+    if (r <= kMuonLaneRank) return muon_run<8>(a, 2 * nproj, dev, stream);
     return r <= 16 ? muon_run<16>(a, 2 * nproj, dev, stream)
          : r <= 32 ? muon_run<32>(a, 2 * nproj, dev, stream)
                    : muon_run<64>(a, 2 * nproj, dev, stream);

@@ -12,7 +12,8 @@ constexpr int kMuonMats = 16;  // two per projection
 constexpr int kMuonThreads = 512;
 constexpr int kMuonStage = 128;  // columns of a tile that does not stay
 constexpr int kMuonMinCluster = 4, kMuonMaxCluster = 16;
-constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr double kNsA64 = 3.4445, kNsB64 = -4.7750, kNsC64 = 2.0315;
+constexpr float kNsA = (float)kNsA64, kNsB = (float)kNsB64, kNsC = (float)kNsC64;
 
 struct MuonMat {
     float *p, *m;
