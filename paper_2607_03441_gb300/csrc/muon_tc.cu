@@ -23,7 +23,7 @@
 
 namespace attt {
 
-constexpr int kTcCols = 440;                          // columns of a CTA at most
+constexpr int kTcCols = 432;                          // columns of a CTA at most, a multiple of an MMA's 16
 constexpr uint32_t kTcSplit = kTcCols * 128u;         // bytes of one of X's tiles
 constexpr uint32_t kTcMat = 64 * 128u;                // of one of an r x r matrix's
 constexpr uint32_t kTcTmem = 512;
@@ -35,7 +35,7 @@ constexpr int kTcPart = 0, kTcRecv = 64 * kTcLD, kTcG = kTcRecv + (64 + kMuonMax
 constexpr int kTcSlab = kTcG + 64 * kTcLD;            // beside the tiles: outgoing copies may still read it
 constexpr uint32_t kTcRest = (kTcSlab + 64 / kMuonMinCluster * kTcLD) * 4u;
 static_assert(kTcSlab * 4u >= 6 * kTcMat && kTcRest >= 7 * kTcMat, "two matrices of three tiles, and a seventh to overrun");
-static_assert(kTcSplit % 1024 == 0 && kTcCols * 68 * 4 <= 3 * kTcSplit, "");
+static_assert(kTcCols % 16 == 0 && kTcSplit % 1024 == 0 && kTcCols * 68 * 4 <= 3 * kTcSplit, "");
 constexpr size_t kTcSmem = 1024 + 3 * kTcSplit + kTcRest;
 static_assert(kTcCols / 128 * 128 + 128 <= 512 && (512 - kTcCols) * 128 <= (int)kTcRest, "the last tile of 128 columns stays in bounds");
 

@@ -70,6 +70,9 @@ CASES = [  # dins, douts, r
     ([1], [1], 1), ([8], [5], 3), ([512], [512], 8), ([3584, 3584], [3584, 512], 16), ([1000], [1001], 12),
     ([130, 7, 129], [64, 2049, 8], 24), ([4096], [1023], 32), ([640, 72], [33, 5120], 64), ([300], [9000], 63),
     ([14336, 64], [64, 27648], 64), ([100] * 8, [200] * 8, 40),
+    # as many columns as a CTA of the tensor-core form holds, and numbers just about it
+    ([4344, 4392, 688, 816, 1152, 72], [3016, 2128, 4256, 1536, 728, 1304], 64), ([432 * 4], [440 * 4], 48),
+    ([5184, 5280, 5176], [5272, 5185, 5279], 64),
     # ranks up to 5: one Gram matrix for all steps; columns that shared memory does not hold
     ([2856, 9], [3512, 100], 4), ([7, 130], [1, 2049], 2), ([100000], [90001], 5), ([100001], [3], 4),
 ]
