@@ -77,21 +77,22 @@ static LpLayout lp_layout(void *ws, int64_t L, int64_t d, int64_t V, int topk) {
     return c;
 }
 
-// (max, sum, moment) of some of a row's sets, as epilogue_logp forms them.  While
-// the max is -inf the sum means nothing but that it may be NaN.
+// (max, sum, moment) of some of a row's logits, as epilogue_logp forms them: the sum leaves
+// out the max's own term, which is 1.  While the max is -inf the sum means nothing but that
+// it may be NaN.
 struct LpPart {
     float m, s, t;
     __device__ __forceinline__ void merge(const LpPart &o, float c2) {
-        const float M = fmaxf(m, o.m);
-        if (M == -INFINITY) {
+        const bool mine = m >= o.m;
+        const LpPart lo = mine ? o : *this, hi = mine ? *this : o;
+        if (hi.m == -INFINITY) {
             s += o.s;
-            t += o.t;
             return;
         }
-        const float a = (m - M) * c2, b = (o.m - M) * c2, fa = ex2(a), fb = ex2(b);
-        t = fa * fmaf(s, fmaxf(a, -1e4f), t) + fb * fmaf(o.s, fmaxf(b, -1e4f), o.t);
-        s = fa * s + fb * o.s;
-        m = M;
+        const float d = (lo.m - hi.m) * c2, f = ex2(d), n = 1.f + lo.s;
+        t = fmaf(f, fmaf(n, fmaxf(d, -1e4f), lo.t), hi.t);
+        s = fmaf(f, n, hi.s);
+        m = hi.m;
     }
     __device__ __forceinline__ LpPart shfl_xor(int o) const {
         return LpPart{__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o),
@@ -113,11 +114,18 @@ struct LpReduceArgs {
     int *status;
 };
 
+// The log of a row's whole sum (in units of the max's term): small values keep their 24 bits,
+// and with them the entropies and log probabilities of rows that are nearly sure.
+__device__ __forceinline__ float lp_log_sum(const LpPart &p) {
+    if (p.m == -INFINITY) return logf(p.s);
+    return p.m < INFINITY ? log1pf(p.s) : __int_as_float(0x7fc00000);
+}
+
 // A row's lse, entropy and log probability of its given token, from its (max, sum,
-// moment) and ln = log(sum).
+// moment) and that log.
 __device__ __forceinline__ void lp_row(const LpReduceArgs &a, int j, const LpPart &p, float ln) {
     if (a.lse) a.lse[j] = fmaf(p.m, a.inv_temp, ln);
-    if (a.entropy) a.entropy[j] = ln - 0.69314718055994531f * (p.t / p.s);
+    if (a.entropy) a.entropy[j] = ln - 0.69314718055994531f * (p.t / (p.m == -INFINITY ? p.s : 1.f + p.s));
     if (a.logp) {
         const int t = a.tgt[j];
         float lp = 0.f;
@@ -387,8 +395,8 @@ __global__ void __launch_bounds__(few_threads(SETS), 1)
                         const bool above = z > st[t].m;
                         const float d = (above ? st[t].m - z : z - st[t].m) * a.c2, e = ex2(d), dm = fmaxf(d, -1e4f);
                         if (above) {
-                            st[t].t = e * fmaf(st[t].s, dm, st[t].t);
-                            st[t].s = fmaf(st[t].s, e, 1.f);
+                            st[t].t = e * fmaf(1.f + st[t].s, dm, st[t].t);
+                            st[t].s = fmaf(st[t].s, e, e);
                             st[t].m = z;
                         } else {
                             st[t].t = fmaf(e, dm, st[t].t);
@@ -548,7 +556,7 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
     }
-    const float ln = logf(p.s);
+    const float ln = lp_log_sum(p);
     if (lane == 0) lp_row(a, j, p, ln);
     if constexpr (TOP) {
         if (lane < a.topk) {

@@ -615,9 +615,11 @@ struct TopList {
     }
 };
 
-// What a run keeps of a row.  With z the accumulator, c = log2 e / T, m the max so far:
-// s = sum 2^((z - m) c) and t = sum 2^((z - m) c) (z - m) c, so that lse = m / T + ln s and
-// the entropy is ln s - ln 2 t / s, both without a difference of large numbers.
+// What a run keeps of a row.  With z the accumulator, c = log2 e / T, m the max so far, over
+// all columns but the (first) one of the max: s = sum 2^((z - m) c) and t = sum 2^((z - m) c)
+// (z - m) c, so that lse = m / T + ln(1 + s) and the entropy is ln(1 + s) - ln 2 t / (1 + s),
+// both without a difference of large numbers, and without the loss that a term of 1 in s
+// would be to rows that are nearly sure (1 + s - 1).
 template <int K>
 struct LogpState {
     float m, s, t;
@@ -671,26 +673,37 @@ __device__ __forceinline__ void epilogue_logp(const GemmArgs &g, LogpState<K> &s
         float bm = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]));
         const float mn = fmaxf(st.m, bm);
         const float ref = mn == -INFINITY ? 0.f : mn, m2 = ref * c2;
-        float s4[4] = {0.f, 0.f, 0.f, 0.f}, t4[4] = {0.f, 0.f, 0.f, 0.f};
+        float s4[4] = {0.f, 0.f, 0.f, 0.f}, t4[4] = {0.f, 0.f, 0.f, 0.f}, equal = 0.f;
+        auto terms = [&](auto &&counts) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float d = fmaf(v[i], c2, -m2);
-            const float e = ex2(d);
-            s4[i & 3] += e;
-            t4[i & 3] = fmaf(e, fmaxf(d, -1e4f), t4[i & 3]);
+            for (int i = 0; i < 32; ++i) {
+                const float d = fmaf(v[i], c2, -m2);
+                const float e = counts(v[i]) ? ex2(d) : 0.f;
+                s4[i & 3] += e;
+                t4[i & 3] = fmaf(e, fmaxf(d, -1e4f), t4[i & 3]);
+            }
+        };
+        if (__any_sync(0xffffffffu, rv && bm >= st.m)) {  // a max is here: its term, and equal ones', are 1
+            terms([&](float x) {
+                if (x == ref) equal += 1.f;
+                return x != ref;
+            });
+            if (bm > st.m) equal -= 1.f;
+        } else {
+            terms([](float) { return true; });
         }
         // terms are 2^(-r) too large, r = m c - m2; the moment's (z - m) c is r too large
         const float r = fmaf(ref, c2, -m2), rs = ex2(-r);
         float bs = (s4[0] + s4[1]) + (s4[2] + s4[3]), bt = (t4[0] + t4[1]) + (t4[2] + t4[3]);
         bt = rs * fmaf(-r, bs, bt);
-        bs *= rs;
-        if (st.m == mn || st.m == -INFINITY) {
+        bs = fmaf(bs, rs, equal);
+        if (bm > st.m) {
+            const float dm = (st.m - mn) * c2, f = ex2(dm), n = 1.f + st.s;
+            st.t = fmaf(f, fmaf(n, fmaxf(dm, -1e4f), st.t), bt);
+            st.s = fmaf(f, n, bs);
+        } else {
             st.s += bs;
             st.t += bt;
-        } else {
-            const float dm = (st.m - mn) * c2, f = ex2(dm);
-            st.t = fmaf(f, fmaf(st.s, fmaxf(dm, -1e4f), st.t), bt);
-            st.s = fmaf(st.s, f, bs);
         }
         st.m = mn;
         if constexpr (K > 0) {

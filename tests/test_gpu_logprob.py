@@ -174,6 +174,28 @@ def test_infinite_and_nan_logits():
     assert got[4][2][0] == 300
 
 
+@pytest.mark.parametrize("L", [1, 20, 40, 700])
+@pytest.mark.parametrize("gap", [9.0, 14.0, 30.0])
+def test_rows_that_are_nearly_sure(L, gap):
+    """One token far above all others, which differ: 1 - p, down to 1e-10, and what follows
+    from it keep their 24 bits.  Terms carry 2^-22 from ex2 and its argument (up to 64
+    in log2 units: 2^-24 of it, 4e-6), sums of them no more: 1e-5 of each value."""
+    d, V = 64, 5000
+    r = np.random.default_rng(int(gap))
+    h, W = np.zeros((L, d)), np.zeros((V, d))
+    h[:, 0] = 1
+    W[:, 0] = r.integers(0, 64, V) / 32
+    sure = r.integers(0, V, L).astype(np.int32)
+    for j in range(L):  # a column of h of its own for every 16th row
+        h[j, 1 + j % 16] = 1
+        sure[j] = sure[j % 16]
+        W[sure[j], 1 + j % 16] = gap
+    want = op.logprobs(h, W, sure, 3)
+    got = _run(h, W, sure, 3, 1.0)
+    for g, w, what in zip(got[:4], want, ("logp", "entropy", "lse", "top_logp")):
+        assert (np.abs(g - w) <= 1e-5 * np.abs(w)).all(), (what, np.abs((g - w) / w).max())
+
+
 def test_one_finite_logit():
     W = np.zeros((300, 8))
     W[:, 0] = -np.inf
