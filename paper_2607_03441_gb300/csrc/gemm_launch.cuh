@@ -39,6 +39,7 @@ struct GemmProblem {
     // EPI_F32_PART: K pieces per tile; each stores its 128-row accumulators
     // (pair: 256) at its part_row of split_ws, BN columns wide.
     int pieces = 1;
+    int fold = 0;  // > 0: row m of the sum of the pieces takes rows m and m + fold
 };
 
 // Pieces per tile for the tiles of a partial last wave: `tiles` tiles over
@@ -68,6 +69,7 @@ inline int tail_pieces(int tiles, int units, int kb_total, int nranks, int regio
 struct SplitReduceArgs {
     const float *part;
     int M, N, BN, pieces, rows, tiles_m;  // rows: accumulator rows per tile (128, pair: 256)
+    int fold;  // > 0: row m of the result is the sum of rows m and m + fold
     int64_t ld;
     float *out;
     __nv_bfloat16 *out16;
@@ -232,6 +234,9 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
     if (epi_block(EPI)) {
         if (!make_tmap_bf16(&tc, ep.G, (uint64_t)ep.G_ld, (uint64_t)p.M, (uint64_t)ep.G_ld * 2, 32, 32, 64))
             return ATTT_ERR_INVALID_ARG;
+        if (EPI == EPI_LOGP_GRAD && ep.G_lo &&
+            !make_tmap_bf16(&ta2, ep.G_lo, (uint64_t)ep.G_ld, (uint64_t)p.M, (uint64_t)ep.G_ld * 2, 32, 32, 64))
+            return ATTT_ERR_INVALID_ARG;
     } else if (EPI == EPI_F32_ACC) {
         if (!make_tmap_f32(&tc, ep.out, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)ep.out_ld * 4, 32, 32))
             return ATTT_ERR_INVALID_ARG;
@@ -348,6 +353,8 @@ attt_status launch_planned(GemmProblem p, const EpiParams &ep, const TilePlan &t
     a.part = p.split_ws;
     a.M = p.M; a.N = p.N; a.BN = t.BN; a.pieces = t.pieces; a.rows = t.pair ? 256 : 128;
     a.tiles_m = (int)cdiv(p.M, a.rows);
+    a.fold = p.fold;
+    if (p.fold > 0) a.M = p.fold;
     a.ld = ep.out_ld; a.alpha = ep.alpha;
     if (OUT16) a.out16 = ep.out16;
     else a.out = ep.out;

@@ -22,15 +22,17 @@ __global__ void __launch_bounds__(kReduceThreads) split_reduce_kernel(const Spli
     if (i >= (int64_t)a.M * n4) return;
     const int row = (int)(i / n4), col = (int)(i - (int64_t)row * n4) * 4;
     const int tn = col / a.BN;
-    // piece p of the tile: `rows` rows of BN columns from part_row(.., p, ..)
-    const int64_t y = part_row(row / a.rows, tn, a.tiles_m, 0, a.pieces, a.rows) + row % a.rows;
-    const float4 *src = reinterpret_cast<const float4 *>(a.part + y * a.BN + (col - tn * a.BN));
     const int64_t step = (int64_t)a.rows * a.BN / 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int from = row; from < row + a.fold + 1; from += a.fold > 0 ? a.fold : 1) {
+        // piece p of the tile: `rows` rows of BN columns from part_row(.., p, ..)
+        const int64_t y = part_row(from / a.rows, tn, a.tiles_m, 0, a.pieces, a.rows) + from % a.rows;
+        const float4 *src = reinterpret_cast<const float4 *>(a.part + y * a.BN + (col - tn * a.BN));
 #pragma unroll 4
-    for (int p = 0; p < a.pieces; ++p) {
-        const float4 v = __ldcg(src + p * step);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        for (int p = 0; p < a.pieces; ++p) {
+            const float4 v = __ldcg(src + p * step);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
     }
     auto fix = [&](float4 &o) {
         if (!a.row_gamma) return;

@@ -92,7 +92,8 @@ struct EpiParams {
     float inv_temp;
     // EPI_LOGP_GRAD: [M] each; gent nullptr: no entropy term
     const float *lse, *entropy, *glogp, *gent;
-    float *lp_loss;  // [M] bf16(x) - x of the given token's entry x; 0 without one
+    float *lp_loss;  // [M] bf16(x) - x of the given token's entry x; 0 without one (nullptr: not wanted)
+    __nv_bfloat16 *G_lo;  // [M, G_ld] what rounding to G took away, bf16; nullptr: not wanted
     int V;  // valid targets are below V (tgt, v0, G, G_ld, inv_temp as above)
 };
 
@@ -780,13 +781,15 @@ __device__ __forceinline__ void logp_flush(const GemmArgs &g, const Span &s, Log
 // vocabulary).  What the given token's entry, a row's largest as a rule, loses
 // there goes to lp_loss, negative, and comes back in fp32 with the second contraction
 // (EPI_BF16's gamma): without it dh is off by 2.4e-3 of its norm, with it by 1.8e-3, of
-// which its own rounding to bf16 is 1.7e-3.
+// which its own rounding to bf16 is 1.7e-3.  Few rows, whose other large entries do not
+// average out (1 to 4 rows: up to 2.9e-3), keep all of what is lost as a second block
+// (G_lo), rows that the second contraction's tiles have room for.
 // Columns past N within the tile are stored as zeros.  A row without a given token
 // (t < 0) has a = 0; an invalid target makes its row NaN.
 template <int SETS>
 __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_base, int tn, int set, int row,
-                                                   uint32_t taddr, const CUtensorMap *tmE, uint32_t sE,
-                                                   uint32_t &ec) {
+                                                   uint32_t taddr, const CUtensorMap *tmE,
+                                                   const CUtensorMap *tmLo, uint32_t sE, uint32_t &ec) {
     const EpiParams &ep = g.ep;
     const int gm = gm_base + row;
     const bool rv = gm < g.M;
@@ -814,7 +817,7 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
             A = fmaf(b * ep.inv_temp, __ldg(ep.entropy + gm), at);
             B = b * ep.inv_temp;
         }
-        if ((t < 0 || t >= ep.V) && tn == 0 && set == 0) ep.lp_loss[gm] = 0.f;
+        if (ep.lp_loss && (t < 0 || t >= ep.V) && tn == 0 && set == 0) ep.lp_loss[gm] = 0.f;
     }
     for (int c = c0; c < c1; c += 32) {
         float v[32];
@@ -831,7 +834,7 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
             for (int i = 0; i < 32; ++i)
                 if (tc == i) {
                     v[i] += at;
-                    if (col0 + i < n_end) ep.lp_loss[gm] = __bfloat162float(__float2bfloat16_rn(v[i])) - v[i];
+                    if (ep.lp_loss && col0 + i < n_end) ep.lp_loss[gm] = __bfloat162float(__float2bfloat16_rn(v[i])) - v[i];
                 }
         }
         if (col0 + 32 > n_end) {
@@ -846,6 +849,15 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
             pk[i / 2] = *reinterpret_cast<uint32_t *>(&b);
         }
         e_block_store(tmE, sE, (int)(ec++), lane, pk, col0, y);
+        if (ep.G_lo) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+                const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&pk[i / 2]));
+                __nv_bfloat162 b = __floats2bfloat162_rn(v[i] - hi.x, v[i + 1] - hi.y);
+                pk[i / 2] = *reinterpret_cast<uint32_t *>(&b);
+            }
+            e_block_store(tmLo, sE, (int)(ec++), lane, pk, col0, y);
+        }
     }
 }
 
@@ -1208,7 +1220,7 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
                 logp_flush<epi_top(EPI), SETS>(g, span, logp, w, nwork, blockIdx.x, gridDim.x, wi.tm,
                                                wi.tm * 128 + row, set);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
-                epilogue_logp_grad<SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC,
+                epilogue_logp_grad<SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC, &tmA2,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else {
                 epilogue_tile<EPI, SETS>(g, wi.tm * 128, wi.tn, set, row, taddr, &tmC,
@@ -1479,7 +1491,7 @@ __global__ void __launch_bounds__(gemm_pair_threads(SETS), 1)
                 epilogue_logp<epi_top(EPI), SETS>(g, logp, gm_base + row, wi.tn, set, taddr);
                 logp_flush<epi_top(EPI), SETS>(g, span, logp, w, nwork, cid, ncl, wi.tm, gm_base + row, set);
             } else if constexpr (EPI == EPI_LOGP_GRAD) {
-                epilogue_logp_grad<SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC,
+                epilogue_logp_grad<SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC, &tmA2,
                                          smem_u32(sE) + (uint32_t)ew * 4096u, bec);
             } else {
                 epilogue_tile<EPI, SETS>(g, gm_base, wi.tn, set, row, taddr, &tmC,

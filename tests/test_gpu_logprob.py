@@ -249,6 +249,24 @@ def test_gradient(L, d, V, inv_temp, ent):
     assert abs((got * u).sum() - slope) <= bound
 
 
+@pytest.mark.parametrize("L,d,V,inv_temp", [(1, 64, 4000, 1.25), (3, 1032, 9100, 1.0), (33, 520, 2001, 2.0),
+                                            (64, 136, 5000, 1.0)])
+def test_gradient_of_few_rows_keeps_the_block(L, d, V, inv_temp):
+    """Up to 64 rows take their dz in two bf16 (2^-16 of each value): dh is off by its own
+    rounding (2^-8 of it) and by fp32 arithmetic alone."""
+    h, W, tgt = _inputs(L + V, L, d, V)
+    a, b = _grads(L, L)
+    f = attt.attt_logprob_forward(_bf16(h), _bf16(W), torch.from_numpy(tgt).to(DEV), inv_temp=inv_temp)
+    dh = attt.attt_logprob_input_grad(_bf16(h), _bf16(W), torch.from_numpy(tgt).to(DEV), f[2],
+                                      torch.from_numpy(a).to(DEV), f[1], torch.from_numpy(b).to(DEV), inv_temp)
+    want, dz = op.logprobs_grad(h, W, tgt, a, b, inv_temp)
+    p = np.exp(h @ W.T * inv_temp - op.logprobs(h, W, None, 0, inv_temp)[2][:, None])
+    terms = p * (np.abs(a) + np.abs(b) * 10)[:, None] * inv_temp
+    slack = ((2.0 ** -16 + 2.0 ** -13) * np.abs(dz) + 1e-5 * terms) @ np.abs(W) + 2.0 ** -20 * np.abs(a)[:, None]
+    err = np.abs(dh.float().cpu().numpy() - want)
+    assert (err <= 2.0 ** -8 * (np.abs(want) + slack) + slack + 1e-7).all()
+
+
 @pytest.mark.parametrize("L,d,V", [(1, 64, 4000), (40, 1032, 4100), (300, 520, 12000)])
 def test_gradient_of_the_given_token_is_not_rounded(L, d, V):
     """Weights halfway between two bf16 values: the given token's own term counts in
