@@ -39,6 +39,11 @@ struct GemmProblem {
     // EPI_F32_PART: K pieces per tile; each stores its 128-row accumulators
     // (pair: 256) at its part_row of split_ws, BN columns wide.
     int pieces = 1;
+    // Loads of one row tile end with its last row (in eights): what rows past M hold is
+    // then anything, and so are their results.  Filling them with zeros takes longer than
+    // leaving them (log probabilities' gradient through 152,064 x 3,584: 1 row 329 us a
+    // call, 378 with all 128 rows loaded; 16 rows 335, 348; 64 rows the same).
+    bool tight = false;
     int fold = 0;  // > 0: row m of the sum of the pieces takes rows m and m + fold
 };
 
@@ -196,7 +201,8 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
     // MN-major operand: storage [K, rows] (rows contiguous), box 64 x 64.
     bool ok;
     // EPI_KL loads 64 rows of A and 64 of A2 into one 128-row tile
-    const uint32_t a_box_rows = EPI == EPI_KL ? 64u : 128u;
+    uint32_t a_box_rows = EPI == EPI_KL ? 64u : 128u;
+    if (p.tight && !A_MN && !p.pair && p.K2 == 0 && p.M < 128) a_box_rows = (uint32_t)round_up(p.M, 8);
     if (!A_MN)
         ok = make_tmap_bf16(&ta, p.a, (uint64_t)p.a_k, (uint64_t)p.a_rows, (uint64_t)p.a_rows_ld * 2, 64, a_box_rows);
     else
@@ -296,6 +302,7 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
     const int rows_tile = EPI == EPI_KL ? 128 : p.pair ? 256 : 128;
     const int group = EPI == EPI_KL ? 8 : 2048 / rows_tile;
     g.group_m = tile_group(p.M, rows_tile, group, 2.0 * p.M * p.K * (EPI == EPI_KL ? 2 : 1));
+    g.a_bytes = a_box_rows * 128u;
     g.status = status ? status : device_status_word(dev);
     g.ep = ep;
 

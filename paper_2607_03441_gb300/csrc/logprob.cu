@@ -706,7 +706,7 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
         GemmProblem p{};
         p.a = d_h + r0 * h_ld; p.a_rows_ld = h_ld; p.a_rows = R; p.a_k = d;
         p.b = d_W; p.b_rows_ld = d; p.b_rows = V; p.b_k = d;
-        p.M = (int)R; p.N = (int)V; p.K = (int)d; p.BN = t.BN; p.pair = t.pair;
+        p.M = (int)R; p.N = (int)V; p.K = (int)d; p.BN = t.BN; p.pair = t.pair; p.tight = true;
         EpiParams ep{};
         ep.tgt = d_tgt ? d_tgt + r0 : nullptr; ep.ztgt = c.ztgt;
         ep.lp_part = c.part; ep.lp_plane = c.plane;
@@ -773,7 +773,7 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             GemmProblem p{};
             p.a = d_h + r0 * h_ld; p.a_rows_ld = h_ld; p.a_rows = R; p.a_k = d;
             p.b = d_W; p.b_rows_ld = d; p.b_rows = V; p.b_k = d;
-            p.M = (int)R; p.N = (int)V; p.K = (int)d; p.BN = t.BN; p.pair = t.pair;
+            p.M = (int)R; p.N = (int)V; p.K = (int)d; p.BN = t.BN; p.pair = t.pair; p.tight = true;
             EpiParams ep{};
             ep.tgt = d_tgt + r0; ep.lse = d_lse + r0; ep.glogp = d_glogp + r0;
             ep.entropy = d_gent ? d_entropy + r0 : nullptr;
@@ -792,6 +792,7 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             p.b = d_W; p.b_rows_ld = d; p.b_rows = d; p.b_k = V;
             p.M = (int)M; p.N = (int)d; p.K = (int)c.ld;
             p.fold = lo ? (int)R : 0;
+            p.tight = true;
             p.pdl = true;
             p.split_ws = c.split_ws; p.split_tick = c.split_tick; p.split_regions = c.regions;
             EpiParams ep{};

@@ -113,6 +113,7 @@ struct GemmArgs {
     int operands_ready;
     int kb_split;  // K blocks of the first operand pair; later ones come from A2 / B2
     int group_m;   // row tiles per group of the tile order (0: all)
+    uint32_t a_bytes;  // of an A stage that a load fills (single CTAs)
     int *status;
     EpiParams ep;
     // Tail split (tc_gemm_kernel / tc_gemm_pair_kernel): tiles [0, whole_tiles)
@@ -1081,7 +1082,7 @@ __global__ void __launch_bounds__(gemm_threads(SETS), 1)
                 for (int kb = wi.kb0; kb < wi.kb1; ++kb) {
                     if (!mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag)) { ok = false; break; }
                     const uint32_t fb = full0 + 8 * stage;
-                    mbar_arrive_expect_tx(fb, kABytes + b_bytes);
+                    mbar_arrive_expect_tx(fb, g.a_bytes + b_bytes);
                     const uint32_t a_dst = smem_u32(sA + (size_t)stage * kABytes);
                     const uint32_t b_dst = smem_u32(sB + (size_t)stage * b_bytes);
                     // K block kb of the first pair, or K block kb - kb_split of the second
