@@ -16,7 +16,11 @@
 // softmax needs no second sweep: lse and H are the forward call's) as a bf16 block
 // G, then dh = G W (4 L V d FLOPs: the logits are formed again).
 // The gradient takes rows in blocks so that G stays bounded.
-// Bound: the tensor core from a few hundred rows on, the head's bytes below.
+// Bound: the tensor core from a few hundred rows on, the head's bytes below.  Through a head
+// of 152,064 x 3,584: 2,048 rows with 8 alternatives 1.16 ms (the burst GEMM rate), 403 rows
+// 324 us (of which a fifth is the padding to 512), the gradient of 93 rows 341 us (the
+// head is read twice: 322 of bytes); of 4,096 rows through 152,064 x 5,120 7.1 ms (1.79
+// PFLOP/s).
 #include <algorithm>
 
 #include "gemm_launch.cuh"

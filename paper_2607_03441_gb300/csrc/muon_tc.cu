@@ -13,10 +13,13 @@
 // the Gram matrix (rank on M and N).  M is 128 throughout: where a matrix has 64 rows the
 // other 64 are whatever follows in shared memory, and their results, in the upper
 // TMEM lanes, are never read.  The r x r products are formed by every CTA on its own
-// (0.7 us each; in slabs with an exchange they took 2.1 in muon.cu), so that only the
+// (1.4 us each; in slabs with an exchange they took 2.1 in muon.cu), so that only the
 // Gram matrices travel.
 // Why: on CUDA cores the products were bound by the 128 bytes that shared memory returns
-// per cycle (a 4 x 8 tile per thread: 128 FMAs per 12 vector reads).
+// per cycle (a 4 x 8 tile per thread: 128 FMAs per 12 vector reads).  The step of q, k, v
+// and o of 5,120 at r 64 (8 matrices, clusters of 12) takes 67 us, 121 with muon.cu's
+// kernel; its bytes would take 7.  Bound: the chain of three Gram matrices with their
+// exchanges, eleven r x r products and three products with X.
 #include <algorithm>
 
 #include "muon.cuh"
