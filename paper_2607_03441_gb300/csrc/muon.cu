@@ -21,15 +21,15 @@
 // memory from the first read of g and m to the update of p (what does not fit
 // goes through a workspace that stays in L2).  The CTAs' Gram matrices are summed
 // through distributed shared memory in CTA order: each CTA gets its slab of rows from
-// all of them, sums, and gives it to all.  At r > 32 the r x r products are formed in
-// slabs too; below that every CTA forms all of it, which takes less time than an
-// exchange.  Exchanges are bulk copies between the CTAs' shared memories counted on
+// all of them, sums, and gives it to all; up to r 16 each gets all of it from all.  At
+// r > 32 the r x r products are formed in slabs too; below that one or two warps of
+// every CTA form all of it, which takes less time than an exchange.  Exchanges are bulk copies between the CTAs' shared memories counted on
 // mbarriers (measured at 8 / 12 to 16 CTAs of 512 threads, 17 KB to each: 0.8 us; plain
 // stores and a cluster barrier 1.1 / 1.6).  fp32 FMA throughout: the Gram matrices need
 // their 24 bits.  Ranks up to 5 and (where the columns fit) of 33 to 64 have kernels of
 // their own, below and in muon_tc.cu.
 // Bound: fp32 FMA issue at r 64 (5 r^2 n of them), exchanges and launch below.  The step of
-// q and v of 3,584 at r 16 (4 matrices, clusters of 16) takes 24.6 us, its bytes 0.6.
+// q and v of 3,584 at r 16 (4 matrices, clusters of 16) takes 22.7 us, its bytes 0.6.
 #include <algorithm>
 #include <array>
 #include <cmath>
@@ -60,7 +60,11 @@ struct MuonShape {
     static constexpr int kRecv = (RP + kMuonMaxCluster) * LD;
     // this CTA's slab of the sum, to be sent (G itself is written again at once)
     static constexpr int kSlab = (RP / kMuonMinCluster) * LD;
-    static constexpr int kFixed = kFirst + kMat + kRecv + kSlab;
+    // RP 16: every CTA's whole matrix goes to all others, and one warp forms the products;
+    // the matrix and what comes for two groups in turn
+    static constexpr bool kWarp = RP == 16;
+    static constexpr int kTurn = (1 + kMuonMaxCluster) * kMat;
+    static constexpr int kFixed = kFirst + (kWarp ? 2 * kTurn : kMat + kRecv + kSlab);
     // Row and column of a Gram tile's first element.
     __device__ static __forceinline__ void tile(int t, int &i0, int &j0) {
         if constexpr (RP > 32) {
@@ -165,11 +169,9 @@ __device__ __forceinline__ void muon_gram(const float *s, int cols, float (&acc)
     }
 }
 
-// The cluster's Gram matrix into G of every CTA, from the threads' shares (exchanges n and
-// n + 1).  `part`: kMat floats, `recv`: kRecv.
+// The CTA's Gram matrix into `part`, from the threads' shares.
 template <int RP>
-__device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP>::TJ], float *scratch, float *part,
-                                              float *recv, float *G, const MuonLink &link, uint32_t n) {
+__device__ __forceinline__ void muon_gram_part(const float (&acc)[4][MuonShape<RP>::TJ], float *scratch, float *part) {
     using S = MuonShape<RP>;
     constexpr int kVecs = S::kTiles * S::TJ;  // vectors of 4 of one set of tiles
     const int sub = threadIdx.x / S::kTiles, tile = threadIdx.x % S::kTiles;
@@ -200,6 +202,15 @@ __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP
             part[(j + 3) * S::LD + i] = v.w;
         }
     }
+}
+
+// The cluster's Gram matrix into G of every CTA, from the threads' shares (exchanges n and
+// n + 1).  `part`: kMat floats, `recv`: kRecv.
+template <int RP>
+__device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP>::TJ], float *scratch, float *part,
+                                              float *recv, float *G, const MuonLink &link, uint32_t n) {
+    using S = MuonShape<RP>;
+    muon_gram_part<RP>(acc, scratch, part);
     const int r0 = muon_row(RP, link.rank, link.cluster), r1 = muon_row(RP, link.rank + 1, link.cluster);
     float *const slab = recv + S::kRecv;
     link.gather<RP, S::LD>(n, part, recv, r0, r1, [&](int at, float4 v) {
@@ -210,17 +221,16 @@ __device__ __forceinline__ void muon_gram_sum(const float (&acc)[4][MuonShape<RP
 }
 
 // z = alpha x y (+ beta w, w_at >= 0) + diag I in every CTA, x and y symmetric and
-// commuting, z none of the others (exchange n where the CTAs form slabs of it).
+// commuting, z none of the others; each CTA forms a slab of it (exchange n).
 template <int RP>
 __device__ __noinline__ void muon_product(int x_at, int y_at, int z_at, float alpha, int w_at, float beta, float diag,
                                           const MuonLink &link, uint32_t n) {
     using S = MuonShape<RP>;
     const float *x = muon_smem(x_at), *y = muon_smem(y_at), *w = w_at < 0 ? nullptr : muon_smem(w_at);
     float *z = muon_smem(z_at);
-    const int r0 = S::kSlabs ? muon_row(RP, link.rank, link.cluster) : 0,
-              r1 = S::kSlabs ? muon_row(RP, link.rank + 1, link.cluster) : RP;
+    const int r0 = muon_row(RP, link.rank, link.cluster), r1 = muon_row(RP, link.rank + 1, link.cluster);
     // threads per vector of 4 results: all of them, as far as a power of two allows
-    const int subs = RP == 16 ? 8 : RP == 32 ? 2 : link.cluster >= 8 ? 4 : 2;
+    const int subs = link.cluster >= 8 ? 4 : 2;
     const int o = threadIdx.x / subs, q = threadIdx.x % subs;
     const int i = r0 + o / (RP / 4), j = o % (RP / 4) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -247,8 +257,128 @@ __device__ __noinline__ void muon_product(int x_at, int y_at, int z_at, float al
         if (i == j + 3) v.w += diag;
         *reinterpret_cast<float4 *>(z + i * S::LD + j) = v;
     }
-    if constexpr (S::kSlabs) link.share<S::LD>(n, z + r0 * S::LD, z, r0, r1, RP);
-    else __syncthreads();
+    link.share<S::LD>(n, z + r0 * S::LD, z, r0, r1, RP);
+}
+
+// z = alpha x y (+ beta w, w_at >= 0) + diag I by one warp, x and y 16 x 16, symmetric and
+// commuting, z none of the others.
+__device__ __noinline__ void muon_warp_product(int x_at, int y_at, int z_at, float alpha, int w_at, float beta,
+                                               float diag) {
+    constexpr int LD = MuonShape<16>::LD;
+    const int lane = threadIdx.x & 31, i = lane >> 1, j = (lane & 1) * 8;
+    const float *x = muon_smem(x_at) + i * LD, *y = muon_smem(y_at) + j;
+    float v[8] = {};
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+        const float4 xk = *reinterpret_cast<const float4 *>(x + k);
+        const float xe[4] = {xk.x, xk.y, xk.z, xk.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 a = *reinterpret_cast<const float4 *>(y + (k + e) * LD),
+                         b = *reinterpret_cast<const float4 *>(y + (k + e) * LD + 4);
+            v[0] = fmaf(xe[e], a.x, v[0]); v[1] = fmaf(xe[e], a.y, v[1]);
+            v[2] = fmaf(xe[e], a.z, v[2]); v[3] = fmaf(xe[e], a.w, v[3]);
+            v[4] = fmaf(xe[e], b.x, v[4]); v[5] = fmaf(xe[e], b.y, v[5]);
+            v[6] = fmaf(xe[e], b.z, v[6]); v[7] = fmaf(xe[e], b.w, v[7]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] *= alpha;
+        if (w_at >= 0) v[e] = fmaf(beta, muon_smem(w_at)[i * LD + j + e], v[e]);
+        if (i == j + e) v[e] += diag;
+    }
+    float4 *z = reinterpret_cast<float4 *>(muon_smem(z_at) + i * LD + j);
+    z[0] = make_float4(v[0], v[1], v[2], v[3]);
+    z[1] = make_float4(v[4], v[5], v[6], v[7]);
+    __syncwarp();
+}
+
+// The same by two warps, x and y 32 x 32: a thread has a tile of 4 x 4 (symmetric: row k of x
+// is its column k), 2 vector reads for 16 FMAs.  q and v of 3,584 at r 32: 37 us, 45 with
+// vectors of 4 by all threads, whose reads took longer than the sums.
+__device__ __noinline__ void muon_two_product(int x_at, int y_at, int z_at, float alpha, int w_at, float beta,
+                                              float diag) {
+    constexpr int LD = MuonShape<32>::LD;
+    const int i0 = threadIdx.x / 8 * 4, j0 = threadIdx.x % 8 * 4;
+    const float *x = muon_smem(x_at) + i0, *y = muon_smem(y_at) + j0;
+    float v[4][4] = {}, o[4][4] = {};  // even and odd k: half the length of a sum
+#pragma unroll 4
+    for (int k = 0; k < 32; k += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float4 xk = *reinterpret_cast<const float4 *>(x + (k + h) * LD),
+                         yk = *reinterpret_cast<const float4 *>(y + (k + h) * LD);
+            const float xe[4] = {xk.x, xk.y, xk.z, xk.w}, ye[4] = {yk.x, yk.y, yk.z, yk.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) (h ? o : v)[i][j] = fmaf(xe[i], ye[j], (h ? o : v)[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (w_at >= 0) w = *reinterpret_cast<const float4 *>(muon_smem(w_at) + (i0 + i) * LD + j0);
+        const float we[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[i][j] = fmaf(beta, we[j], (v[i][j] + o[i][j]) * alpha);
+            if (i0 + i == j0 + j) v[i][j] += diag;
+        }
+        *reinterpret_cast<float4 *>(muon_smem(z_at) + (i0 + i) * LD + j0) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+    }
+    named_barrier_sync(1, 64);
+}
+
+// One warp: exchange n (the CTAs' whole matrices, this one's at `turn`, the others' behind
+// it), their sum in rank order and the group's products.  Both take a
+// warp's time and not the block's: q and v of 3,584 at r 16 took 24.6 us with two
+// exchanges (slabs of the sum) a group and products by all threads, 22.7 so.
+__device__ __noinline__ void muon_warp_matrix(const MuonLink &link, uint32_t n, int turn, bool first, bool pair,
+                                             float eps) {
+    using S = MuonShape<16>;
+    constexpr int oG = 0, oB = S::kMat, oT = 2 * S::kMat;
+    constexpr uint32_t kBytes = 4 * S::kMat;
+    const int lane = threadIdx.x & 31;
+    float *const G = muon_smem(oG), *const part = muon_smem(turn), *const recv = part + S::kMat;
+    if (lane == 0) link.expect(n, (uint32_t)(link.cluster - 1) * kBytes);
+    if (lane < link.cluster && lane != link.rank)
+        link.send(n, smem_u32(recv + link.rank * S::kMat), smem_u32(part), kBytes, lane);
+    __syncwarp();
+    link.receive(n);
+    float trace = 0.f;
+    float4 sum[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = lane + 32 * h, at = e / 4 * S::LD + e % 4 * 4;
+        sum[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = 0; c < link.cluster; ++c)
+            sum[h] = add4(sum[h], *reinterpret_cast<const float4 *>((c == link.rank ? part : recv + c * S::kMat) + at));
+        const int k = e / 4 - e % 4 * 4;  // the diagonal's place in the vector
+        trace += k == 0 ? sum[h].x : k == 1 ? sum[h].y : k == 2 ? sum[h].z : k == 3 ? sum[h].w : 0.f;
+    }
+    float scale = 1.f;
+    if (first) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) trace += __shfl_xor_sync(0xffffffffu, trace, o);
+        scale = 1.f / (sqrtf(trace) + eps);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = lane + 32 * h;
+        *reinterpret_cast<float4 *>(G + e / 4 * S::LD + e % 4 * 4) =
+            make_float4(sum[h].x * scale * scale, sum[h].y * scale * scale, sum[h].z * scale * scale,
+                        sum[h].w * scale * scale);
+    }
+    __syncwarp();
+    const float s0 = pair ? 1.f : scale;
+    muon_warp_product(oG, oG, oB, kNsC * s0, oG, kNsB * s0, kNsA * s0);
+    if (!pair) return;  // P is B
+    muon_warp_product(oB, oG, oT, 1.f, -1, 0.f, 0.f);
+    muon_warp_product(oT, oB, oG, 1.f, -1, 0.f, 0.f);
+    muon_warp_product(oG, oG, oT, kNsC, oG, kNsB, kNsA);
+    muon_warp_product(oT, oB, oG, scale, -1, 0.f, 0.f);  // P is over G
 }
 
 // X <- P X for NC x CL columns (`left` of them, more than (NC - 1) x CL), in place.
@@ -351,38 +481,62 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
 
     const int groups = (a.steps + 1) / 2, single = a.steps % 2 ? groups / 2 : -1;  // pairs, the odd step amidst them
     for (int gi = 0; gi < groups; ++gi) {
-        if (gi > 0) cluster_sync();  // every CTA has what this one's matrices were sent for
-        muon_gram_sum<RP>(acc, G, part, recv, G, link, n);
-        n += 2;
-        float scale = 1.f;
-        if (gi == 0) {
-            if (threadIdx.x < 32) {
-                float v = 0.f;
-                for (int i = threadIdx.x; i < RP; i += 32) v += G[i * S::LD + i];
-                for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (threadIdx.x == 0) s_scale = 1.f / (sqrtf(v) + a.eps);
-            }
-            __syncthreads();
-            scale = s_scale;
-            for (int e = threadIdx.x; e < RP * RP; e += kMuonThreads) {
-                float &x = G[e / RP * S::LD + e % RP];
-                x = x * scale * scale;
-            }
-            __syncthreads();
-        }
-        // B = a I + b G + c G^2, and for a pair of steps G <- B G B, P = (a I + b G + c G^2) B
-        // (a single first step takes the scale into B, as X_0 has it in u)
         int oP = oB;
-        const float s0 = gi == single ? scale : 1.f;
-        muon_product<RP>(oG, oG, oB, kNsC * s0, oG, kNsB * s0, kNsA * s0, link, n++);
-        if (gi != single) {
-            muon_product<RP>(oB, oG, oT, 1.f, -1, 0.f, 0.f, link, n++);
-            muon_product<RP>(oT, oB, oG, 1.f, -1, 0.f, 0.f, link, n++);
-            muon_product<RP>(oG, oG, oT, kNsC, oG, kNsB, kNsA, link, n++);
-            muon_product<RP>(oT, oB, oG, scale, -1, 0.f, 0.f, link, n++);
-            oP = oG;
+        if constexpr (S::kWarp) {
+            // (two groups' places in turn: what a CTA sends for the next but one follows all that
+            // the others sent for the next, and so their reading of this)
+            const int turn = S::kFirst + (gi & 1) * S::kTurn;
+            muon_gram_part<RP>(acc, G, muon_smem(turn));
+            fence_proxy_async_smem();
+            __syncthreads();
+            if (threadIdx.x < 32) muon_warp_matrix(link, (uint32_t)gi, turn, gi == 0, gi != single, a.eps);
+            if (gi != single) oP = oG;
+            __syncthreads();
+        } else {
+            if (gi > 0) cluster_sync();  // every CTA has what this one's matrices were sent for
+            muon_gram_sum<RP>(acc, G, part, recv, G, link, n);
+            n += 2;
+            float scale = 1.f;
+            if (gi == 0) {
+                if (threadIdx.x < 32) {
+                    float v = 0.f;
+                    for (int i = threadIdx.x; i < RP; i += 32) v += G[i * S::LD + i];
+                    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    if (threadIdx.x == 0) s_scale = 1.f / (sqrtf(v) + a.eps);
+                }
+                __syncthreads();
+                scale = s_scale;
+                for (int e = threadIdx.x; e < RP * RP; e += kMuonThreads) {
+                    float &x = G[e / RP * S::LD + e % RP];
+                    x = x * scale * scale;
+                }
+                __syncthreads();
+            }
+            // B = a I + b G + c G^2, and for a pair of steps G <- B G B, P = (a I + b G + c G^2) B
+            // (a single first step takes the scale into B, as X_0 has it in u)
+            const float s0 = gi == single ? scale : 1.f;
+            if (gi != single) oP = oG;
+            if constexpr (S::kSlabs) {
+                muon_product<RP>(oG, oG, oB, kNsC * s0, oG, kNsB * s0, kNsA * s0, link, n++);
+                if (gi != single) {
+                    muon_product<RP>(oB, oG, oT, 1.f, -1, 0.f, 0.f, link, n++);
+                    muon_product<RP>(oT, oB, oG, 1.f, -1, 0.f, 0.f, link, n++);
+                    muon_product<RP>(oG, oG, oT, kNsC, oG, kNsB, kNsA, link, n++);
+                    muon_product<RP>(oT, oB, oG, scale, -1, 0.f, 0.f, link, n++);
+                }
+            } else {
+                if (threadIdx.x < 64) {
+                    muon_two_product(oG, oG, oB, kNsC * s0, oG, kNsB * s0, kNsA * s0);
+                    if (gi != single) {
+                        muon_two_product(oB, oG, oT, 1.f, -1, 0.f, 0.f);
+                        muon_two_product(oT, oB, oG, 1.f, -1, 0.f, 0.f);
+                        muon_two_product(oG, oG, oT, kNsC, oG, kNsB, kNsA);
+                        muon_two_product(oT, oB, oG, scale, -1, 0.f, 0.f);
+                    }
+                }
+                __syncthreads();
+            }
         }
-        if constexpr (!S::kSlabs) n = 2 * (gi + 1);  // the products were no exchanges
         const bool last = gi + 1 == groups;
         muon_apply<RP>(oX, oP, stay);
 #pragma unroll
@@ -426,8 +580,8 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
 // 1.  One exchange (128 bytes from each CTA to each) instead of six.  Over 138 matrices of
 // rank 4 the step is off the 64-bit one by 1.2e-7 as a rule and 3.7e-7 at most (the other
 // ranks' kernel: 3.3e-7 and 1e-6; element by element in fp32: up to 7e-7).  Two projections
-// of 3,584 at rank 5 take 16.5 us, 24.6 with the other ranks' kernel; seven of up to 5,120
-// at rank 4 18.5, 28.9.  Bound: launch, load and update, and 64-bit FMA issue (a warp's
+// of 3,584 at rank 5 take 16.5 us, 22.7 with the other ranks' kernel; seven of up to 5,120
+// at rank 4 18.5, 28.8.  Bound: launch, load and update, and 64-bit FMA issue (a warp's
 // takes some 60 cycles, which is why r 8 would gain nothing).
 // ---------------------------------------------------------------------------
 
