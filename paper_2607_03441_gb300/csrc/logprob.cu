@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
     griddep_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % WARPS;
     const int j = blockIdx.x * (kLpWarps / WARPS) + warp / WARPS;
-    if (WARPS == 1 && j >= a.rows) return;  // (a block of one row always has it)
+    const bool row = j < a.rows;
     const float c2 = a.inv_temp * kLog2e;
     LpPart p{-INFINITY, 0.f, 0.f};
     LpKey top = kLpNone;
@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
     } else {
         const int first = j / a.tile_rows * a.tiles_n;
         const int units = run_unit(a.nwork, first + a.tiles_n - 1, a.units) - run_unit(a.nwork, first, a.units) + 1;
-        const int nsets = a.sets * units * (a.split ? 2 : 1);
+        const int nsets = row ? a.sets * units * (a.split ? 2 : 1) : 0;
         for (int t = w + lane * WARPS; t < nsets; t += 32 * WARPS) {
             const int64_t o = (int64_t)t * a.rows + j;
             p.merge(LpPart{__ldcg(a.part + o), __ldcg(a.part + a.plane + o), __ldcg(a.part + 2 * a.plane + o)}, c2);
@@ -550,17 +550,18 @@ __global__ void __launch_bounds__(kLpWarps * 32) logprob_reduce_kernel(const LpR
             for (int n = WARPS / 2; n > 0; n /= 2) {
                 s_top[warp][lane] = top;
                 __syncthreads();
-                if (warp < n) lp_merge(top, s_top[warp + n][lane], lane);
+                if (w < n) lp_merge(top, s_top[warp + n][lane], lane);
                 __syncthreads();
             }
         } else {
             __syncthreads();
         }
         if (w > 0) return;
-        p = lane < WARPS ? s_part[lane] : LpPart{-INFINITY, 0.f, 0.f};
+        p = lane < WARPS ? s_part[warp + lane] : LpPart{-INFINITY, 0.f, 0.f};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) p.merge(p.shfl_xor(o), c2);
     }
+    if (!row) return;
     const float ln = lp_log_sum(p);
     if (lane == 0) lp_row(a, j, p, ln);
     if constexpr (TOP) {
@@ -587,11 +588,17 @@ static attt_status launch_reduce_as(const LpReduceArgs &a, cudaStream_t stream) 
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
 }
 
-// A block per row while there are many sets and few rows, a warp per row else.
+// The fewer rows, the more sets each has (and SMs to spare): a block per row, half of one,
+// or a warp.  Hidden size 752 through 13,323, us a call with 16 / 8 / 1 warps per row: with 8
+// alternatives 500 rows 41 / 41 / 70, 1,000 rows 60 / 53 / 63, 2,000 rows 94 / 76 / 72;
+// without, 1,000 rows 28.8 / 27.4 / 26.1.  (171 rows x 1,424 through 12,055 with one: 22.6 / 32 / 70.)
 template <bool TOP>
 static attt_status launch_reduce(const LpReduceArgs &a, cudaStream_t stream) {
     if (a.tile_rows == 0) return launch_reduce_as<TOP, kLpWarps, true>(a, stream);
-    return a.rows <= 1024 ? launch_reduce_as<TOP, kLpWarps, false>(a, stream) : launch_reduce_as<TOP, 1, false>(a, stream);
+    if (a.rows <= 384) return launch_reduce_as<TOP, kLpWarps, false>(a, stream);
+    if constexpr (TOP)
+        if (a.rows <= 1536) return launch_reduce_as<TOP, kLpWarps / 2, false>(a, stream);
+    return launch_reduce_as<TOP, 1, false>(a, stream);
 }
 
 template <bool TOP, int SETS>

@@ -23,8 +23,8 @@
 // through distributed shared memory in CTA order: each CTA gets its slab of rows from
 // all of them, sums, and gives it to all; up to r 16 each gets all of it from all.  At
 // r > 32 the r x r products are formed in slabs too; below that one or two warps of
-// every CTA form all of it, which takes less time than an exchange.  Exchanges are bulk copies between the CTAs' shared memories counted on
-// mbarriers (measured at 8 / 12 to 16 CTAs of 512 threads, 17 KB to each: 0.8 us; plain
+// every CTA form all of it, which takes less time than an exchange.  Exchanges are bulk
+// copies between the CTAs' shared memories counted on mbarriers (measured at 8 / 12 to 16 CTAs of 512 threads, 17 KB to each: 0.8 us; plain
 // stores and a cluster barrier 1.1 / 1.6).  fp32 FMA throughout: the Gram matrices need
 // their 24 bits.  Ranks up to 5 and (where the columns fit) of 33 to 64 have kernels of
 // their own, below and in muon_tc.cu.

@@ -72,3 +72,30 @@ def test_rounds_repeat():
     a = ex.train(rows=64, width=128, vocab=2048, rank=8, rounds=6, verbose=False)
     b = ex.train(rows=64, width=128, vocab=2048, rank=8, rounds=6, verbose=False)
     assert a == b
+
+
+def test_an_update_in_a_graph():
+    """A captured update does what the calls do one by one, bit for bit."""
+    L, d, V, r = 70, 128, 3000, 16
+    g = torch.Generator(device=DEV).manual_seed(5)
+
+    def normal(*shape, std=1.0):
+        return (torch.randn(shape, generator=g, device=DEV) * std).to(torch.bfloat16)
+
+    W0, Wlm, x = normal(d, d, std=d ** -0.5), normal(V, d, std=2 * d ** -0.5), normal(L, d)
+    A, B = normal(d, r, std=d ** -0.5), normal(r, d, std=0.1)
+    tokens = torch.randint(0, V, (L,), generator=g, device=DEV, dtype=torch.int32)
+    adv = torch.randn(L, generator=g, device=DEV)
+    plain, captured = (ex.Policy(W0, Wlm, A, B, L) for _ in range(2))
+    for _ in range(3):
+        plain.gradients(x, tokens, adv, beta=0.01)
+        plain.step(0.02)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.gradients(x, tokens, adv, beta=0.01)
+        captured.step(0.02)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(plain.A32, captured.A32) and torch.equal(plain.B32, captured.B32)
+    assert attt.attt_device_status() == 0
