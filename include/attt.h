@@ -527,9 +527,9 @@ ATTT_API attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, co
  *   d_dh[j, :] = sum_v dz_jv W_v                                   (bf16 [L, d])
  * with a_j = glogp_j, or 0 where t_j = -1.  d_gent (and then d_entropy) may be
  * NULL: no entropy term.  dz is rounded to bf16 once, but for the given token's,
- * which counts in full; products are bf16, sums fp32.  No gradient for W (it is
- * frozen).  Requirements as above, d_dh 16-byte
- * aligned, d_ws at least attt_logprob_grad_workspace_bytes(L, d, V) bytes.
+ * which counts in full (up to 64 rows: all of it to two bf16); products are bf16,
+ * sums fp32.  No gradient for W (it is frozen).  Requirements as above, d_dh
+ * 16-byte aligned, d_ws at least attt_logprob_grad_workspace_bytes(L, d, V) bytes.
  * Another token sets ATTT_ERR_TOKEN_RANGE and makes its row NaN.
  */
 ATTT_API attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 *d_W,
