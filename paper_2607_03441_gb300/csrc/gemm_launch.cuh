@@ -347,12 +347,14 @@ attt_status launch_gemm(const GemmProblem &p, const EpiParams &ep, int dev, cuda
 }
 
 // A contraction with an fp32 (ep.out) or bf16 (ep.out16) result on the tiles of
-// `t`: whole tiles with the fused epilogue, or K pieces and the reduction.
+// `t`: whole tiles with the fused epilogue, or K pieces and the reduction, which also
+// adds the rows that p.fold joins (a plan of whole tiles is then one piece per tile).
 template <bool OUT16, bool A_MN, bool B_MN>
 attt_status launch_planned(GemmProblem p, const EpiParams &ep, const TilePlan &t, int dev, cudaStream_t stream) {
     p.pair = t.pair;
     p.BN = t.BN;
-    if (t.pieces == 1) return launch_gemm<OUT16 ? EPI_BF16 : EPI_F32_ACC, A_MN, B_MN>(p, ep, dev, stream);
+    if (t.pieces == 1 && p.fold == 0)
+        return launch_gemm<OUT16 ? EPI_BF16 : EPI_F32_ACC, A_MN, B_MN>(p, ep, dev, stream);
     p.pieces = t.pieces;
     const attt_status st = launch_gemm<EPI_F32_PART, A_MN, B_MN>(p, ep, dev, stream);
     if (st != ATTT_OK) return st;

@@ -35,7 +35,11 @@ constexpr int64_t kLpHiddenBytes = 48ll << 20;  // the hidden states of a row bl
 constexpr int64_t kLpHeadBytes = 48ll << 20;    // a head that L2 holds beside them (tc_gemm.cuh: Span)
 constexpr int64_t kLpRunRows = 16384;           // and its rows
 constexpr int kFewRows = 32;  // rows of a call that reads the head as the M operand, at most
-constexpr int kLoRows = 64;   // rows of a gradient call whose block takes two bf16 per value, at most: one tile
+// Rows of a gradient call whose block takes two bf16 per value, at most: both blocks fit one
+// tile of 128 rows.  More would pay for what they do not need, as dh is rounded to bf16 itself
+// (1.66e-3 of its norm): 93 rows x 3,584 through 152,064 340 us with one, error 1.79e-3, and
+// 367 with two, 1.67e-3; 4,096 x 5,120 7.1 ms, 1.84e-3, and 11.3 ms, 1.68e-3.
+constexpr int kLoRows = 64;
 constexpr int kLpSplitRegions = 320;  // K pieces of the second contraction: 128 KB each
 
 inline int lp_sets(int64_t d) { return cdiv(d, 64) <= kTwoSetBlocks ? 2 : 1; }
@@ -645,8 +649,11 @@ static GradLayout grad_layout(void *ws, int64_t L, int64_t d, int64_t V) {
     c.rows = lp_block_rows(L, 2 * c.ld, kLpGBytes);
     const int64_t t2 = 2 * kMaxPieces * cdiv(c.rows, 256) * cdiv(d, 256);
     c.regions = (int)(t2 < kLpSplitRegions ? t2 : kLpSplitRegions);
-    Carve cv{static_cast<char *>(ws), 0};
     c.lo = L <= kLoRows;
+    // the sum that joins G's two blocks reads partials: those of a row of whole tiles fit at least
+    // (up to 256 accumulator rows of d columns and of what a tile is wider)
+    if (c.lo) c.regions = (int)std::max<int64_t>(c.regions, 2 * (cdiv(d, 256) + 1));
+    Carve cv{static_cast<char *>(ws), 0};
     c.G = cv.take<__nv_bfloat16>((size_t)((c.lo ? 2 : 1) * c.rows * c.ld));
     c.loss = cv.take<float>((size_t)c.rows);
     c.split_ws = cv.take<float>((size_t)c.regions * 128 * 256);
@@ -772,11 +779,10 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
     const int sets = lp_sets(d);
     for (int64_t r0 = 0; r0 < L; r0 += c.rows) {
         const int64_t R = L - r0 < c.rows ? L - r0 : c.rows;
-        TilePlan td = plan_tiles(c.lo ? 2 * R : R, d, c.ld / 64, num_sms(dev), c.regions, true, true);
-        const bool lo = c.lo && td.pieces > 1;  // the sum of the pieces adds the two rows
-        if (c.lo && !lo) td = plan_tiles(R, d, c.ld / 64, num_sms(dev), c.regions, true, true);
+        const int64_t M = c.lo ? 2 * R : R;  // the sum of the pieces adds the two rows of each
+        const TilePlan td = plan_tiles(M, d, c.ld / 64, num_sms(dev), c.regions, !c.lo, true);
         // whole tiles: the last wave's may be cut, with arrival counters that start at 0
-        if (td.pieces == 1 &&
+        if (td.pieces == 1 && !c.lo &&
             cudaMemsetAsync(c.split_tick, 0, sizeof(unsigned int) * (size_t)c.regions, stream) != cudaSuccess)
             return ATTT_ERR_CUDA;
         {   // G from the logits
@@ -791,24 +797,23 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
             ep.gent = d_gent ? d_gent + r0 : nullptr;
             ep.inv_temp = inv_temp; ep.V = (int)V;
             ep.G = c.G; ep.G_ld = c.ld;
-            if (lo) ep.G_lo = c.G + R * c.ld;
+            if (c.lo) ep.G_lo = c.G + R * c.ld;
             else ep.lp_loss = c.loss;
             st = launch_logits<EPI_LOGP_GRAD>(p, ep, sets, dev, stream);
             if (st != ATTT_OK) return st;
         }
         {   // dh = G W
             GemmProblem p{};
-            const int64_t M = lo ? 2 * R : R;
             p.a = c.G; p.a_rows_ld = c.ld; p.a_rows = M; p.a_k = c.ld;
             p.b = d_W; p.b_rows_ld = d; p.b_rows = d; p.b_k = V;
             p.M = (int)M; p.N = (int)d; p.K = (int)c.ld;
-            p.fold = lo ? (int)R : 0;
+            p.fold = c.lo ? (int)R : 0;
             p.tight = true;
             p.pdl = true;
             p.split_ws = c.split_ws; p.split_tick = c.split_tick; p.split_regions = c.regions;
             EpiParams ep{};
             ep.out16 = reinterpret_cast<__nv_bfloat16 *>(d_dh) + r0 * d; ep.out_ld = d; ep.alpha = 1.0f;
-            if (!lo) {
+            if (!c.lo) {
                 ep.row_gamma = c.loss; ep.fix_tgt = d_tgt + r0;
                 ep.fix_W = reinterpret_cast<const __nv_bfloat16 *>(d_W); ep.fix_ld = d; ep.fix_V = (int)V;
             }
