@@ -353,9 +353,9 @@ ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, co
  * momentum (the dA of B = 0) gives X = 0.  A matrix with a NaN or an infinity in u,
  * or with |u|_F^2 beyond fp32, becomes NaN as a whole; the others do not feel it.
  * Requirements: 1 <= nproj <= 8, 1 <= r <= 64, 1 <= din, dout <= 2^25,
- * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps > 0, 1 <= ns_steps <= 16, all
- * finite, no two matrices alike, d_ws at least attt_lora_muon_workspace_bytes(...)
- * bytes and 256-byte aligned.  One launch.
+ * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps >= 1e-12 (fp32 holds its
+ * square), 1 <= ns_steps <= 16, all finite, no two matrices alike, d_ws at least
+ * attt_lora_muon_workspace_bytes(...) bytes and 256-byte aligned.  One launch.
  */
 ATTT_API attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_B32,
                                          const float *const *d_dA, const float *const *d_dB, float *const *d_mA,

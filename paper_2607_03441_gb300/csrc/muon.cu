@@ -362,7 +362,7 @@ __device__ __noinline__ void muon_warp_matrix(const MuonLink &link, uint32_t n, 
     if (first) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) trace += __shfl_xor_sync(0xffffffffu, trace, o);
-        scale = 1.f / (sqrtf(trace) + eps);
+        scale = muon_scale(trace, eps);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
                     float v = 0.f;
                     for (int i = threadIdx.x; i < RP; i += 32) v += G[i * S::LD + i];
                     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                    if (threadIdx.x == 0) s_scale = 1.f / (sqrtf(v) + a.eps);
+                    if (threadIdx.x == 0) s_scale = muon_scale(v, a.eps);
                 }
                 __syncthreads();
                 scale = s_scale;
@@ -677,7 +677,9 @@ __device__ __noinline__ void muon_lane_matrix(const MuonArgs &a, int rank) {
     double g = __shfl_sync(0xffffffffu, (double)sum.h + (double)sum.l, muon_lane_sum(min(i, j), max(i, j)));
     double v = 0.;
     for (int k = 0; k < r; ++k) v += __shfl_sync(0xffffffffu, g, k * (r + 1));
-    const double scale = 1. / (sqrt(v) + (double)a.eps), diag = i == j ? kNsA64 : 0.;
+    // (as muon_scale: beyond fp32 NaN, although this sum would hold it)
+    const double scale = v <= (double)FLT_MAX ? 1. / (sqrt(v) + (double)a.eps) : __longlong_as_double(0x7ff8000000000000ll);
+    const double diag = i == j ? kNsA64 : 0.;
     g *= scale * scale;
     double p = i == j ? scale : 0.;
     for (int k = 0; k < a.steps; ++k) {
@@ -909,7 +911,7 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
     using namespace attt;
     if (!muon_sizes(nproj, din, dout, r) || !d_A32 || !d_B32 || !d_dA || !d_dB || !d_mA || !d_mB)
         return ATTT_ERR_INVALID_ARG;
-    if (!(momentum >= 0.f && momentum < 1.f) || !(weight_decay >= 0.f) || !(rms > 0.f) || !(eps > 0.f) ||
+    if (!(momentum >= 0.f && momentum < 1.f) || !(weight_decay >= 0.f) || !(rms > 0.f) || !(eps >= kMuonMinEps) ||
         !std::isfinite(lr) || !std::isfinite(rms) || !std::isfinite(eps) || !std::isfinite(weight_decay) ||
         ns_steps < 1 || ns_steps > 16)
         return ATTT_ERR_INVALID_ARG;

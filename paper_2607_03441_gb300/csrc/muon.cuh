@@ -3,6 +3,8 @@
 // matrix's elements in global memory.
 #pragma once
 
+#include <cfloat>
+
 #include "attt_common.cuh"
 #include "attt_host.h"
 
@@ -13,6 +15,9 @@ constexpr int kMuonThreads = 512;
 constexpr int kMuonStage = 128;  // columns of a tile that does not stay
 constexpr int kMuonMinCluster = 4, kMuonMaxCluster = 16;
 constexpr double kNsA64 = 3.4445, kNsB64 = -4.7750, kNsC64 = 2.0315;
+// The least eps: |u|_F^2 near its square is a normal fp32 number, and so are the squares of
+// u's elements where they count beside eps.
+constexpr float kMuonMinEps = 1e-12f;
 constexpr float kNsA = (float)kNsA64, kNsB = (float)kNsB64, kNsC = (float)kNsC64;
 
 struct MuonMat {
@@ -35,6 +40,13 @@ struct MuonArgs {
     float mu, keep, eps;  // keep = 1 - lr wd
     int *status;
 };
+
+// 1 / (|u|_F + eps) from |u|_F^2, the Gram matrix's trace.  Beyond fp32 NaN, and with it the whole
+// matrix: the diagonal's elements may all be finite where their sum is not, and 1 / inf
+// would make an update of 0.
+__device__ __forceinline__ float muon_scale(float trace, float eps) {
+    return trace <= FLT_MAX ? 1.f / (sqrtf(trace) + eps) : __int_as_float(0x7fc00000);
+}
 
 // Rows [first, second) of an r x r matrix that CTA `rank` of `cluster` forms.
 __device__ __forceinline__ int muon_row(int RP, int rank, int cluster) { return rank * RP / cluster; }

@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
             if (warp == 0) {
                 float v = G[lane * (kTcLD + 1)] + G[(lane + 32) * (kTcLD + 1)];
                 for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (lane == 0) s_scale = 1.f / (sqrtf(v) + a.eps);
+                if (lane == 0) s_scale = muon_scale(v, a.eps);
             }
             __syncthreads();
             scale = s_scale;
