@@ -352,6 +352,9 @@ ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, co
  * entries are not NULL.  fp32 products and sums; a zero gradient with zero
  * momentum (the dA of B = 0) gives X = 0.  A matrix with a NaN or an infinity in u,
  * or with |u|_F^2 beyond fp32, becomes NaN as a whole; the others do not feel it.
+ * Where a wait of the kernel runs out (ATTT_ERR_TIMEOUT in the device status word),
+ * the columns of p whose X it left incomplete, and their bf16 copies, stay as they
+ * were; m has taken its g.
  * Requirements: 1 <= nproj <= 8, 1 <= r <= 64, 1 <= din, dout <= 2^25,
  * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps >= 1e-12 (fp32 holds its
  * square), 1 <= ns_steps <= 16, all finite, no two matrices alike, d_ws at least

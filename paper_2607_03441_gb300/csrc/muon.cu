@@ -343,7 +343,7 @@ __device__ __noinline__ void muon_warp_matrix(const MuonLink &link, uint32_t n, 
     const int lane = threadIdx.x & 31;
     float *const G = muon_smem(oG), *const part = muon_smem(turn), *const recv = part + S::kMat;
     if (lane == 0) link.expect(n, (uint32_t)(link.cluster - 1) * kBytes);
-    if (lane < link.cluster && lane != link.rank)
+    if (lane < link.cluster && lane != link.rank && !link.lost())
         link.send(n, smem_u32(recv + link.rank * S::kMat), smem_u32(part), kBytes, lane);
     __syncwarp();
     link.receive(n);
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < S::TJ; ++j) acc[i][j] = 0.f;
-        if (last) muon_update<RP>(a, t, oX, c_begin, stay);
+        if (last) muon_update<RP>(a, t, oX, c_begin, stay, link);
         else muon_gram<RP>(X, stay, acc);
         if constexpr (STREAM) {
             for (int64_t c = stay; c < cols; c += kMuonStage) {
@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_kernel(const __grid_cons
                 __syncthreads();
                 muon_apply<RP>(o_stage, oP, now);
                 if (last) {
-                    muon_update<RP>(a, t, o_stage, c_begin + c, now);
+                    muon_update<RP>(a, t, o_stage, c_begin + c, now, link);
                 } else {
                     muon_gram<RP>(stage, now, acc);
                     for (int e = threadIdx.x; e < now * (RP / 4); e += kMuonThreads)
@@ -773,7 +773,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_lane_kernel(const __grid
     __syncthreads();
     muon_lane_apply(X, stay);
     __syncthreads();
-    muon_update<RP>(a, t, oX, c_begin, stay);
+    muon_update<RP>(a, t, oX, c_begin, stay, link);
     if constexpr (STREAM) {
         for (int64_t c = stay; c < cols; c += kMuonStage) {
             const int now = (int)min((int64_t)kMuonStage, cols - c);
@@ -781,7 +781,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_lane_kernel(const __grid
             __syncthreads();
             muon_lane_apply(stage, now);
             __syncthreads();
-            muon_update<RP>(a, t, o_stage, c_begin + c, now);
+            muon_update<RP>(a, t, o_stage, c_begin + c, now, link);
             __syncthreads();
         }
     }

@@ -73,8 +73,11 @@ struct MuonLink {
                      "r"(src), "r"(bytes), "r"(mapa_shared(bar0 + 8u * (n & 1u), to))
                      : "memory");
     }
+    // Whether a wait of this CTA has run out.
+    __device__ __forceinline__ bool lost() const { return *abort_flag != 0; }
     // All threads: exchange n has arrived.  If it does not within the limit, the status word
-    // says so and the CTA goes on to its end on garbage, waiting for nothing.
+    // says so and the CTA goes on to its end on garbage, waiting for nothing, sending nothing
+    // (so that the others' waits run out too) and leaving p as it is.
     __device__ __forceinline__ void receive(uint32_t n) const {
         if (!mbar_wait(bar0 + 8u * (n & 1u), (n >> 1) & 1u, abort_flag)) {
             *abort_flag = 1;
@@ -91,7 +94,7 @@ struct MuonLink {
         fence_proxy_async_smem();
         __syncthreads();
         if (threadIdx.x == 0) expect(n, (uint32_t)((cluster - 1) * rows * LD * 4));
-        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank) {
+        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank && !lost()) {
             const int o0 = muon_row(RP, threadIdx.x, cluster), o = muon_row(RP, threadIdx.x + 1, cluster) - o0;
             if (o > 0)
                 send(n, smem_u32(recv + rank * o * LD), smem_u32(part + o0 * LD), (uint32_t)(o * LD * 4), threadIdx.x);
@@ -118,7 +121,7 @@ struct MuonLink {
         fence_proxy_async_smem();
         __syncthreads();
         if (threadIdx.x == 0) expect(n, (uint32_t)((total - (r1 - r0)) * LD * 4));
-        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank && r1 > r0)
+        if (threadIdx.x < (unsigned)cluster && (int)threadIdx.x != rank && r1 > r0 && !lost())
             send(n, smem_u32(z + r0 * LD), smem_u32(src), (uint32_t)((r1 - r0) * LD * 4), threadIdx.x);
         receive(n);
     }
@@ -172,7 +175,7 @@ __device__ __forceinline__ void muon_items(const MuonMat &t, int r, uint32_t inv
 // The first column's first element.
 __device__ __forceinline__ int64_t muon_origin(const MuonMat &t, int r, int64_t c0) { return t.tall ? c0 * r : c0; }
 
-// p <- keep p - step X for the columns, and the bf16 copy.
+// p <- keep p - step X for the columns, and the bf16 copy (muon_update: unless X is garbage).
 template <int RP, bool V4>
 __device__ __forceinline__ void muon_update_as(const MuonArgs &a, const MuonMat &t, const float *s, int64_t c0,
                                                int cols) {
@@ -217,7 +220,9 @@ __device__ __forceinline__ void muon_update_as(const MuonArgs &a, const MuonMat 
 }
 
 template <int RP>
-__device__ __noinline__ void muon_update(const MuonArgs &a, const MuonMat &t, int s_at, int64_t c0, int cols) {
+__device__ __noinline__ void muon_update(const MuonArgs &a, const MuonMat &t, int s_at, int64_t c0, int cols,
+                                         const MuonLink &link) {
+    if (link.lost()) return;
     if (t.vec) muon_update_as<RP, true>(a, t, muon_smem(s_at), c0, cols);
     else muon_update_as<RP, false>(a, t, muon_smem(s_at), c0, cols);
 }

@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
             }
         }
         settle();
-        if (last) muon_update<64>(a, t, o_x, c_begin, cols);
+        if (last) muon_update<64>(a, t, o_x, c_begin, cols, link);
     }
     tc_fence_before();
     cluster_sync();  // no CTA leaves while it is sent to
