@@ -235,10 +235,23 @@ def _f32_of(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
     return t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
 
 
-def _out_f32(t: Optional[torch.Tensor], shape, name: str, dev) -> torch.Tensor:
+def _empty(*size, dtype, device, stream) -> torch.Tensor:
+    """A new tensor that a call on `stream` (None: the current one) writes.  Of another
+    stream's memory: what the caller's stream frees or takes next is not what the
+    call still waits to use, a workspace among it; a result that the caller's stream
+    has read is not given away before that."""
+    if stream is None:
+        return torch.empty(*size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(*size, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _out_f32(t: Optional[torch.Tensor], shape, name: str, dev, stream) -> torch.Tensor:
     """`t`, checked, or a new float32 tensor of that shape."""
     if t is None:
-        return torch.empty(shape, dtype=torch.float32, device=dev)
+        return _empty(shape, dtype=torch.float32, device=dev, stream=stream)
     _expect(t, shape, torch.float32, name)
     return t
 
@@ -372,7 +385,7 @@ def attt_history_count(h: History, ngrams: torch.Tensor, out: Optional[torch.Ten
     m = ngrams.shape[0]
     _expect(out, (m,), torch.int32, "out")
     if out is None:
-        out = torch.empty(m, dtype=torch.int32, device=ngrams.device)
+        out = _empty(m, dtype=torch.int32, device=ngrams.device, stream=stream)
     _check((_lib or load_library()).attt_history_count(h.handle, _ptr(ngrams), m, _ptr(out), _stream(stream)),
            "attt_history_count")
     return out
@@ -386,7 +399,7 @@ def attt_ngram_weights(h: History, tokens: torch.Tensor, w_min: float = 0.05,
     L = tokens.numel()
     _expect(out, (L,), torch.float32, "out")
     if out is None:
-        out = torch.empty(L, dtype=torch.float32, device=tokens.device)
+        out = _empty(L, dtype=torch.float32, device=tokens.device, stream=stream)
     _check((_lib or load_library()).attt_ngram_weights(
         h.handle, _ptr(tokens), L, float(w_min), _ptr(out), _stream(stream)), "attt_ngram_weights")
     return out
@@ -421,11 +434,11 @@ def attt_weighted_ce_fwd_bwd(h: torch.Tensor, W: torch.Tensor, tgt: torch.Tensor
     if loss is not None and (loss.numel() < 1 or loss.dtype != torch.float32):
         raise ValueError("loss: expected a float32 tensor of at least one element")
     if loss is None:
-        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        loss = _empty(1, dtype=torch.float32, device=dev, stream=stream)
     if dh is None:
-        dh = torch.empty(L, d, dtype=torch.float32, device=dev)
+        dh = _empty(L, d, dtype=torch.float32, device=dev, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_ce_workspace_bytes(L, d, V), dtype=torch.uint8, device=dev)
+        workspace = _empty(attt_ce_workspace_bytes(L, d, V), dtype=torch.uint8, device=dev, stream=stream)
     if tgt.dtype != torch.int32 or w.dtype != torch.float32:
         raise ValueError("tgt must be int32 and w float32")
     _check((_lib or load_library()).attt_weighted_ce_fwd_bwd(
@@ -505,11 +518,11 @@ def attt_lora_grad(x: torch.Tensor, dys: Sequence[torch.Tensor], As: Sequence[to
     k = len(dys)
     dev = x.device
     if dAs is None:
-        dAs = [torch.empty(din, r, dtype=torch.float32, device=dev) for _ in range(k)]
+        dAs = [_empty(din, r, dtype=torch.float32, device=dev, stream=stream) for _ in range(k)]
     if dBs is None:
-        dBs = [torch.empty(r, do, dtype=torch.float32, device=dev) for do in douts]
+        dBs = [_empty(r, do, dtype=torch.float32, device=dev, stream=stream) for do in douts]
     if workspace is None:
-        workspace = torch.empty(attt_lora_workspace_bytes(L, din, douts, r), dtype=torch.uint8, device=dev)
+        workspace = _empty(attt_lora_workspace_bytes(L, din, douts, r), dtype=torch.uint8, device=dev, stream=stream)
     buf, (p_dy, p_dout, p_A, p_B, p_dA, p_dB) = _lora_arrays(dys, douts, As, Bs, dAs, dBs)
     _check((_lib or load_library()).attt_lora_grad(
         _bf16(x), L, din, k, p_dy, p_dout, p_A, p_B, r, float(scale), p_dA, p_dB, _ptr(workspace), workspace.numel(),
@@ -579,10 +592,10 @@ def attt_lora_forward(x: torch.Tensor, W0: torch.Tensor, A: torch.Tensor, B: tor
     _expect(B, (r, dout), torch.bfloat16, "B")
     _expect(h, (L, dout), torch.bfloat16, "h")
     if h is None:
-        h = torch.empty(L, dout, dtype=torch.bfloat16, device=x.device)
+        h = _empty(L, dout, dtype=torch.bfloat16, device=x.device, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_lora_forward_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
-                                device=x.device)
+        workspace = _empty(attt_lora_forward_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
+                                device=x.device, stream=stream)
     _check((_lib or load_library()).attt_lora_forward(
         _bf16(x), _bf16(W0), _bf16(A), _bf16(B), L, din, dout, int(r), float(scale), _bf16(h), _ptr(workspace),
         workspace.numel(), _stream(stream)), "attt_lora_forward")
@@ -601,10 +614,10 @@ def attt_lora_input_grad(dy: torch.Tensor, W0: torch.Tensor, A: torch.Tensor, B:
     _expect(B, (r, dout), torch.bfloat16, "B")
     _expect(dx, (L, din), torch.float32, "dx")
     if dx is None:
-        dx = torch.empty(L, din, dtype=torch.float32, device=dy.device)
+        dx = _empty(L, din, dtype=torch.float32, device=dy.device, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_lora_input_grad_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
-                                device=dy.device)
+        workspace = _empty(attt_lora_input_grad_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
+                                device=dy.device, stream=stream)
     _check((_lib or load_library()).attt_lora_input_grad(
         _bf16(dy), _bf16(W0), _bf16(A), _bf16(B), L, din, dout, int(r), float(scale), _ptr(dx), _ptr(workspace),
         workspace.numel(), _stream(stream)), "attt_lora_input_grad")
@@ -616,7 +629,7 @@ def attt_cast_bf16(src: torch.Tensor, dst: Optional[torch.Tensor] = None, stream
     if src.dtype != torch.float32:
         raise ValueError(f"expected float32, got {src.dtype}")
     if dst is None:
-        dst = torch.empty(src.shape, dtype=torch.bfloat16, device=src.device)
+        dst = _empty(src.shape, dtype=torch.bfloat16, device=src.device, stream=stream)
     if dst.numel() != src.numel():
         raise ValueError(f"dst: expected {src.numel()} elements, got {dst.numel()}")
     _check((_lib or load_library()).attt_cast_bf16(_ptr(src), _bf16(dst), src.numel(), _stream(stream)),
@@ -719,9 +732,9 @@ class Episode:
         if tuple(x.shape) != (L, self.cfg.din):
             raise ValueError("x must be [L, din]")
         if kl is None:
-            kl = torch.empty(L, dtype=torch.float32, device=x.device)
+            kl = _empty(L, dtype=torch.float32, device=x.device, stream=stream)
         if kl_mean is None:
-            kl_mean = torch.empty(1, dtype=torch.float32, device=x.device)
+            kl_mean = _empty(1, dtype=torch.float32, device=x.device, stream=stream)
         _check(self._lib.attt_episode_drift(self.handle, _bf16(x), L, _ptr(kl), _ptr(kl_mean), _stream(stream)),
                "attt_episode_drift")
         return kl, kl_mean
@@ -729,8 +742,8 @@ class Episode:
     def read_adapter(self, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(A [din, r], B [r, d]) fp32 copies of the current adapter."""
         c = self.cfg
-        A = torch.empty((c.din, c.r), dtype=torch.float32, device=self.device)
-        B = torch.empty((c.r, c.d), dtype=torch.float32, device=self.device)
+        A = _empty((c.din, c.r), dtype=torch.float32, device=self.device, stream=stream)
+        B = _empty((c.r, c.d), dtype=torch.float32, device=self.device, stream=stream)
         _check(self._lib.attt_episode_read_adapter(self.handle, _ptr(A), _ptr(B), _stream(stream)),
                "attt_episode_read_adapter")
         return A, B
@@ -775,11 +788,11 @@ def attt_kl_drift(hp: torch.Tensor, hq: torch.Tensor, W: torch.Tensor, kl: Optio
     _expect(kl_mean, (1,), torch.float32, "kl_mean")
     dev = hp.device
     if kl is None:
-        kl = torch.empty(L, dtype=torch.float32, device=dev)
+        kl = _empty(L, dtype=torch.float32, device=dev, stream=stream)
     if kl_mean is None:
-        kl_mean = torch.empty(1, dtype=torch.float32, device=dev)
+        kl_mean = _empty(1, dtype=torch.float32, device=dev, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_kl_workspace_bytes(L, d, V), dtype=torch.uint8, device=dev)
+        workspace = _empty(attt_kl_workspace_bytes(L, d, V), dtype=torch.uint8, device=dev, stream=stream)
     _check((_lib or load_library()).attt_kl_drift(_bf16(hp), _bf16(hq), _bf16(W), L, d, V, _ptr(kl), _ptr(kl_mean),
                                         _ptr(workspace), workspace.numel(), _stream(stream)), "attt_kl_drift")
     return kl, kl_mean
@@ -812,11 +825,11 @@ def attt_layer_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: Optional
     shape, dtype, code = _norm_check(x)
     L, d = shape
     if y is None:
-        y = torch.empty(L, d, dtype=dtype, device=x.device)
+        y = _empty(L, d, dtype=dtype, device=x.device, stream=stream)
     if mean is None:
-        mean = torch.empty(L, dtype=_F32, device=x.device)
+        mean = _empty(L, dtype=_F32, device=x.device, stream=stream)
     if rstd is None:
-        rstd = torch.empty(L, dtype=_F32, device=x.device)
+        rstd = _empty(L, dtype=_F32, device=x.device, stream=stream)
     px, x_ld = _rows_ptr(x, "x")
     py, y_ld = _rows_of(y, shape, dtype, "y")
     _check((_lib or load_library()).attt_layer_norm_forward(
@@ -839,13 +852,13 @@ def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Ten
     shape, dtype, code = _norm_check(x)
     L, d = shape
     if dx is None:
-        dx = torch.empty(L, d, dtype=dtype, device=x.device)
+        dx = _empty(L, d, dtype=dtype, device=x.device, stream=stream)
     if dgamma is None:
-        dgamma = torch.empty(d, dtype=_F32, device=x.device)
+        dgamma = _empty(d, dtype=_F32, device=x.device, stream=stream)
     if dbeta is None:
-        dbeta = torch.empty(d, dtype=_F32, device=x.device)
+        dbeta = _empty(d, dtype=_F32, device=x.device, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=x.device)
+        workspace = _empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=x.device, stream=stream)
     pg, g_ld = _rows_of(dy, shape, dtype, "dy")
     px, x_ld = _rows_ptr(x, "x")
     po, o_ld = _rows_of(dx, shape, dtype, "dx")
@@ -899,15 +912,15 @@ def attt_logprob_forward(h: torch.Tensor, W: torch.Tensor, tgt: Optional[torch.T
     if tgt is None and logp is not None:
         raise ValueError("logp: there are no given tokens")
     if tgt is not None:
-        logp = _out_f32(logp, (L,), "logp", dev)
-    entropy = _out_f32(entropy, (L,), "entropy", dev)
-    lse = _out_f32(lse, (L,), "lse", dev)
-    top_logp = _out_f32(top_logp, (L, topk), "top_logp", dev)
+        logp = _out_f32(logp, (L,), "logp", dev, stream)
+    entropy = _out_f32(entropy, (L,), "entropy", dev, stream)
+    lse = _out_f32(lse, (L,), "lse", dev, stream)
+    top_logp = _out_f32(top_logp, (L, topk), "top_logp", dev, stream)
     _expect(top_id, (L, topk), torch.int32, "top_id")
     if top_id is None:
-        top_id = torch.empty(L, topk, dtype=torch.int32, device=dev)
+        top_id = _empty(L, topk, dtype=torch.int32, device=dev, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_logprob_workspace_bytes(L, d, V, topk), dtype=torch.uint8, device=dev)
+        workspace = _empty(attt_logprob_workspace_bytes(L, d, V, topk), dtype=torch.uint8, device=dev, stream=stream)
     ph, ld = _rows_ptr(h, "h")
     _check((_lib or load_library()).attt_logprob_forward(
         ph, ld, _ptr(W), _ptr(tgt), L, d, V, float(inv_temp), topk, _ptr(logp), _ptr(entropy), _ptr(lse),
@@ -928,9 +941,10 @@ def attt_logprob_input_grad(h: torch.Tensor, W: torch.Tensor, tgt: torch.Tensor,
         _expect(t, (L,), torch.float32, name)
     _expect(dh, (L, d), torch.bfloat16, "dh")
     if dh is None:
-        dh = torch.empty(L, d, dtype=torch.bfloat16, device=h.device)
+        dh = _empty(L, d, dtype=torch.bfloat16, device=h.device, stream=stream)
     if workspace is None:
-        workspace = torch.empty(attt_logprob_grad_workspace_bytes(L, d, V), dtype=torch.uint8, device=h.device)
+        workspace = _empty(attt_logprob_grad_workspace_bytes(L, d, V), dtype=torch.uint8, device=h.device,
+                           stream=stream)
     ph, ld = _rows_ptr(h, "h")
     _check((_lib or load_library()).attt_logprob_input_grad(
         ph, ld, _ptr(W), _ptr(tgt), _ptr(lse), _ptr(entropy), _ptr(glogp), _ptr(gent), L, d, V, float(inv_temp),
@@ -997,9 +1011,9 @@ def attt_repetition(s: WordSets, text: torch.Tensor, tau: float = 0.5, out: Opti
     _expect(keep, (1,), torch.int32, "keep")
     dev = text.device
     if out is None:
-        out = torch.empty(2, dtype=torch.float32, device=dev)
+        out = _empty(2, dtype=torch.float32, device=dev, stream=stream)
     if keep is None:
-        keep = torch.empty(1, dtype=torch.int32, device=dev)
+        keep = _empty(1, dtype=torch.int32, device=dev, stream=stream)
     n = text.numel()
     base = _ptr(out)
     _check((_lib or load_library()).attt_repetition(s.handle, _ptr(text) if n else None, n, float(tau), base, base + 4,
@@ -1067,8 +1081,8 @@ class Batch:
 
     def read_adapter(self, e: int, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         c = self.cfg
-        A = torch.empty((c.din, c.r), dtype=torch.float32, device=self.device)
-        B = torch.empty((c.r, c.d), dtype=torch.float32, device=self.device)
+        A = _empty((c.din, c.r), dtype=torch.float32, device=self.device, stream=stream)
+        B = _empty((c.r, c.d), dtype=torch.float32, device=self.device, stream=stream)
         _check(self._lib.attt_batch_read_adapter(self.handle, int(e), _ptr(A), _ptr(B), _stream(stream)),
                "attt_batch_read_adapter")
         return A, B
@@ -1137,8 +1151,8 @@ def attt_lora_muon_step(A32s: Sequence[torch.Tensor], B32s: Sequence[torch.Tenso
             if t is not None and (t.shape != shape or t.dtype != dtype):
                 _expect(t, shape, dtype, f"{name}[{i}]")
     if workspace is None:
-        workspace = torch.empty(attt_lora_muon_workspace_bytes(dins, douts, r), dtype=torch.uint8,
-                                device=A32s[0].device)
+        workspace = _empty(attt_lora_muon_workspace_bytes(dins, douts, r), dtype=torch.uint8,
+                                device=A32s[0].device, stream=stream)
     vals = dins + douts
     for ts in (A32s, B32s, dAs, dBs, mAs, mBs, A16s or (), B16s or ()):
         vals += [_ptr(t) or 0 for t in ts]
