@@ -462,7 +462,7 @@ ATTT_API attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, cons
                                              void *d_y, int64_t y_ld, float *d_mean, float *d_rstd,
                                              attt_stream stream);
 
-/* Workspace bytes attt_layer_norm_backward needs. */
+/* Workspace bytes attt_layer_norm_backward needs.  0 for sizes that it refuses. */
 ATTT_API size_t attt_layer_norm_workspace_bytes(int64_t L, int64_t d);
 
 /*

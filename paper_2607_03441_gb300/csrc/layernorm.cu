@@ -798,9 +798,11 @@ static attt_status ln_backward_run(const T *dy, const T *x, const float *gamma, 
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
 }
 
-static bool ln_sizes(int64_t L, int64_t d, int dtype) {
-    return L >= 0 && d >= 1 && (dtype == ATTT_BF16 || dtype == ATTT_F32);
+static attt_status ln_sizes(int64_t L, int64_t d) {
+    if (L < 0 || d < 1) return ATTT_ERR_INVALID_ARG;
+    return L > (1ll << 31) - 1 || d > (1ll << 24) ? ATTT_ERR_UNSUPPORTED : ATTT_OK;
 }
+static bool ln_type(int dtype) { return dtype == ATTT_BF16 || dtype == ATTT_F32; }
 
 // Whether rows from p, `ld` elements apart, lie on 16-byte boundaries from end to end.
 static bool ln_vector(const void *p, int64_t ld, int64_t d, size_t esize) {
@@ -816,14 +818,16 @@ attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, const float *
                                     float *d_rstd, attt_stream stream) {
     ATTT_NVTX_RANGE();
     using namespace attt;
-    if (!ln_sizes(L, d, dtype) || !(eps >= 0.f) || x_ld < d || y_ld < d) return ATTT_ERR_INVALID_ARG;
+    if (!ln_type(dtype) || !(eps >= 0.f) || x_ld < d || y_ld < d) return ATTT_ERR_INVALID_ARG;
     if (!d_gamma || (L > 0 && (!d_x || !d_y))) return ATTT_ERR_INVALID_ARG;
     const size_t es = dtype == ATTT_BF16 ? 2 : 4;
     if (reinterpret_cast<uintptr_t>(d_x) % es || reinterpret_cast<uintptr_t>(d_y) % es) return ATTT_ERR_INVALID_ARG;
-    if (L > (1ll << 31) - 1 || d > (1ll << 24) || x_ld > (1ll << 36) || y_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
+    attt_status st = ln_sizes(L, d);
+    if (st != ATTT_OK) return st;
+    if (x_ld > (1ll << 36) || y_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
     if (L == 0) return ATTT_OK;
     int dev;
-    const attt_status st = current_device(&dev);
+    st = current_device(&dev);
     if (st != ATTT_OK) return st;
     LnShape s{};
     s.L = L; s.d = (int)d; s.x_ld = x_ld; s.y_ld = y_ld; s.eps = eps; s.inv_d = 1.f / (float)d;
@@ -842,7 +846,7 @@ attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, const float *
 }
 
 size_t attt_layer_norm_workspace_bytes(int64_t L, int64_t d) {
-    if (L < 0 || d < 1) return 0;
+    if (attt::ln_sizes(L, d) != ATTT_OK) return 0;
     const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(L, attt::kLnMaxBlocks));
     return (size_t)attt::round_up(rows * 2 * d * (int64_t)sizeof(float), 256);
 }
@@ -853,16 +857,17 @@ attt_status attt_layer_norm_backward(const void *d_dy, int64_t dy_ld, const void
                                      void *d_ws, size_t ws_bytes, attt_stream stream) {
     ATTT_NVTX_RANGE();
     using namespace attt;
-    if (!ln_sizes(L, d, dtype) || dy_ld < d || x_ld < d || dx_ld < d) return ATTT_ERR_INVALID_ARG;
+    if (!ln_type(dtype) || dy_ld < d || x_ld < d || dx_ld < d) return ATTT_ERR_INVALID_ARG;
     if (!d_gamma || (L > 0 && (!d_dy || !d_x || !d_mean || !d_rstd || !d_dx))) return ATTT_ERR_INVALID_ARG;
     const size_t es = dtype == ATTT_BF16 ? 2 : 4;
     for (const void *p : {d_dy, d_x, (const void *)d_dx})
         if (reinterpret_cast<uintptr_t>(p) % es) return ATTT_ERR_INVALID_ARG;
-    if (L > (1ll << 31) - 1 || d > (1ll << 24) || dy_ld > (1ll << 36) || x_ld > (1ll << 36) || dx_ld > (1ll << 36))
-        return ATTT_ERR_UNSUPPORTED;
+    attt_status st = ln_sizes(L, d);
+    if (st != ATTT_OK) return st;
+    if (dy_ld > (1ll << 36) || x_ld > (1ll << 36) || dx_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_layer_norm_workspace_bytes(L, d)) return ATTT_ERR_WORKSPACE;
     int dev;
-    const attt_status st = current_device(&dev);
+    st = current_device(&dev);
     if (st != ATTT_OK) return st;
     LnShape s{};
     s.L = L; s.d = (int)d; s.x_ld = x_ld; s.y_ld = dx_ld; s.g_ld = dy_ld; s.inv_d = 1.f / (float)d;

@@ -662,12 +662,20 @@ static GradLayout grad_layout(void *ws, int64_t L, int64_t d, int64_t V) {
     return c;
 }
 
+// The sizes that both calls and their workspaces take.
+static attt_status lp_sizes(int64_t L, int64_t d, int64_t V) {
+    if (L < 1 || V < 1 || d < 8 || d % 8 != 0) return ATTT_ERR_INVALID_ARG;
+    return L > (1ll << 30) || V > (1ll << 30) || d > (1ll << 20) ? ATTT_ERR_UNSUPPORTED : ATTT_OK;
+}
+
 // What both calls ask of their operands.
 static attt_status lp_check(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 *d_W, int64_t L, int64_t d, int64_t V,
                             float inv_temp) {
-    if (!d_h || !d_W || L < 1 || V < 1 || d < 8 || d % 8 != 0 || h_ld < d || h_ld % 8 != 0) return ATTT_ERR_INVALID_ARG;
+    if (!d_h || !d_W || h_ld < d || h_ld % 8 != 0) return ATTT_ERR_INVALID_ARG;
     if (!(inv_temp > 0.f) || !(inv_temp <= 1e4f)) return ATTT_ERR_INVALID_ARG;
-    if (L > (1ll << 30) || V > (1ll << 30) || d > (1ll << 20) || h_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
+    const attt_status st = lp_sizes(L, d, V);
+    if (st != ATTT_OK) return st;
+    if (h_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
     if (!aligned16(d_h) || !aligned16(d_W)) return ATTT_ERR_INVALID_ARG;
     return ATTT_OK;
 }
@@ -677,7 +685,7 @@ static attt_status lp_check(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 
 extern "C" {
 
 size_t attt_logprob_workspace_bytes(int64_t L, int64_t d, int64_t V, int topk) {
-    if (L < 1 || V < 1 || d < 1 || topk < 0 || topk > attt::kLpTopMax) return 0;
+    if (attt::lp_sizes(L, d, V) != ATTT_OK || topk < 0 || topk > attt::kLpTopMax || topk > V) return 0;
     return attt::lp_layout(nullptr, L, d, V, topk).bytes;
 }
 
@@ -757,7 +765,7 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
 }
 
 size_t attt_logprob_grad_workspace_bytes(int64_t L, int64_t d, int64_t V) {
-    if (L < 1 || V < 1 || d < 1) return 0;
+    if (attt::lp_sizes(L, d, V) != ATTT_OK) return 0;
     return attt::grad_layout(nullptr, L, d, V).bytes;
 }
 
