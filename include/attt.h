@@ -357,8 +357,9 @@ ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, co
  * were; m has taken its g.
  * Requirements: 1 <= nproj <= 8, 1 <= r <= 64, 1 <= din, dout <= 2^25,
  * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps >= 1e-12 (fp32 holds its
- * square), 1 <= ns_steps <= 16, all finite, no two matrices alike, d_ws at least
- * attt_lora_muon_workspace_bytes(...) bytes and 256-byte aligned.  One launch.
+ * square), 1 <= ns_steps <= 16, all finite, no two matrices alike, pointers aligned
+ * to their type, d_ws at least attt_lora_muon_workspace_bytes(...) bytes and 256-byte
+ * aligned.  One launch.
  */
 ATTT_API attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_B32,
                                          const float *const *d_dA, const float *const *d_dB, float *const *d_mA,
@@ -512,10 +513,10 @@ ATTT_API size_t attt_logprob_grad_workspace_bytes(int64_t L, int64_t d, int64_t 
  * row with a NaN or +inf logit, or without a finite one, has lse, logp (of a
  * given token) and entropy NaN or -inf as the formulas have.  Requirements: L >= 1,
  * V >= 1, d >= 8 and d % 8 == 0, h_ld >= d and a multiple of 8, d_h and d_W
- * 16-byte aligned, 0 < inv_temp <= 10,000, 0 <= topk <= ATTT_LOGPROB_MAX_TOP and
- * <= V, d_ws at least attt_logprob_workspace_bytes(L, d, V, topk) bytes and
- * 256-byte aligned.  Another token sets ATTT_ERR_TOKEN_RANGE in the device
- * status word and makes its logp NaN.
+ * 16-byte aligned, the others to their type, 0 < inv_temp <= 10,000,
+ * 0 <= topk <= ATTT_LOGPROB_MAX_TOP and <= V, d_ws at least
+ * attt_logprob_workspace_bytes(L, d, V, topk) bytes and 256-byte aligned.  Another
+ * token sets ATTT_ERR_TOKEN_RANGE in the device status word and makes its logp NaN.
  */
 ATTT_API attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_bf16 *d_W,
                                           const int32_t *d_tgt, int64_t L, int64_t d, int64_t V, float inv_temp,

@@ -113,6 +113,11 @@ struct NvtxRange {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned256(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+// Whether all of these (NULL too) lie on multiples of `bytes`.
+template <class... T>
+bool aligned_to(size_t bytes, const T *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) % bytes == 0) && ...);
+}
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
 

@@ -821,7 +821,7 @@ attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, const float *
     if (!ln_type(dtype) || !(eps >= 0.f) || x_ld < d || y_ld < d) return ATTT_ERR_INVALID_ARG;
     if (!d_gamma || (L > 0 && (!d_x || !d_y))) return ATTT_ERR_INVALID_ARG;
     const size_t es = dtype == ATTT_BF16 ? 2 : 4;
-    if (reinterpret_cast<uintptr_t>(d_x) % es || reinterpret_cast<uintptr_t>(d_y) % es) return ATTT_ERR_INVALID_ARG;
+    if (!aligned_to(es, d_x, d_y) || !aligned_to(4, d_gamma, d_beta, d_mean, d_rstd)) return ATTT_ERR_INVALID_ARG;
     attt_status st = ln_sizes(L, d);
     if (st != ATTT_OK) return st;
     if (x_ld > (1ll << 36) || y_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;
@@ -860,8 +860,8 @@ attt_status attt_layer_norm_backward(const void *d_dy, int64_t dy_ld, const void
     if (!ln_type(dtype) || dy_ld < d || x_ld < d || dx_ld < d) return ATTT_ERR_INVALID_ARG;
     if (!d_gamma || (L > 0 && (!d_dy || !d_x || !d_mean || !d_rstd || !d_dx))) return ATTT_ERR_INVALID_ARG;
     const size_t es = dtype == ATTT_BF16 ? 2 : 4;
-    for (const void *p : {d_dy, d_x, (const void *)d_dx})
-        if (reinterpret_cast<uintptr_t>(p) % es) return ATTT_ERR_INVALID_ARG;
+    if (!aligned_to(es, d_dy, d_x, d_dx) || !aligned_to(4, d_gamma, d_mean, d_rstd, d_dgamma, d_dbeta))
+        return ATTT_ERR_INVALID_ARG;
     attt_status st = ln_sizes(L, d);
     if (st != ATTT_OK) return st;
     if (dy_ld > (1ll << 36) || x_ld > (1ll << 36) || dx_ld > (1ll << 36)) return ATTT_ERR_UNSUPPORTED;

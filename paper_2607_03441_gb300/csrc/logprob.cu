@@ -701,6 +701,7 @@ attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, const attt_
         (topk > 0) != (d_top_logp != nullptr) || (topk > 0) != (d_top_id != nullptr))
         return ATTT_ERR_INVALID_ARG;
     if (!d_logp && !d_entropy && !d_lse && topk == 0) return ATTT_ERR_INVALID_ARG;
+    if (!aligned_to(4, d_tgt, d_logp, d_entropy, d_lse, d_top_logp, d_top_id)) return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_logprob_workspace_bytes(L, d, V, topk))
         return ATTT_ERR_WORKSPACE;
     int dev;
@@ -778,6 +779,7 @@ attt_status attt_logprob_input_grad(const attt_bf16 *d_h, int64_t h_ld, const at
     attt_status st = lp_check(d_h, h_ld, d_W, L, d, V, inv_temp);
     if (st != ATTT_OK) return st;
     if (!d_tgt || !d_lse || !d_glogp || (d_gent && !d_entropy) || !d_dh || !aligned16(d_dh)) return ATTT_ERR_INVALID_ARG;
+    if (!aligned_to(4, d_tgt, d_lse, d_entropy, d_glogp, d_gent)) return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_logprob_grad_workspace_bytes(L, d, V)) return ATTT_ERR_WORKSPACE;
     int dev;
     st = current_device(&dev);

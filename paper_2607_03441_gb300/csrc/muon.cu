@@ -916,7 +916,10 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
         ns_steps < 1 || ns_steps > 16)
         return ATTT_ERR_INVALID_ARG;
     for (int i = 0; i < nproj; ++i)
-        if (!d_A32[i] || !d_B32[i] || !d_dA[i] || !d_dB[i] || !d_mA[i] || !d_mB[i]) return ATTT_ERR_INVALID_ARG;
+        if (!d_A32[i] || !d_B32[i] || !d_dA[i] || !d_dB[i] || !d_mA[i] || !d_mB[i] ||
+            !aligned_to(4, d_A32[i], d_B32[i], d_dA[i], d_dB[i], d_mA[i], d_mB[i]) ||
+            !aligned_to(2, d_A16 ? d_A16[i] : nullptr, d_B16 ? d_B16[i] : nullptr))
+            return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_lora_muon_workspace_bytes(nproj, din, dout, r))
         return ATTT_ERR_WORKSPACE;
     int dev;
