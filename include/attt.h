@@ -357,9 +357,9 @@ ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, co
  * were; m has taken its g.
  * Requirements: 1 <= nproj <= 8, 1 <= r <= 64, 1 <= din, dout <= 2^25,
  * 0 <= momentum < 1, weight_decay >= 0, rms > 0, eps >= 1e-12 (fp32 holds its
- * square), 1 <= ns_steps <= 16, all finite, no two matrices alike, pointers aligned
- * to their type, d_ws at least attt_lora_muon_workspace_bytes(...) bytes and 256-byte
- * aligned.  One launch.
+ * square), 1 <= ns_steps <= 16, all finite, no two arrays alike but for gradients,
+ * pointers aligned to their type, d_ws at least attt_lora_muon_workspace_bytes(...)
+ * bytes and 256-byte aligned.  One launch.
  */
 ATTT_API attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_B32,
                                          const float *const *d_dA, const float *const *d_dB, float *const *d_mA,

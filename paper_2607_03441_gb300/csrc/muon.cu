@@ -33,6 +33,7 @@
 #include <algorithm>
 #include <array>
 #include <cmath>
+#include <functional>
 #include <map>
 #include <mutex>
 #include <utility>
@@ -804,6 +805,25 @@ static bool muon_sizes(int nproj, const int64_t *din, const int64_t *dout, int r
     return true;
 }
 
+// Whether no two of a call's arrays start at the same place, but for gradients, which are
+// only read.
+static bool muon_apart(int nproj, float *const *A32, float *const *B32, const float *const *dA,
+                       const float *const *dB, float *const *mA, float *const *mB, attt_bf16 *const *A16,
+                       attt_bf16 *const *B16) {
+    const void *written[3 * kMuonMats];
+    int n = 0;
+    for (int i = 0; i < nproj; ++i)
+        for (const void *p : {(const void *)A32[i], (const void *)B32[i], (const void *)mA[i], (const void *)mB[i],
+                              (const void *)(A16 ? A16[i] : nullptr), (const void *)(B16 ? B16[i] : nullptr)})
+            if (p) written[n++] = p;
+    std::sort(written, written + n, std::less<const void *>());
+    if (std::adjacent_find(written, written + n) != written + n) return false;
+    for (int i = 0; i < nproj; ++i)
+        for (const void *p : {(const void *)dA[i], (const void *)dB[i]})
+            if (std::binary_search(written, written + n, p, std::less<const void *>())) return false;
+    return true;
+}
+
 bool muon_clusters(const void *kern, size_t smem, int dev, int (&most)[kMuonMaxCluster + 1]) {
     static std::mutex mu;
     static std::map<std::pair<const void *, int>, std::array<int, kMuonMaxCluster + 1>> known;
@@ -920,6 +940,7 @@ attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *const *d_
             !aligned_to(4, d_A32[i], d_B32[i], d_dA[i], d_dB[i], d_mA[i], d_mB[i]) ||
             !aligned_to(2, d_A16 ? d_A16[i] : nullptr, d_B16 ? d_B16[i] : nullptr))
             return ATTT_ERR_INVALID_ARG;
+    if (!muon_apart(nproj, d_A32, d_B32, d_dA, d_dB, d_mA, d_mB, d_A16, d_B16)) return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_lora_muon_workspace_bytes(nproj, din, dout, r))
         return ATTT_ERR_WORKSPACE;
     int dev;

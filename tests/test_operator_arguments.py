@@ -113,3 +113,10 @@ def test_muon_refuses_addresses_its_types_do_not_have(lib, name, off):
     if name.endswith("16") and off == 2:
         return  # a bf16 may lie there
     assert _muon(lib, **{name: P + (9 << 12) + off}) == attt.ATTT_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("name,other", [("A32", "A32"), ("B32", "A32"), ("mA", "mA"), ("mB", "A32"), ("dA", "A32"),
+                                        ("dB", "mB"), ("A16", "A16"), ("B16", "A16"), ("A16", "B32")])
+def test_muon_refuses_matrices_that_are_alike(lib, name, other):
+    """What is written belongs to one matrix alone: the step's clusters run at once."""
+    assert _muon(lib, **{name: P + (MUON.index(other) << 12)}) == attt.ATTT_ERR_INVALID_ARG
