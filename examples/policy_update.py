@@ -74,7 +74,7 @@ class Policy:
         attt.attt_logprob_input_grad(n, self.Wlm, tokens, lse, advantage * (-1.0 / L), entropy, gent, self.inv_temp,
                                      dh=self.dn, workspace=self.ws)
         attt.attt_layer_norm_backward(self.dn, self.h, self.gamma, self.mean, self.rstd, dx=self.dh,
-                                      workspace=self.ws)
+                                      workspace=self.ws, weights=False)
         attt.attt_lora_grad(x, [self.dh], [self.A16], [self.B16], self.scale, dAs=[self.dA], dBs=[self.dB],
                             workspace=self.ws)
         return self.dA, self.dB, logp, entropy

@@ -845,17 +845,18 @@ def attt_layer_norm_workspace_bytes(L: int, d: int) -> int:
 def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, mean: torch.Tensor,
                              rstd: torch.Tensor, dx: Optional[torch.Tensor] = None,
                              dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
-                             workspace: Optional[torch.Tensor] = None, stream=None):
+                             workspace: Optional[torch.Tensor] = None, stream=None, weights: bool = True):
     """Gradients of the layer norm's x, gamma and beta from dy (bf16 or fp32 [L, d]),
     with the forward call's mean and rstd.  Returns (dx, dgamma, dbeta): dx of x's
-    type, fp32 [d] twice."""
+    type, fp32 [d] twice.  Without `weights` (a frozen norm) gamma's and beta's are
+    formed only where a tensor for them is given, else None."""
     shape, dtype, code = _norm_check(x)
     L, d = shape
     if dx is None:
         dx = _empty(L, d, dtype=dtype, device=x.device, stream=stream)
-    if dgamma is None:
+    if dgamma is None and weights:
         dgamma = _empty(d, dtype=_F32, device=x.device, stream=stream)
-    if dbeta is None:
+    if dbeta is None and weights:
         dbeta = _empty(d, dtype=_F32, device=x.device, stream=stream)
     if workspace is None:
         workspace = _empty(attt_layer_norm_workspace_bytes(L, d), dtype=torch.uint8, device=x.device, stream=stream)
