@@ -4,8 +4,9 @@
 // fp32 values are split into three bf16 each, x = h + m + l (8 + 8 + 8 bits, exact), and
 // a product of two matrices is six of theirs, l h + h l + m m + m h + h m + h h, the small
 // ones first: what is left out is below 2^-24 of |x| |y|, and what the accumulators
-// truncate is of the order of an fp32 sum's rounding (updates in emulation 1.0e-6 to
-// 2.1e-6 off for singular values over a factor of 1 to 10,000; fp32 FMA 1.5e-6 to 5e-6).
+// truncate is of the order of an fp32 sum's rounding (updates 0.6e-6 to 1.5e-6 off for ranks
+// of 33 to 64, 3,000 columns and singular values over a factor of 1 to 100; the plain steps
+// in fp32 1.1e-6 to 2.6e-6).
 //
 // A CTA's columns of X are kept as three tiles of [column][64] bf16 (128-byte rows,
 // 128-byte swizzle).  Read with the rank along K they are the A operand of X <- P X
@@ -14,12 +15,17 @@
 // other 64 are whatever follows in shared memory, and their results, in the upper
 // TMEM lanes, are never read.  The r x r products are formed by every CTA on its own
 // (1.4 us each; in slabs with an exchange they took 2.1 in muon.cu), so that only the
-// Gram matrices travel.
+// Gram matrices travel.  They are formed without a multiple of I: with M = m I + M', m from
+// the mean of G's diagonal, x y is x'y' by the MMAs and x y' + x'y + x y I in fp32.  An MMA
+// cuts off what its smaller products have below the last bit of its largest, always towards
+// zero, so that a diagonal far above the rest loses some of its own sum in every product:
+// products of the whole matrices left X off by up to 9e-6 where the singular values are alike.
 // Why: on CUDA cores the products were bound by the 128 bytes that shared memory returns
 // per cycle (a 4 x 8 tile per thread: 128 FMAs per 12 vector reads).  The step of q, k, v
 // and o of 5,120 at r 64 (8 matrices, clusters of 12) takes 67 us, 121 with muon.cu's
-// kernel; its bytes would take 7.  Bound: the chain of three Gram matrices with their
-// exchanges, eleven r x r products and three products with X.
+// kernel; its bytes would take 7.  Bound: a chain of loads, three Gram matrices with two
+// exchanges of 0.8 us each, eleven r x r products (with these some 20 us), three products
+// with X and the update; how the rest is shared among its links was not measured.
 #include <algorithm>
 
 #include "muon.cuh"
@@ -246,7 +252,6 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
     float *const R = f0 + (pad + 3 * kTcSplit) / 4;
     float *const part = R + kTcPart, *const recv = R + kTcRecv, *const G = R + kTcG, *const slab = R + kTcSlab;
     const int o_x = (int)(pad / 4);  // the update's fp32 columns, over the tiles
-    __shared__ float s_scale;
     __shared__ __align__(8) uint64_t s_bars[3];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
@@ -310,9 +315,9 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
     // An r x r matrix is in the first two quarters' lanes: row 32 q + lane, columns 16 part4 ..
     const bool mine = q < 2;
     const int row = 32 * q + lane, col = 16 * part4;  // (rows 64 .. 127: the upper lanes)
-    float keep[16];  // this thread's elements of G, fp32
-    // z = alpha x y (+ beta keep) + diag I from the split x at xa and y at ya to za
-    auto product = [&](uint32_t xa, uint32_t ya, uint32_t za, float alpha, float beta, float diag, bool hold) {
+    // z = x y from the split x at xa and y at ya: form(i, v) turns the thread's value i of x y into
+    // that of the matrix that goes to za
+    auto product = [&](uint32_t xa, uint32_t ya, uint32_t za, auto &&form) {
         if (!mine) {
             ++mmas;
             return;
@@ -322,11 +327,7 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
         float v[16];
         tc_read(tmem, q, kTcPoly + col, v);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[i] = fmaf(beta, keep[i], alpha * v[i]);
-            if (col + i == row) v[i] += diag;
-            if (hold) keep[i] = v[i];
-        }
+        for (int i = 0; i < 16; ++i) v[i] = form(i, v[i]);
         tc_put16(za, kTcMat, row, col, v);
         settle_few();
     };
@@ -375,38 +376,47 @@ __global__ void __launch_bounds__(kMuonThreads, 1) muon_tc_kernel(const __grid_c
         });
         link.share<kTcLD>(n + 1, slab, G, r0, r1, 64);
         n += 2;
-        float scale = 1.f;
-        if (gi == 0) {
-            if (warp == 0) {
-                float v = G[lane * (kTcLD + 1)] + G[(lane + 32) * (kTcLD + 1)];
-                for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (lane == 0) s_scale = muon_scale(v, a.eps);
-            }
-            __syncthreads();
-            scale = s_scale;
-        }
+        // every warp for itself: |X|_F^2, the scale of the first one, and the mean d of G's diagonal
+        float trace = G[lane * (kTcLD + 1)] + G[(lane + 32) * (kTcLD + 1)];
+        for (int o = 16; o > 0; o >>= 1) trace += __shfl_xor_sync(0xffffffffu, trace, o);
+        const float scale = gi == 0 ? muon_scale(trace, a.eps) : 1.f;
+        const float d = trace * scale * scale / (float)a.r;
+        // M = m I + M' for each matrix: e, eb and f are this thread's elements of some of the M'
+        float e[16], eb[16], f[16];
         if (mine) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const float4 v = *reinterpret_cast<const float4 *>(G + row * kTcLD + col + i);
-                keep[i] = v.x * scale * scale; keep[i + 1] = v.y * scale * scale;
-                keep[i + 2] = v.z * scale * scale; keep[i + 3] = v.w * scale * scale;
+                e[i] = v.x * scale * scale; e[i + 1] = v.y * scale * scale;
+                e[i + 2] = v.z * scale * scale; e[i + 3] = v.w * scale * scale;
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (col + i == row) e[i] -= d;
         }
         __syncthreads();  // G has been read: the tiles may be written over it
-        if (mine) tc_put16(b1, kTcMat, row, col, keep);
+        if (mine) tc_put16(b1, kTcMat, row, col, e);
         settle();
         // B = a I + b G + c G^2, and for a pair of steps G <- B G B, P = (a I + b G + c G^2) B
+        const float db = fmaf(d, fmaf(kNsC, d, kNsB), kNsA), lin = fmaf(2.f * kNsC, d, kNsB);
         uint32_t P;
         if (gi != single) {
-            product(b1, b1, b2, kNsC, kNsB, kNsA, false);     // B
-            product(b2, b1, b1, 1.f, 0.f, 0.f, false);        // B G
-            product(b1, b2, b1, 1.f, 0.f, 0.f, true);         // G of the second step
-            product(b1, b1, b1, kNsC, kNsB, kNsA, false);     // its B
-            product(b1, b2, b1, scale, 0.f, 0.f, false);
+            const float dt = db * d, d2 = dt * db, db2 = fmaf(d2, fmaf(kNsC, d2, kNsB), kNsA),
+                        lin2 = fmaf(2.f * kNsC, d2, kNsB), dp = scale * (db2 * db);
+            product(b1, b1, b2, [&](int i, float v) { return eb[i] = fmaf(kNsC, v, lin * e[i]); });           // B
+            product(b2, b1, b1, [&](int i, float v) { return f[i] = fmaf(db, e[i], fmaf(d, eb[i], v)); });    // B G
+            product(b1, b2, b1, [&](int i, float v) { return e[i] = fmaf(dt, eb[i], fmaf(db, f[i], v)); });   // second G
+            product(b1, b1, b1, [&](int i, float v) { return f[i] = fmaf(kNsC, v, lin2 * e[i]); });           // its B
+            product(b1, b2, b1, [&](int i, float v) {
+                const float p = scale * fmaf(db2, eb[i], fmaf(db, f[i], v));
+                return col + i == row ? p + dp : p;
+            });
             P = b1;
         } else {
-            product(b1, b1, b2, kNsC * scale, kNsB * scale, kNsA * scale, false);
+            product(b1, b1, b2, [&](int i, float v) {
+                const float p = scale * fmaf(kNsC, v, lin * e[i]);
+                return col + i == row ? fmaf(scale, db, p) : p;
+            });
             P = b2;
         }
         __syncthreads();
