@@ -338,7 +338,8 @@ ATTT_API attt_status attt_lora_adamw_step(float *d_A32, float *d_B32, const floa
 ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, const int64_t *dout, int r);
 
 /*
- * A step along orthogonalised momentum (Muon) as a third alternative, for nproj
+ * A step along orthogonalised momentum (Muon) in the place of the two above, for a
+ * caller's own loop (attt_episode_* takes SGD or AdamW, attt_batch_* SGD), for nproj
  * projections at once (host arrays of nproj device pointers and sizes): for each
  * matrix X of A_p [din[p], r] and B_p [r, dout[p]] with gradient g and momentum m
  * (fp32, caller-owned, zero before the first step):
@@ -349,9 +350,11 @@ ATTT_API size_t attt_lora_muon_workspace_bytes(int nproj, const int64_t *din, co
  *   p <- p (1 - lr weight_decay) - lr rms sqrt(max(rows, columns)) X
  * so that the update's root mean square is about lr rms.  The bf16 copies are
  * refreshed (round to nearest even) when the arrays d_A16, d_B16 and their
- * entries are not NULL.  fp32 products and sums; a zero gradient with zero
- * momentum (the dA of B = 0) gives X = 0.  A matrix with a NaN or an infinity in u,
- * or with |u|_F^2 beyond fp32, becomes NaN as a whole; the others do not feel it.
+ * entries are not NULL.  Products and sums are those of fp32 or better (ranks up to
+ * 5: pairs of fp32 and 64 bits; 33 to 64: fp32 values as three bf16 each, summed in
+ * fp32); a zero gradient with zero momentum (the dA of B = 0) gives X = 0.  A matrix
+ * with a NaN or an infinity in u, or with |u|_F^2 beyond fp32, becomes NaN as a whole;
+ * the others do not feel it.
  * Where a wait of the kernel runs out (ATTT_ERR_TIMEOUT in the device status word),
  * the columns of p whose X it left incomplete, and their bf16 copies, stay as they
  * were; m has taken its g.
@@ -453,10 +456,11 @@ typedef enum attt_dtype { ATTT_BF16 = 0, ATTT_F32 = 1 } attt_dtype;
  *   mean_j = mean(x_j),  rstd_j = 1 / sqrt(mean((x_j - mean_j)^2) + eps)
  *   y_j = (x_j - mean_j) rstd_j gamma + beta   (type `dtype`, at d_y + j y_ld)
  * gamma and beta fp32 [d] (beta NULL: none), d_mean and d_rstd fp32 [L] (either may
- * be NULL).  All sums fp32, one rounding at the end.  Requirements: L >= 0 (0
- * launches nothing), 1 <= d <= 2^24, x_ld, y_ld >= d, eps >= 0, pointers aligned to
- * their type.  Rows whose addresses are multiples of 16 bytes are read and
- * written 16 bytes at a time, others value by value.
+ * be NULL).  All sums fp32, one rounding at the end; a row whose squares' sum is
+ * beyond fp32 has rstd 0.  Requirements: L >= 0 (0 launches nothing),
+ * 1 <= d <= 2^24, x_ld, y_ld >= d, eps >= 0, pointers aligned to their type.  Fastest
+ * where x, y, gamma and beta lie on 16 bytes and rows and their distances are
+ * multiples of 16 bytes long.
  */
 ATTT_API attt_status attt_layer_norm_forward(const void *d_x, int64_t x_ld, const float *d_gamma,
                                              const float *d_beta, int64_t L, int64_t d, float eps, int dtype,
@@ -474,7 +478,7 @@ ATTT_API size_t attt_layer_norm_workspace_bytes(int64_t L, int64_t d);
  *                                                        NULL; zeros for L = 0)
  * The sums over the rows are fp32 in a fixed order.  Requirements as above, d_ws at
  * least attt_layer_norm_workspace_bytes(L, d) bytes and 256-byte aligned.  Two
- * launches.
+ * launches, or one where dgamma and dbeta are NULL.
  */
 ATTT_API attt_status attt_layer_norm_backward(const void *d_dy, int64_t dy_ld, const void *d_x, int64_t x_ld,
                                               const float *d_gamma, const float *d_mean, const float *d_rstd,
@@ -532,7 +536,8 @@ ATTT_API attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, co
  * with a_j = glogp_j, or 0 where t_j = -1.  d_gent (and then d_entropy) may be
  * NULL: no entropy term.  dz is rounded to bf16 once, but for the given token's,
  * which counts in full (up to 64 rows: all of it to two bf16); products are bf16,
- * sums fp32.  No gradient for W (it is frozen).  Requirements as above, d_dh
+ * sums fp32.  p is exp(z inv_temp - lse), so that lse's own rounding, 2^-24 |lse|, is
+ * p's relative error.  No gradient for W (it is frozen).  Requirements as above, d_dh
  * 16-byte aligned, d_ws at least attt_logprob_grad_workspace_bytes(L, d, V) bytes.
  * Another token sets ATTT_ERR_TOKEN_RANGE and makes its row NaN.
  */

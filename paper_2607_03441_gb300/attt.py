@@ -595,7 +595,7 @@ def attt_lora_forward(x: torch.Tensor, W0: torch.Tensor, A: torch.Tensor, B: tor
         h = _empty(L, dout, dtype=torch.bfloat16, device=x.device, stream=stream)
     if workspace is None:
         workspace = _empty(attt_lora_forward_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
-                                device=x.device, stream=stream)
+                           device=x.device, stream=stream)
     _check((_lib or load_library()).attt_lora_forward(
         _bf16(x), _bf16(W0), _bf16(A), _bf16(B), L, din, dout, int(r), float(scale), _bf16(h), _ptr(workspace),
         workspace.numel(), _stream(stream)), "attt_lora_forward")
@@ -617,7 +617,7 @@ def attt_lora_input_grad(dy: torch.Tensor, W0: torch.Tensor, A: torch.Tensor, B:
         dx = _empty(L, din, dtype=torch.float32, device=dy.device, stream=stream)
     if workspace is None:
         workspace = _empty(attt_lora_input_grad_workspace_bytes(L, din, dout, r), dtype=torch.uint8,
-                                device=dy.device, stream=stream)
+                           device=dy.device, stream=stream)
     _check((_lib or load_library()).attt_lora_input_grad(
         _bf16(dy), _bf16(W0), _bf16(A), _bf16(B), L, din, dout, int(r), float(scale), _ptr(dx), _ptr(workspace),
         workspace.numel(), _stream(stream)), "attt_lora_input_grad")
@@ -1153,7 +1153,7 @@ def attt_lora_muon_step(A32s: Sequence[torch.Tensor], B32s: Sequence[torch.Tenso
                 _expect(t, shape, dtype, f"{name}[{i}]")
     if workspace is None:
         workspace = _empty(attt_lora_muon_workspace_bytes(dins, douts, r), dtype=torch.uint8,
-                                device=A32s[0].device, stream=stream)
+                           device=A32s[0].device, stream=stream)
     vals = dins + douts
     for ts in (A32s, B32s, dAs, dBs, mAs, mBs, A16s or (), B16s or ()):
         vals += [_ptr(t) or 0 for t in ts]

@@ -22,9 +22,10 @@
 // issue slots and waits: hence two values per instruction, few warps per row, and no
 // branches between a thread's vectors.
 // Figures (8,192 rows, both kernels of the backward): 5,120 bf16 32 us forward (77% of
-// the copy bandwidth) and 47-50 backward (75-80%); 5,001 bf16 43 and 81, 5,001 fp32 63
-// and 88.  One block per row without the ring took 47 and 148, and value by value from
-// global memory 176 and 310 at 5,001 bf16.
+// the copy bandwidth) and 47-50 backward (75-80%; 48 without the weights' sums); 5,001 bf16
+// 43 and 81, 5,001 fp32 63 and 88, value by value from the window.  One block per row
+// without the ring took 47 and 148, and value by value from global memory 176 and 310 at
+// 5,001 bf16.
 #include <algorithm>
 
 #include "attt_common.cuh"
@@ -533,7 +534,8 @@ __global__ void __launch_bounds__(kLnThreads, 1)
 // ---------------------------------------------------------------------------
 // Rows that no ring holds (d from about 16,000, backward 8,000, on): a block per row at
 // a time, value by value, from L2 after the first read; the backward's sums stay in
-// the block's partial rows.
+// the block's partial rows.  2,048 rows x 20,480: bf16 67 us forward and 241 backward, fp32
+// 94 and 259 (bytes: 25, 37, 49 and 74).
 // ---------------------------------------------------------------------------
 
 constexpr int kLnWide = 1024;

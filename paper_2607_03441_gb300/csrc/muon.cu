@@ -24,12 +24,15 @@
 // all of them, sums, and gives it to all; up to r 16 each gets all of it from all.  At
 // r > 32 the r x r products are formed in slabs too; below that one or two warps of
 // every CTA form all of it, which takes less time than an exchange.  Exchanges are bulk
-// copies between the CTAs' shared memories counted on mbarriers (measured at 8 / 12 to 16 CTAs of 512 threads, 17 KB to each: 0.8 us; plain
-// stores and a cluster barrier 1.1 / 1.6).  fp32 FMA throughout: the Gram matrices need
-// their 24 bits.  Ranks up to 5 and (where the columns fit) of 33 to 64 have kernels of
-// their own, below and in muon_tc.cu.
+// copies between the CTAs' shared memories counted on mbarriers (measured at 8 / 12 to 16
+// CTAs of 512 threads, 17 KB to each: 0.8 us; plain stores and a cluster barrier 1.1 /
+// 1.6).  fp32 FMA throughout: the Gram matrices need their 24 bits.  Ranks up to 5 and
+// (where the columns of every matrix of the call fit) of 33 to 64 have kernels of their
+// own, below and in muon_tc.cu.
 // Bound: fp32 FMA issue at r 64 (5 r^2 n of them), exchanges and launch below.  The step of
-// q and v of 3,584 at r 16 (4 matrices, clusters of 16) takes 22.7 us, its bytes 0.6.
+// q and v of 3,584 at r 16 (4 matrices, clusters of 16) takes 23 us, its bytes 0.6; of
+// seven projections up to 18,944 wide 128 us at r 8, 386 at r 32 and, on this kernel for
+// all of them, 1,170 at r 64.
 #include <algorithm>
 #include <array>
 #include <cmath>
