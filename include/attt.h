@@ -534,7 +534,8 @@ ATTT_API attt_status attt_logprob_forward(const attt_bf16 *d_h, int64_t h_ld, co
  *   dz_jv = inv_temp (a_j [v = t_j] - p_jv (a_j + gent_j (log p_jv + entropy_j)))
  *   d_dh[j, :] = sum_v dz_jv W_v                                   (bf16 [L, d])
  * with a_j = glogp_j, or 0 where t_j = -1.  d_gent (and then d_entropy) may be
- * NULL: no entropy term.  dz is rounded to bf16 once, but for the given token's,
+ * NULL: no entropy term.  A row with t_j = -1 and no entropy term, or gent_j = 0, has
+ * d_dh = 0 whatever h_j holds (padding).  dz is rounded to bf16 once, but for the given token's,
  * which counts in full (up to 64 rows: all of it to two bf16); products are bf16,
  * sums fp32.  p is exp(z inv_temp - lse), so that lse's own rounding, 2^-24 |lse|, is
  * p's relative error.  No gradient for W (it is frozen).  Requirements as above, d_dh

@@ -786,7 +786,8 @@ __device__ __forceinline__ void logp_flush(const GemmArgs &g, const Span &s, Log
 // average out (1 to 4 rows: up to 2.9e-3), keep all of what is lost as a second block
 // (G_lo), rows that the second contraction's tiles have room for.
 // Columns past N within the tile are stored as zeros.  A row without a given token
-// (t < 0) has a = 0; an invalid target makes its row NaN.
+// (t = -1) has a = 0, and is 0 where its entropy does not count either; an invalid target
+// makes its row NaN.
 template <int SETS>
 __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_base, int tn, int set, int row,
                                                    uint32_t taddr, const CUtensorMap *tmE,
@@ -803,8 +804,10 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
     // z / T log2 e and lse log2 e, which peaked rows (lse 130) feel in 1 - p
     float lse = 0.f, A = 0.f, B = 0.f, at = 0.f;
     int t = -1;
+    bool empty = false;  // the row counts nowhere: 0, whatever its logits are (NaN times 0 is not)
     if (rv) {
         t = __ldg(ep.tgt + gm);
+        empty = t == -1 && !ep.gent;
         float a = t == -1 ? 0.f : __ldg(ep.glogp + gm);
         if (t < -1 || t >= ep.V) {
             if (tn == 0 && set == 0) record_error(g.status, ATTT_ERR_TOKEN_RANGE);
@@ -815,6 +818,7 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
         A = at;
         if (ep.gent) {
             const float b = __ldg(ep.gent + gm);
+            empty = t == -1 && b == 0.f;
             A = fmaf(b * ep.inv_temp, __ldg(ep.entropy + gm), at);
             B = b * ep.inv_temp;
         }
@@ -828,7 +832,7 @@ __device__ __forceinline__ void epilogue_logp_grad(const GemmArgs &g, int gm_bas
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             const float lp = fmaf(v[i], ep.inv_temp, -lse);
-            v[i] = -ex2(lp * kLog2e) * fmaf(B, fmaxf(lp, -1e4f), A);
+            v[i] = empty ? 0.f : -ex2(lp * kLog2e) * fmaf(B, fmaxf(lp, -1e4f), A);
         }
         if (tc >= 0 && tc < 32) {
 #pragma unroll
