@@ -11,7 +11,8 @@ blocks, with their plain forms:
              of the gate and up projections, from which the adapters'
              gradients follow (attt_gated_ffn_backward);
   adamw      the AdamW step of all adapters of a model at once, with moments in
-             32 bits or in 8 (attt_adamw_step, attt_adamw_read_state).
+             32 bits or in 8 (attt_adamw_create, attt_adamw_step,
+             attt_adamw_read_state).
 
 Where `own` is false, run() computes them from elementary torch operations in
 32 bits.  Ranges (draw): 1 to 8,192 rows; 1 to 64 heads of 32 to 256 values,
@@ -439,30 +440,28 @@ def _call_ffn_grad(s):
     return out
 
 
-def _views(s):
-    """The tensors in the program's buffers."""
-    cut = {name: [s[name][a:a + n] for a, n in zip(s["starts"], s["sizes"])] for name in ("p", "g", "m", "v", "p16")}
+def _optimizer(s):
+    """The handle over the tensors in the program's buffers."""
+    from paper_2607_03441_gb300 import attt
+    t = {name: [s[name][a:a + n] for a, n in zip(s["starts"], s["sizes"])] for name in ("p", "g", "m", "v", "p16")}
+    scales = {}
     if s["bits"] == 8:
-        starts = [a // BLOCK for a in s["starts"]]
         for name in ("ms", "vs"):
-            cut[name] = [s[name][a:a + b] for a, b in zip(starts, s["blocks"])]
-        for name in ("m32", "v32"):
-            s[name] = torch.zeros_like(s["p"])
-            cut[name] = [s[name][a:a + n] for a, n in zip(s["starts"], s["sizes"])]
-    return cut
+            scales[name[0] + "_scales"] = [s[name][a // BLOCK:a // BLOCK + b] for a, b in zip(s["starts"], s["blocks"])]
+    return attt.attt_adamw_create(t["p"], t["g"], t["m"], t["v"], p16s=t["p16"], **scales)
 
 
 def _call_adamw(s):
     from paper_2607_03441_gb300 import attt
-    t = _kept(s, "views", lambda: _views(s))
+    opt = _kept(s, "opt", lambda: _optimizer(s))
     s["step"] += 1
-    scales = {"m_scales": t["ms"], "v_scales": t["vs"], "seed": s["step"]} if s["bits"] == 8 else {}
-    attt.attt_adamw_step(t["p"], t["g"], t["m"], t["v"], LR, betas=(BETA1, BETA2), eps=ADAM_EPS, weight_decay=DECAY,
-                         step=s["step"], p16s=t["p16"], **scales)
+    attt.attt_adamw_step(opt, LR, betas=(BETA1, BETA2), eps=ADAM_EPS, weight_decay=DECAY, step=s["step"],
+                         seed=s["step"])
     if s["bits"] == 32:
         return {name: s[name] for name in ("p", "p16", "m", "v")}
-    attt.attt_adamw_read_state(t["m"], t["v"], t["ms"], t["vs"], m32s=t["m32"], v32s=t["v32"])
-    return {"p": s["p"], "p16": s["p16"], "m": s["m32"], "v": s["v32"]}
+    m, v = _kept(s, "values", lambda: (torch.empty_like(s["p"]), torch.empty_like(s["p"])))
+    attt.attt_adamw_read_state(opt, m, v)
+    return {"p": s["p"], "p16": s["p16"], "m": m, "v": v}
 
 
 _calls = {"rope": _call_rope, "rope_grad": _call_rope_grad, "ffn": _call_ffn, "ffn_grad": _call_ffn_grad,
