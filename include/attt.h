@@ -21,7 +21,7 @@
  *
  * Conventions shared by every call:
  *   - Pointers named d_* are device pointers on the current CUDA device; the
- *     caller owns them.  The library owns only attt_history objects.
+ *     caller owns them.  The library owns only the objects that it creates.
  *   - bf16 tensors are passed as attt_bf16 (the IEEE binary32 upper half).
  *   - Matrices are row-major with the last dimension contiguous.
  *   - Every call is asynchronous on `stream` (a cudaStream_t; NULL = the
@@ -372,6 +372,66 @@ ATTT_API attt_status attt_lora_muon_step(int nproj, float *const *d_A32, float *
                                          size_t ws_bytes, attt_stream stream);
 
 /* ------------------------------------------------------------------------ */
+/* AdamW over many tensors (the adapters of all of a model's projections) in */
+/* one launch, with moments in 32 bits or in 8.                              */
+/* ------------------------------------------------------------------------ */
+
+typedef struct attt_adamw attt_adamw;
+
+/* Values that share a scale where moments are held in 8 bits. */
+#define ATTT_ADAMW_BLOCK 256
+
+/*
+ * A step over `count` tensors of n[k] values on the current device: parameters d_p[k] and
+ * gradients d_g[k] (fp32), moments d_m[k] and d_v[k], and bf16 copies d_p16[k] (the array or an
+ * entry NULL: none).  The arrays are HOST arrays, copied; the tensors are the caller's, borrowed,
+ * and stay where they are while the handle lives.
+ *   state_bits = 32: moments fp32, zero before the first step; d_ms and d_vs NULL.
+ *   state_bits = 8:  moments uint8, with fp32 scales d_ms[k], d_vs[k] per block of
+ *     ATTT_ADAMW_BLOCK values (the last one shorter), codes and scales zero before the first
+ *     step.  A code c with exponent e = c >> k (4 bits) and c's low k bits as l stands for
+ *     (1 + l 2^-k) 2^(e - 15), or l 2^(-14 - k) where e = 0, times its block's scale: m in
+ *     bits 0 to 6 with k = 3 and its sign in bit 7; sqrt(v) in 8 bits with k = 4.
+ * Requirements: count >= 1, n[k] >= 0, pointers aligned to their type, and no two of the
+ * arrays that a step writes sharing a byte, nor a gradient lying in one of them
+ * (ATTT_ERR_INVALID_ARG).  Allocates and copies a table (not during a stream capture).
+ * *out is set on success.
+ */
+ATTT_API attt_status attt_adamw_create(int count, float *const *d_p, const float *const *d_g, void *const *d_m,
+                                       void *const *d_v, float *const *d_ms, float *const *d_vs,
+                                       attt_bf16 *const *d_p16, const int64_t *n, int state_bits, attt_adamw **out);
+
+/* Frees the handle's table (synchronises the device), not the tensors. */
+ATTT_API attt_status attt_adamw_destroy(attt_adamw *h);
+
+/*
+ * One step of every tensor, `step` = 1 for the first, formulas and rounding as
+ * attt_lora_adamw_step (with moments in 32 bits the same bits):
+ *   p <- p (1 - lr wd);  m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
+ *   p <- p - (lr / (1 - b1^step)) m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * p from the moments before they are rounded to 8 bits.  Those are divided by a scale that makes
+ * a block's largest |m| (sqrt(v)) the largest code's, and rounded to a neighbouring code, upwards
+ * with the probability of what is cut off (in 2^-16), by a hash of (seed, k, index): a caller
+ * gives every step another seed, and the same seed repeats a step bit for bit.  A block whose
+ * largest value is below 2^-100 becomes zeros, one with a NaN or an infinity NaN as a whole;
+ * with 32 bits only its own value feels it.  Requirements: 0 <= b1, b2 < 1, eps > 0 in
+ * fp32, weight_decay >= 0, step >= 1, all finite; the handle's device current.  One launch; a
+ * captured step repeats its own `step` and seed.
+ */
+ATTT_API attt_status attt_adamw_step(attt_adamw *h, double lr, double beta1, double beta2, double eps,
+                                     double weight_decay, int64_t step, uint64_t seed, attt_stream stream);
+
+/* Values that attt_adamw_read_state writes to each of its arrays: every tensor's, rounded up to whole blocks. */
+ATTT_API int64_t attt_adamw_state_values(const attt_adamw *h);
+
+/*
+ * The moments as fp32 values (for a checkpoint, or to go on in 32 bits): tensor k's from value
+ * ATTT_ADAMW_BLOCK (sum of ceil(n[j] / ATTT_ADAMW_BLOCK), j < k) on, zeros behind its last.  Either
+ * array may be NULL, not both; 16-byte aligned.
+ */
+ATTT_API attt_status attt_adamw_read_state(const attt_adamw *h, float *d_m32, float *d_v32, attt_stream stream);
+
+/* ------------------------------------------------------------------------ */
 /* The adapted projection of a chained update: the LoRA-adapted linear map   */
 /* y = x W0 + s (x A) B (Appendix C adapter; W0 frozen) whose output is the  */
 /* LM head's input h, so that the second gradient step of an update         */
@@ -485,6 +545,130 @@ ATTT_API attt_status attt_layer_norm_backward(const void *d_dy, int64_t dy_ld, c
                                               int64_t L, int64_t d, int dtype, void *d_dx, int64_t dx_ld,
                                               float *d_dgamma, float *d_dbeta, void *d_ws, size_t ws_bytes,
                                               attt_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Queries and keys of an adapted block, between their projections and the  */
+/* attention: the norm of every head and the position rotation in one pass, */
+/* and its gradient.                                                        */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Rotation frequencies w_i, i < rot / 2, as the calls below take them: turns per
+ * position in units of 2^-64, written to host_freq (a HOST array of rot / 2; the
+ * caller copies it to the device once).  w_i = base^(-2 i / rot) radians, scaled for
+ * contexts longer than those trained on:
+ *   context = 0:  w_i / factor for every i (positions divided by factor);
+ *   context > 0:  pairs that turn more than `high` times over `context` positions keep
+ *                 w_i, those that turn less than `low` times take w_i / factor, and
+ *                 between them w_i (k + (1 - k) / factor) with
+ *                 k = (context w_i / (2 pi) - low) / (high - low).
+ * factor = 1: no scaling.  Requirements: rot even, 2 <= rot <= 512, base >= 1,
+ * factor >= 1, context >= 0, 0 <= low < high (context > 0), all finite.  Host-only.
+ */
+ATTT_API attt_status attt_rope_frequencies(int64_t rot, double base, double factor, double context, double low,
+                                           double high, uint64_t *host_freq);
+
+/*
+ * One of up to two tensors of a call (queries, keys): `heads` heads of D values for
+ * each of T tokens, token t's head h at t ld + h hs elements; they may lie in the rows of
+ * one projection's output, and tokens may follow heads or heads tokens.
+ */
+typedef struct attt_rope_part {
+    const void *d_x;            /* the heads (backward: the forward call's; NULL where d_gamma is) */
+    void *d_y;                  /* result (backward: the gradient of d_x)                          */
+    const void *d_dy;           /* backward: the gradient of the forward call's result             */
+    const float *d_gamma;       /* fp32 [D] weight of the norm; NULL: no norm                      */
+    float *d_dgamma;            /* backward: its gradient, fp32 [D]; NULL: not wanted              */
+    int64_t x_ld, x_hs, y_ld, y_hs, dy_ld, dy_hs;
+    int heads;
+} attt_rope_part;
+
+/*
+ * For every head x of every part (`dtype` values, at token t's position pos = d_pos[t]):
+ *   z = x / sqrt(mean(x^2) + eps) gamma     (gamma given; else z = x)
+ *   y = z with the pairs (a, b) of its first `rot` values turned by pos w_i:
+ *       (a, b) -> mscale (a cos - b sin, a sin + b cos)
+ * pair i being values i and i + rot / 2, or 2 i and 2 i + 1 (interleaved != 0); the other
+ * D - rot values stay z's.  d_pos int32 [T] (any values), d_freq uint64 [rot / 2]
+ * (attt_rope_frequencies).  fp32 arithmetic, angles exact to 2^-64 of a turn per position,
+ * one rounding at the end.  y may be x itself, with the same strides.  Requirements:
+ * 1 <= nparts <= 2, T >= 0 (0 launches nothing), D even, 2 <= D <= 512, rot even,
+ * 0 <= rot <= D (0: the norm alone), 1 <= heads <= 65,536, eps >= 0, mscale finite,
+ * strides >= 0, results' heads apart from each other, pointers aligned to their type.
+ * Fastest where heads begin on 16 bytes and rot / 2 (interleaved: rot) and D are multiples
+ * of 16 and 32 bytes.  One launch.
+ */
+ATTT_API attt_status attt_rope_forward(const attt_rope_part *parts, int nparts, const int32_t *d_pos,
+                                       const uint64_t *d_freq, int64_t T, int64_t D, int64_t rot, float eps,
+                                       int interleaved, float mscale, int dtype, attt_stream stream);
+
+/* Workspace bytes attt_rope_backward needs.  0 for sizes that it refuses. */
+ATTT_API size_t attt_rope_workspace_bytes(int64_t T, int64_t D);
+
+/*
+ * The gradients of the forward call's x and gamma from that of y (d_dy), with the same
+ * arguments; dz is dy turned back (and times mscale), xh = x / sqrt(mean(x^2) + eps):
+ *   dx = (dz gamma - xh mean(dz gamma xh)) / sqrt(mean(x^2) + eps)    (`dtype`; no norm: dz)
+ *   dgamma = sum over tokens and heads of dz xh                        (fp32, in a fixed order;
+ *                                                                       zeros for T = 0)
+ * d_y may be d_dy or d_x itself, with the same strides.  d_ws, at least
+ * attt_rope_workspace_bytes(T, D) bytes and 256-byte aligned, may be NULL where no dgamma is
+ * wanted.  One launch, or two with a dgamma.
+ */
+ATTT_API attt_status attt_rope_backward(const attt_rope_part *parts, int nparts, const int32_t *d_pos,
+                                        const uint64_t *d_freq, int64_t T, int64_t D, int64_t rot, float eps,
+                                        int interleaved, float mscale, int dtype, void *d_ws, size_t ws_bytes,
+                                        attt_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* The gated feed-forward block with an adapter on each of its projections, */
+/* forward and gradient.                                                    */
+/* ------------------------------------------------------------------------ */
+
+/* Activations of the gate: g / (1 + exp(-g)), and g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2. */
+typedef enum attt_activation { ATTT_SILU = 0, ATTT_GELU_TANH = 1 } attt_activation;
+
+/* Workspace bytes of the two calls below (r = 0: no adapters).  0 for sizes that they refuse. */
+ATTT_API size_t attt_gated_ffn_workspace_bytes(int64_t L, int64_t d, int64_t f, int r);
+
+/*
+ * With x = d_x (bf16 [L, d]), Wg, Wu (bf16 [d, f]), Wd (bf16 [f, d]) frozen, and adapters
+ * (A_0, B_0) of the gate, (A_1, B_1) of the up and (A_2, B_2) of the down projection, bf16
+ * A_0, A_1 [d, r], A_2 [f, r], B_0, B_1 [r, f], B_2 [r, d], s = scale:
+ *   g = x Wg + s (x A_0) B_0,  u = x Wu + s (x A_1) B_1
+ *   h = act(g) u                    (bf16 [L, f] into d_h, wanted by the adapters' gradients)
+ *   y = h Wd + s (h A_2) B_2        (bf16 [L, d] into d_y)
+ * d_g and d_u (bf16 [L, f], both or neither) receive g and u for the backward call; h is
+ * formed from them in fp32.  d_A and d_B are HOST arrays of three device pointers, NULL both
+ * (and r = 0) for no adapters; a projection without one has NULL in both.  s (x A) and
+ * s (h A_2) are rounded to bf16 once, as h is for y; products are bf16, sums fp32.
+ * Requirements: L >= 0 (0 launches nothing), d, f >= 8 and multiples of 8, 0 <= r <= 64,
+ * tensor pointers 16-byte aligned, d_ws at least attt_gated_ffn_workspace_bytes(L, d, f, r)
+ * bytes and 256-byte aligned.  Two to seven launches.
+ */
+ATTT_API attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, const attt_bf16 *d_Wu,
+                                            const attt_bf16 *d_Wd, const attt_bf16 *const *d_A,
+                                            const attt_bf16 *const *d_B, int64_t L, int64_t d, int64_t f, int r,
+                                            float scale, int act, attt_bf16 *d_y, attt_bf16 *d_h, attt_bf16 *d_g,
+                                            attt_bf16 *d_u, void *d_ws, size_t ws_bytes, attt_stream stream);
+
+/*
+ * The gradients of the forward call's factors and input from that of y (dy = d_dy, bf16
+ * [L, d]), with the forward call's g and u:
+ *   dh = dy Wd^T + s (dy B_2^T) A_2^T        (in fp32, not kept)
+ *   dg = dh u act'(g),  du = dh act(g)       (bf16 [L, f])
+ *   dx = dg Wg^T + s (dg B_0^T) A_0^T + du Wu^T + s (du B_1^T) A_1^T   (bf16 [L, d])
+ * d_dx may be NULL: not wanted.  dg and du are the upstream gradients that attt_lora_grad takes
+ * for the gate's and up's adapters, dy with h in the place of x for the down's.  dx is
+ * formed from dg and du as rounded to bf16; the products with B^T are rounded to bf16 once.
+ * Requirements as above.  Two to seven launches.
+ */
+ATTT_API attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg, const attt_bf16 *d_Wu,
+                                             const attt_bf16 *d_Wd, const attt_bf16 *const *d_A,
+                                             const attt_bf16 *const *d_B, const attt_bf16 *d_g, const attt_bf16 *d_u,
+                                             int64_t L, int64_t d, int64_t f, int r, float scale, int act,
+                                             attt_bf16 *d_dx, attt_bf16 *d_dg, attt_bf16 *d_du, void *d_ws,
+                                             size_t ws_bytes, attt_stream stream);
 
 /* ------------------------------------------------------------------------ */
 /* Log probabilities through the frozen LM head: of given tokens, with the  */

@@ -64,6 +64,14 @@ class BatchConfig(ctypes.Structure):
                 ("lr", ctypes.c_float), ("grad_steps", ctypes.c_int)]
 
 
+class RopePart(ctypes.Structure):
+    """attt_rope_part (field order and types as in attt.h)."""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("gamma", ctypes.c_void_p),
+                ("dgamma", ctypes.c_void_p), ("x_ld", ctypes.c_int64), ("x_hs", ctypes.c_int64),
+                ("y_ld", ctypes.c_int64), ("y_hs", ctypes.c_int64), ("dy_ld", ctypes.c_int64),
+                ("dy_hs", ctypes.c_int64), ("heads", ctypes.c_int)]
+
+
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Loads libattt.so (raises if it has not been built)."""
     global _lib
@@ -128,6 +136,19 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "attt_layer_norm_forward": (i32, [P, i64, P, P, i64, i64, f32, i32, P, i64, P, P, P]),
             "attt_layer_norm_workspace_bytes": (sz, [i64, i64]),
             "attt_layer_norm_backward": (i32, [P, i64, P, i64, P, P, P, i64, i64, i32, P, i64, P, P, P, sz, P]),
+            "attt_rope_frequencies": (i32, [i64, f64, f64, f64, f64, f64, P]),
+            "attt_rope_forward": (i32, [P, i32, P, P, i64, i64, i64, f32, i32, f32, i32, P]),
+            "attt_rope_workspace_bytes": (sz, [i64, i64]),
+            "attt_rope_backward": (i32, [P, i32, P, P, i64, i64, i64, f32, i32, f32, i32, P, sz, P]),
+            "attt_gated_ffn_workspace_bytes": (sz, [i64, i64, i64, i32]),
+            "attt_gated_ffn_forward": (i32, [P, P, P, P, P, P, i64, i64, i64, i32, f32, i32, P, P, P, P, P, sz, P]),
+            "attt_gated_ffn_backward": (i32, [P, P, P, P, P, P, P, P, i64, i64, i64, i32, f32, i32, P, P, P, P, sz,
+                                              P]),
+            "attt_adamw_create": (i32, [i32, P, P, P, P, P, P, P, P, i32, ctypes.POINTER(P)]),
+            "attt_adamw_destroy": (i32, [P]),
+            "attt_adamw_step": (i32, [P, f64, f64, f64, f64, f64, i64, ctypes.c_uint64, P]),
+            "attt_adamw_state_values": (i64, [P]),
+            "attt_adamw_read_state": (i32, [P, P, P, P]),
             "attt_logprob_workspace_bytes": (sz, [i64, i64, i64, i32]),
             "attt_logprob_grad_workspace_bytes": (sz, [i64, i64, i64]),
             "attt_logprob_forward": (i32, [P, i64, P, P, i64, i64, i64, f32, i32, P, P, P, P, P, P, sz, P]),
@@ -869,6 +890,340 @@ def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Ten
         code, po, o_ld, _f32_of(dgamma, vec, "dgamma"), _f32_of(dbeta, vec, "dbeta"), _ptr(workspace),
         workspace.numel(), _stream(stream)), "attt_layer_norm_backward")
     return dx, dgamma, dbeta
+
+
+# --------------------------------------------------------------------------
+# queries and keys: norm of the heads and position rotation
+# --------------------------------------------------------------------------
+
+def attt_rope_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, context: float = 0.0, low: float = 1.0,
+                          high: float = 32.0, device=None) -> torch.Tensor:
+    """Rotation frequencies (int64 [rot / 2], 2^-64 turns per position), made once: `factor`
+    and `context` scale them for longer contexts.  On `device` (None: the CPU)."""
+    rot = int(rot)
+    out = torch.empty(max(rot // 2, 0), dtype=torch.int64)
+    _check(load_library().attt_rope_frequencies(rot, float(base), float(factor), float(context), float(low),
+                                                float(high), out.data_ptr()), "attt_rope_frequencies")
+    return out if device is None else out.to(device)
+
+
+def _heads(t: torch.Tensor, shape, dtype, name: str):
+    """(address, strides of tokens and heads) of heads whose values are contiguous."""
+    if t.shape != shape or t.dtype != dtype:
+        _expect(t, shape, dtype, name)
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    ld, hs, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: expected heads whose values are contiguous")
+    return t.data_ptr(), ld, hs
+
+
+def _rope_check(xs, pos, freq, gammas):
+    """(number of parts, shapes, type, its name in the C ABI, rot)."""
+    k = len(xs)
+    if k < 1 or k > 2:
+        raise ValueError("one or two tensors of heads are expected")
+    if gammas is not None and len(gammas) != k:
+        raise ValueError("gammas must have one entry per tensor")
+    if xs[0].dim() != 3:
+        raise ValueError(f"expected [T, heads, D] tensors, got shape {tuple(xs[0].shape)}")
+    T, _, D = xs[0].shape
+    dtype = xs[0].dtype
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"expected bfloat16 or float32 heads, got {dtype}")
+    for t in xs:
+        if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D:
+            raise ValueError(f"expected [{T}, heads, {D}] tensors, got shape {tuple(t.shape)}")
+    _expect(pos, (T,), torch.int32, "pos")
+    if freq.dtype != torch.int64 or freq.dim() != 1:
+        raise ValueError("freq: expected an int64 vector (attt_rope_frequencies)")
+    return T, D, dtype, code, 2 * freq.shape[0]
+
+
+def attt_rope_forward(xs: Sequence[torch.Tensor], pos: torch.Tensor, freq: torch.Tensor,
+                      gammas: Optional[Sequence[Optional[torch.Tensor]]] = None, eps: float = 1e-6,
+                      interleaved: bool = False, mscale: float = 1.0, ys: Optional[Sequence[torch.Tensor]] = None,
+                      stream=None):
+    """Norm (where gammas has a weight, fp32 [D]) and rotation of the heads of one or two
+    tensors (bf16 or fp32 [T, heads, D], any strides of tokens and heads) at the positions
+    pos (int32 [T]).  Returns ys (they may be xs)."""
+    T, D, dtype, code, rot = _rope_check(xs, pos, freq, gammas)
+    if ys is None:
+        ys = [_empty(x.shape, dtype=dtype, device=x.device, stream=stream) for x in xs]
+    elif len(ys) != len(xs):
+        raise ValueError("ys must have one entry per tensor")
+    parts = (RopePart * len(xs))()
+    for i, (p, x, y) in enumerate(zip(parts, xs, ys)):
+        p.x, p.x_ld, p.x_hs = _heads(x, x.shape, dtype, "xs")
+        p.y, p.y_ld, p.y_hs = _heads(y, x.shape, dtype, "ys")
+        p.gamma = _f32_of(gammas[i], (D,), "gammas") if gammas is not None else None
+        p.heads = x.shape[1]
+    _check((_lib or load_library()).attt_rope_forward(
+        ctypes.addressof(parts), len(xs), _ptr(pos), _ptr(freq), T, D, rot, eps, 1 if interleaved else 0, mscale, code,
+        _stream(stream)), "attt_rope_forward")
+    return ys
+
+
+def attt_rope_workspace_bytes(T: int, D: int) -> int:
+    return int(load_library().attt_rope_workspace_bytes(int(T), int(D)))
+
+
+def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Optional[torch.Tensor]]], pos: torch.Tensor,
+                       freq: torch.Tensor, gammas: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                       eps: float = 1e-6, interleaved: bool = False, mscale: float = 1.0,
+                       dxs: Optional[Sequence[torch.Tensor]] = None,
+                       dgammas: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None, weights: bool = True):
+    """Gradients of the forward call's xs and gammas from dys.  xs may be None (or have None)
+    where there is no norm.  Returns (dxs, dgammas): fp32 [D] or None each; without
+    `weights` (frozen norms) dgammas are formed only where tensors for them are given."""
+    T, D, dtype, code, rot = _rope_check(dys, pos, freq, gammas)
+    k = len(dys)
+    dev = dys[0].device
+    if xs is not None and len(xs) != k or dxs is not None and len(dxs) != k or dgammas is not None and len(dgammas) != k:
+        raise ValueError("xs, dxs and dgammas must have one entry per tensor")
+    if dxs is None:
+        dxs = [_empty(t.shape, dtype=dtype, device=dev, stream=stream) for t in dys]
+    if dgammas is None:
+        dgammas = [_empty(D, dtype=_F32, device=dev, stream=stream)
+                   if weights and gammas is not None and gammas[i] is not None else None for i in range(k)]
+    parts = (RopePart * k)()
+    sums = False
+    for i, (p, dy, dx, dg) in enumerate(zip(parts, dys, dxs, dgammas)):
+        p.dy, p.dy_ld, p.dy_hs = _heads(dy, dy.shape, dtype, "dys")
+        p.y, p.y_ld, p.y_hs = _heads(dx, dy.shape, dtype, "dxs")
+        if gammas is not None and gammas[i] is not None:
+            if xs is None or xs[i] is None:
+                raise ValueError("xs: the norm's gradient needs the forward call's heads")
+            p.x, p.x_ld, p.x_hs = _heads(xs[i], dy.shape, dtype, "xs")
+            p.gamma = _f32_of(gammas[i], (D,), "gammas")
+            p.dgamma = _f32_of(dg, (D,), "dgammas")
+            sums = sums or dg is not None
+        elif dg is not None:
+            raise ValueError("dgammas: there is no norm to have a gradient")
+        p.heads = dy.shape[1]
+    if workspace is None and sums:
+        workspace = _empty(attt_rope_workspace_bytes(T, D), dtype=torch.uint8, device=dev, stream=stream)
+    _check((_lib or load_library()).attt_rope_backward(
+        ctypes.addressof(parts), k, _ptr(pos), _ptr(freq), T, D, rot, eps, 1 if interleaved else 0, mscale, code,
+        _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)), "attt_rope_backward")
+    return dxs, dgammas
+
+
+# --------------------------------------------------------------------------
+# the gated feed-forward block
+# --------------------------------------------------------------------------
+
+_ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+_BF16 = torch.bfloat16
+
+
+def attt_gated_ffn_workspace_bytes(L: int, d: int, f: int, r: int = 0) -> int:
+    return int(load_library().attt_gated_ffn_workspace_bytes(int(L), int(d), int(f), int(r)))
+
+
+def _bf16_of(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
+    """_expect (bfloat16) and _ptr in one."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != _BF16:
+        _expect(t, shape, _BF16, name)
+    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
+
+
+def _ffn_check(x: torch.Tensor, Wg: torch.Tensor, Wu, Wd, As, Bs, act: str):
+    """(L, d, f, r, code of the activation, addresses of x and the weights, the C call's
+    arrays of adapters with the addresses of A and B)."""
+    if x.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("expected 2-D activations and weights")
+    L, d = x.shape
+    f = Wg.shape[1]
+    code = _ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError(f"act: expected one of {sorted(_ACTIVATIONS)}, got {act!r}")
+    w = (_bf16_of(x, (L, d), "x or dy"), _bf16_of(Wg, (d, f), "Wg"), _bf16_of(Wu, (d, f), "Wu"),
+         _bf16_of(Wd, (f, d), "Wd"))
+    if (As is None) != (Bs is None) or As is not None and (len(As) != 3 or len(Bs) != 3):
+        raise ValueError("As and Bs must have three entries each (gate, up, down), or both be None")
+    given = [A for A in As if A is not None] if As is not None else []
+    if not given:
+        if Bs is not None and any(B is not None for B in Bs):
+            raise ValueError("As and Bs must have None in the same places")
+        return L, d, f, 0, code, w, None, None, None
+    if given[0].dim() != 2:
+        raise ValueError("As: expected 2-D tensors")
+    r = given[0].shape[1]
+    buf = (ctypes.c_int64 * 6)()
+    for i, (A, B) in enumerate(zip(As, Bs)):
+        if (A is None) != (B is None):
+            raise ValueError("As and Bs must have None in the same places")
+        if A is not None:
+            wide, out = (f, d) if i == 2 else (d, f)
+            buf[i] = _bf16_of(A, (wide, r), f"As[{i}]")
+            buf[3 + i] = _bf16_of(B, (r, out), f"Bs[{i}]")
+    at = ctypes.addressof(buf)
+    return L, d, f, r, code, w, buf, at, at + 24
+
+
+def attt_gated_ffn_forward(x: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor,
+                           As: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                           Bs: Optional[Sequence[Optional[torch.Tensor]]] = None, scale: float = 1.0,
+                           act: str = "silu", y: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None,
+                           g: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None, save: bool = False):
+    """The block y = h Wd + s (h A_2) B_2, h = act(g) u, with g and u projections of x (all
+    bf16; As and Bs: the adapters of gate, up and down, or None).  Returns (y, h, g, u);
+    g and u, which the backward call takes, where `save` asks for them or tensors are given."""
+    L, d, f, r, code, w, keep, pA, pB = _ffn_check(x, Wg, Wu, Wd, As, Bs, act)
+    dev = x.device
+    if y is None:
+        y = _empty(L, d, dtype=_BF16, device=dev, stream=stream)
+    if h is None:
+        h = _empty(L, f, dtype=_BF16, device=dev, stream=stream)
+    if save or g is not None or u is not None:
+        if g is None:
+            g = _empty(L, f, dtype=_BF16, device=dev, stream=stream)
+        if u is None:
+            u = _empty(L, f, dtype=_BF16, device=dev, stream=stream)
+    if workspace is None:
+        workspace = _empty(attt_gated_ffn_workspace_bytes(L, d, f, r), dtype=torch.uint8, device=dev, stream=stream)
+    _check((_lib or load_library()).attt_gated_ffn_forward(
+        *w, pA, pB, L, d, f, r, scale, code, _bf16_of(y, (L, d), "y"), _bf16_of(h, (L, f), "h"),
+        _bf16_of(g, (L, f), "g"), _bf16_of(u, (L, f), "u"), _ptr(workspace), workspace.numel(), _stream(stream)),
+        "attt_gated_ffn_forward")
+    return y, h, g, u
+
+
+def attt_gated_ffn_backward(dy: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, g: torch.Tensor,
+                            u: torch.Tensor, As: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                            Bs: Optional[Sequence[Optional[torch.Tensor]]] = None, scale: float = 1.0,
+                            act: str = "silu", dx: Optional[torch.Tensor] = None, dg: Optional[torch.Tensor] = None,
+                            du: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None,
+                            input_grad: bool = True):
+    """The block's gradients from dy, with the forward call's g and u.  Returns (dx, dg, du):
+    dg and du are the upstream gradients of the gate's and up's adapters.  Without
+    `input_grad`, dx is formed only where a tensor for it is given."""
+    L, d, f, r, code, w, keep, pA, pB = _ffn_check(dy, Wg, Wu, Wd, As, Bs, act)
+    dev = dy.device
+    if dx is None and input_grad:
+        dx = _empty(L, d, dtype=_BF16, device=dev, stream=stream)
+    if dg is None:
+        dg = _empty(L, f, dtype=_BF16, device=dev, stream=stream)
+    if du is None:
+        du = _empty(L, f, dtype=_BF16, device=dev, stream=stream)
+    if workspace is None:
+        workspace = _empty(attt_gated_ffn_workspace_bytes(L, d, f, r), dtype=torch.uint8, device=dev, stream=stream)
+    _check((_lib or load_library()).attt_gated_ffn_backward(
+        *w, pA, pB, _bf16_of(g, (L, f), "g"), _bf16_of(u, (L, f), "u"), L, d, f, r, scale, code,
+        _bf16_of(dx, (L, d), "dx"), _bf16_of(dg, (L, f), "dg"), _bf16_of(du, (L, f), "du"), _ptr(workspace),
+        workspace.numel(), _stream(stream)), "attt_gated_ffn_backward")
+    return dx, dg, du
+
+
+# --------------------------------------------------------------------------
+# AdamW over many tensors
+# --------------------------------------------------------------------------
+
+ADAMW_BLOCK = 256
+
+
+class AdamW:
+    """Owning handle of an attt_adamw (destroyed with the object).  The tensors are
+    borrowed by the library: this object keeps references to them."""
+
+    def __init__(self, ps, gs, ms, vs, m_scales=None, v_scales=None, p16s=None):
+        self.handle = None
+        k = len(ps)
+        if k < 1:
+            raise ValueError("at least one tensor is required")
+        bits8 = ms[0].dtype == torch.uint8 if len(ms) else False
+        lists = [("ps", ps, _F32), ("gs", gs, _F32), ("ms", ms, torch.uint8 if bits8 else _F32),
+                 ("vs", vs, torch.uint8 if bits8 else _F32)]
+        if (m_scales is None) != (v_scales is None) or bits8 != (m_scales is not None):
+            raise ValueError("moments in 8 bits (uint8), and no others, have m_scales and v_scales")
+        device = ps[0].device
+        arrays = []
+        for name, ts, dtype in lists + [("p16s", p16s, _BF16), ("m_scales", m_scales, _F32), ("v_scales", v_scales, _F32)]:
+            if ts is None:
+                arrays.append(None)
+                continue
+            if len(ts) != k:
+                raise ValueError(f"{name} must have one entry per tensor")
+            vals = []
+            for i, (t, p) in enumerate(zip(ts, ps)):
+                if t is None and name == "p16s":
+                    vals.append(0)
+                    continue
+                shape = (-(-p.numel() // ADAMW_BLOCK),) if name.endswith("scales") else p.shape
+                _expect(t, shape, dtype, f"{name}[{i}]")
+                if t.device != device:
+                    raise ValueError(f"{name}[{i}]: expected a tensor on {device}")
+                vals.append(_ptr(t) if t.numel() else 0)
+            arrays.append((ctypes.c_int64 * k)(*vals))
+        sizes = (ctypes.c_int64 * k)(*[t.numel() for t in ps])
+        p, g, m, v, p16, sm, sv = (None if a is None else ctypes.addressof(a) for a in arrays)
+        self._lib = load_library()
+        h = ctypes.c_void_p()
+        with torch.cuda.device(device):
+            _check(self._lib.attt_adamw_create(k, p, g, m, v, sm, sv, p16, ctypes.addressof(sizes), 8 if bits8 else 32,
+                                               ctypes.byref(h)), "attt_adamw_create")
+        self.handle = h
+        self.bits, self.device = 8 if bits8 else 32, device
+        self._keep = (list(ps), list(gs), list(ms), list(vs), m_scales and list(m_scales), v_scales and list(v_scales),
+                      p16s and list(p16s))
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            self._lib.attt_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def attt_adamw_create(ps: Sequence[torch.Tensor], gs: Sequence[torch.Tensor], ms: Sequence[torch.Tensor],
+                      vs: Sequence[torch.Tensor], m_scales: Optional[Sequence[torch.Tensor]] = None,
+                      v_scales: Optional[Sequence[torch.Tensor]] = None,
+                      p16s: Optional[Sequence[Optional[torch.Tensor]]] = None) -> AdamW:
+    """A step over the parameters ps (fp32) with gradients gs (fp32) and moments ms and vs (fp32,
+    or uint8 with fp32 scales per ADAMW_BLOCK values; zeros before the first step), and bf16
+    copies p16s."""
+    return AdamW(ps, gs, ms, vs, m_scales, v_scales, p16s)
+
+
+def attt_adamw_destroy(opt: AdamW) -> None:
+    opt.close()
+
+
+def attt_adamw_step(opt: AdamW, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                    step: int = 1, seed: int = 0, stream=None) -> None:
+    """One step of every tensor (`step` = 1 for the first; another seed each, where moments are
+    in 8 bits)."""
+    _check((_lib or load_library()).attt_adamw_step(opt.handle, lr, betas[0], betas[1], eps, weight_decay, step,
+                                                    int(seed) & 0xFFFFFFFFFFFFFFFF, _stream(stream)), "attt_adamw_step")
+
+
+def attt_adamw_state_values(opt: AdamW) -> int:
+    """Values of attt_adamw_read_state's arrays."""
+    return int(load_library().attt_adamw_state_values(opt.handle))
+
+
+def attt_adamw_read_state(opt: AdamW, m32: Optional[torch.Tensor] = None, v32: Optional[torch.Tensor] = None,
+                          stream=None):
+    """The moments' values (fp32 [attt_adamw_state_values], every tensor from its first block
+    on).  Returns (m32, v32)."""
+    n = attt_adamw_state_values(opt)
+    if m32 is None and v32 is None:
+        m32, v32 = (_empty(n, dtype=_F32, device=opt.device, stream=stream) for _ in range(2))
+    pm, pv = _f32_of(m32, (n,), "m32"), _f32_of(v32, (n,), "v32")
+    _check((_lib or load_library()).attt_adamw_read_state(opt.handle, pm if n else None, pv if n else None,
+                                                          _stream(stream)) if n else ATTT_OK, "attt_adamw_read_state")
+    return m32, v32
 
 
 # --------------------------------------------------------------------------

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 #include <stddef.h>
@@ -96,6 +97,18 @@ attt_status batch_grads(const attt_bf16 *d_x, const attt_bf16 *d_dy, const int64
 attt_status batch_input_grad(const attt_bf16 *d_dy, const int64_t *off, int E, const attt_bf16 *d_W0, int64_t din,
                              int64_t d, int r, float scale, float *d_dx, int64_t rows_bound, void *d_ws,
                              size_t ws_bytes, cudaStream_t stream);
+
+// Products of activations with an adapter's matrix (lora.cu): out16[m, i rpad + c] =
+// bf16(scale (a_i M_i)[m, c]), c < rpad = r rounded up to 16, for n <= 2 activations a_i (bf16
+// [L, K]) and M_i [K, r] (mn; r a multiple of 8) or M_i^T [r, K].  `pdl`: launched
+// as a dependent of the stream's previous kernel, which it waits for.
+struct RankProduct {
+    const void *a, *m;
+    int64_t K;
+    bool mn;
+};
+attt_status rank_products(int n, const RankProduct *list, int64_t L, int r, int rpad, float scale,
+                          __nv_bfloat16 *out16, bool pdl, int dev, cudaStream_t stream);
 
 // Device address of attt_lora_grad_noalloc's static status word on `dev`, or
 // nullptr if that entry point has not been set up on the device.

@@ -534,6 +534,35 @@ static attt_status skinny_project(const attt_bf16 *d_a, const void *d_m, int64_t
     return launch_skinny<false>(maps, g, cdiv(L, 128), c, pdl, dev, stream);
 }
 
+// out16[m, i rpad + c] = bf16(scale sum_k a_i[m, k] M_i[k, c]) for c < rpad (zero past r), the
+// products of the gated feed-forward block's adapters (ffn.cu): on as many CTAs per
+// 128-row tile as are resident together, else one.
+attt_status rank_products(int n, const RankProduct *list, int64_t L, int r, int rpad, float scale,
+                          __nv_bfloat16 *out16, bool pdl, int dev, cudaStream_t stream) {
+    SkinnyMaps maps;
+    SkinnyArgs g{};
+    const int64_t rows = cdiv(L, 128);
+    int64_t kb = cdiv(list[0].K, 64);
+    for (int i = 1; i < n; ++i) kb = cdiv(list[i].K, 64) < kb ? cdiv(list[i].K, 64) : kb;
+    int c = skinny_cluster(rows * n, kb, dev);
+    if (c < 1) c = 1;
+    for (int i = 0; i < n; ++i) {
+        const RankProduct &q = list[i];
+        if (!tmap_a(&maps.a[i], q.a, q.K, L)) return ATTT_ERR_INVALID_ARG;
+        const bool ok = q.mn ? make_tmap_bf16(&maps.b[i], q.m, (uint64_t)r, (uint64_t)q.K, (uint64_t)r * 2, 64, 64)
+                             : make_tmap_bf16(&maps.b[i], q.m, (uint64_t)q.K, (uint64_t)r, (uint64_t)q.K * 2, 64,
+                                              (uint32_t)rpad);
+        if (!ok) return ATTT_ERR_INVALID_ARG;
+        SkinnySeg &s = g.seg[i];
+        s.a = s.b = i; s.nb = 1; s.n = rpad; s.b_mn = q.mn ? 1 : 0; s.kb = (int)cdiv(q.K, 64); s.N = rpad;
+        s.out = GOUT_N16; s.alpha = scale; s.r = r; s.rpad = rpad; s.ld = (int64_t)n * rpad;
+        s.out16 = out16 + (int64_t)i * rpad;
+        g.grp[i] = SkinnyGroup{(int)(rows * i), c, i, 1, (int)L, rpad, {}};
+    }
+    g.ngroup = g.nmaps_a = g.nmaps_b = n;
+    return launch_skinny<false>(maps, g, rows * n, c, pdl, dev, stream);
+}
+
 // How the passes of attt_lora_grad run as skinny launches: the clusters of each
 // pass; whether pass 1 gives u and every v_p of a row tile to one cluster
 // (merged) or to one each; and in pass 2, how many tiles of a dB_p share a
