@@ -405,8 +405,9 @@ ATTT_API attt_status attt_adamw_create(int count, float *const *d_p, const float
 ATTT_API attt_status attt_adamw_destroy(attt_adamw *h);
 
 /*
- * One step of every tensor, `step` = 1 for the first, formulas and rounding as
- * attt_lora_adamw_step (with moments in 32 bits the same bits):
+ * One step of every tensor, `step` = 1 for the first, with the formulas of
+ * attt_lora_adamw_step, and with moments in 32 bits its rounding and so the same bits (in 8
+ * bits m and v are rounded as there, and the update of p is good to 2^-21 of itself):
  *   p <- p (1 - lr wd);  m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
  *   p <- p - (lr / (1 - b1^step)) m / (sqrt(v) / sqrt(1 - b2^step) + eps)
  * p from the moments before they are rounded to 8 bits.  Those are divided by a scale that makes

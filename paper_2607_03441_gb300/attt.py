@@ -908,38 +908,44 @@ def attt_rope_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, 
 
 
 def _heads(t: torch.Tensor, shape, dtype, name: str):
-    """(address, strides of tokens and heads) of heads whose values are contiguous."""
+    """Address and strides of tokens and heads of a [T, heads, D] tensor whose values are
+    contiguous."""
     if t.shape != shape or t.dtype != dtype:
         _expect(t, shape, dtype, name)
+    ld, hs, one = t.stride()
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    ld, hs, one = t.stride()
     if one != 1 and shape[2] > 1:
         raise ValueError(f"{name}: expected heads whose values are contiguous")
     return t.data_ptr(), ld, hs
 
 
 def _rope_check(xs, pos, freq, gammas):
-    """(number of parts, shapes, type, its name in the C ABI, rot)."""
+    """(T, D, type, its name in the C ABI) of a call's heads."""
     k = len(xs)
     if k < 1 or k > 2:
         raise ValueError("one or two tensors of heads are expected")
     if gammas is not None and len(gammas) != k:
         raise ValueError("gammas must have one entry per tensor")
-    if xs[0].dim() != 3:
-        raise ValueError(f"expected [T, heads, D] tensors, got shape {tuple(xs[0].shape)}")
-    T, _, D = xs[0].shape
-    dtype = xs[0].dtype
+    shape, dtype = xs[0].shape, xs[0].dtype
+    if len(shape) != 3:
+        raise ValueError(f"expected [T, heads, D] tensors, got shape {tuple(shape)}")
+    T, _, D = shape
     code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError(f"expected bfloat16 or float32 heads, got {dtype}")
-    for t in xs:
-        if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D:
-            raise ValueError(f"expected [{T}, heads, {D}] tensors, got shape {tuple(t.shape)}")
-    _expect(pos, (T,), torch.int32, "pos")
+    if k == 2:
+        other = xs[1].shape
+        if len(other) != 3 or other[0] != T or other[2] != D:
+            raise ValueError(f"expected [{T}, heads, {D}] tensors, got shape {tuple(other)}")
+    if pos.shape != (T,) or pos.dtype != torch.int32:
+        _expect(pos, (T,), torch.int32, "pos")
     if freq.dtype != torch.int64 or freq.dim() != 1:
         raise ValueError("freq: expected an int64 vector (attt_rope_frequencies)")
-    return T, D, dtype, code, 2 * freq.shape[0]
+    return T, D, dtype, code
+
+
+_ROPE_PARTS = {k: ctypes.c_int64 * (12 * k) for k in (1, 2)}  # attt_rope_part's words
 
 
 def attt_rope_forward(xs: Sequence[torch.Tensor], pos: torch.Tensor, freq: torch.Tensor,
@@ -949,25 +955,27 @@ def attt_rope_forward(xs: Sequence[torch.Tensor], pos: torch.Tensor, freq: torch
     """Norm (where gammas has a weight, fp32 [D]) and rotation of the heads of one or two
     tensors (bf16 or fp32 [T, heads, D], any strides of tokens and heads) at the positions
     pos (int32 [T]).  Returns ys (they may be xs)."""
-    T, D, dtype, code, rot = _rope_check(xs, pos, freq, gammas)
+    T, D, dtype, code = _rope_check(xs, pos, freq, gammas)
     if ys is None:
         ys = [_empty(x.shape, dtype=dtype, device=x.device, stream=stream) for x in xs]
     elif len(ys) != len(xs):
         raise ValueError("ys must have one entry per tensor")
-    parts = (RopePart * len(xs))()
-    for i, (p, x, y) in enumerate(zip(parts, xs, ys)):
-        p.x, p.x_ld, p.x_hs = _heads(x, x.shape, dtype, "xs")
-        p.y, p.y_ld, p.y_hs = _heads(y, x.shape, dtype, "ys")
-        p.gamma = _f32_of(gammas[i], (D,), "gammas") if gammas is not None else None
-        p.heads = x.shape[1]
+    words = []
+    for i, x in enumerate(xs):
+        shape = x.shape
+        px, x_ld, x_hs = _heads(x, shape, dtype, "xs")
+        py, y_ld, y_hs = _heads(ys[i], shape, dtype, "ys")
+        g = gammas[i] if gammas is not None else None
+        words += (px, py, 0, 0 if g is None else _f32_of(g, (D,), "gammas"), 0, x_ld, x_hs, y_ld, y_hs, 0, 0, shape[1])
+    parts = _ROPE_PARTS[len(xs)](*words)
     _check((_lib or load_library()).attt_rope_forward(
-        ctypes.addressof(parts), len(xs), _ptr(pos), _ptr(freq), T, D, rot, eps, 1 if interleaved else 0, mscale, code,
-        _stream(stream)), "attt_rope_forward")
+        ctypes.addressof(parts), len(xs), _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0,
+        mscale, code, _stream(stream)), "attt_rope_forward")
     return ys
 
 
 def attt_rope_workspace_bytes(T: int, D: int) -> int:
-    return int(load_library().attt_rope_workspace_bytes(int(T), int(D)))
+    return int((_lib or load_library()).attt_rope_workspace_bytes(int(T), int(D)))
 
 
 def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Optional[torch.Tensor]]], pos: torch.Tensor,
@@ -979,7 +987,7 @@ def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Option
     """Gradients of the forward call's xs and gammas from dys.  xs may be None (or have None)
     where there is no norm.  Returns (dxs, dgammas): fp32 [D] or None each; without
     `weights` (frozen norms) dgammas are formed only where tensors for them are given."""
-    T, D, dtype, code, rot = _rope_check(dys, pos, freq, gammas)
+    T, D, dtype, code = _rope_check(dys, pos, freq, gammas)
     k = len(dys)
     dev = dys[0].device
     if xs is not None and len(xs) != k or dxs is not None and len(dxs) != k or dgammas is not None and len(dgammas) != k:
@@ -989,26 +997,32 @@ def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Option
     if dgammas is None:
         dgammas = [_empty(D, dtype=_F32, device=dev, stream=stream)
                    if weights and gammas is not None and gammas[i] is not None else None for i in range(k)]
-    parts = (RopePart * k)()
+    words = []
     sums = False
-    for i, (p, dy, dx, dg) in enumerate(zip(parts, dys, dxs, dgammas)):
-        p.dy, p.dy_ld, p.dy_hs = _heads(dy, dy.shape, dtype, "dys")
-        p.y, p.y_ld, p.y_hs = _heads(dx, dy.shape, dtype, "dxs")
-        if gammas is not None and gammas[i] is not None:
+    for i, dy in enumerate(dys):
+        shape = dy.shape
+        pdy, dy_ld, dy_hs = _heads(dy, shape, dtype, "dys")
+        pdx, dx_ld, dx_hs = _heads(dxs[i], shape, dtype, "dxs")
+        px = x_ld = x_hs = pg = pdg = 0
+        g, dg = gammas[i] if gammas is not None else None, dgammas[i]
+        if g is not None:
             if xs is None or xs[i] is None:
                 raise ValueError("xs: the norm's gradient needs the forward call's heads")
-            p.x, p.x_ld, p.x_hs = _heads(xs[i], dy.shape, dtype, "xs")
-            p.gamma = _f32_of(gammas[i], (D,), "gammas")
-            p.dgamma = _f32_of(dg, (D,), "dgammas")
-            sums = sums or dg is not None
+            px, x_ld, x_hs = _heads(xs[i], shape, dtype, "xs")
+            pg = _f32_of(g, (D,), "gammas")
+            if dg is not None:
+                pdg = _f32_of(dg, (D,), "dgammas")
+                sums = True
         elif dg is not None:
             raise ValueError("dgammas: there is no norm to have a gradient")
-        p.heads = dy.shape[1]
+        words += (px, pdx, pdy, pg, pdg, x_ld, x_hs, dx_ld, dx_hs, dy_ld, dy_hs, shape[1])
+    parts = _ROPE_PARTS[k](*words)
     if workspace is None and sums:
         workspace = _empty(attt_rope_workspace_bytes(T, D), dtype=torch.uint8, device=dev, stream=stream)
     _check((_lib or load_library()).attt_rope_backward(
-        ctypes.addressof(parts), k, _ptr(pos), _ptr(freq), T, D, rot, eps, 1 if interleaved else 0, mscale, code,
-        _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)), "attt_rope_backward")
+        ctypes.addressof(parts), k, _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0, mscale,
+        code, _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)),
+        "attt_rope_backward")
     return dxs, dgammas
 
 

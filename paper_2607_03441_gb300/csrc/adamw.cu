@@ -4,7 +4,7 @@
 //   m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
 //   p <- p (1 - lr wd) - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 // with every operation rounded on its own, as attt_lora_adamw_step: with moments in 32
-// bits the two give the same bits.
+// bits the two give the same bits (in 8 bits p's quotients are approximate, m and v are not).
 //
 // Moments in 8 bits: blocks of 256 values with one fp32 scale each.  A code is a number of 4
 // exponent bits and k mantissa bits (exponent 0: without the leading one): 0 to 2 - 2^-k in
@@ -21,6 +21,8 @@
 // reduction over the warp.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
+#include <memory>
 #include <new>
 #include <type_traits>
 #include <utility>
@@ -32,7 +34,9 @@
 namespace attt {
 
 constexpr int kAdamBlock = 256;  // values of a scale, and of a warp's step
-constexpr int kAdamWarps = 8;
+constexpr int kAdamWarps = 4;
+constexpr int kAdamStep8 = 5, kAdamStep32 = 5, kAdamRead = 10;  // blocks per SM
+constexpr int kAdamAhead = 1;  // blocks of a warp that are asked for before their turn
 constexpr float kAdamTiny = 0x1p-100f;  // blocks without a value of this size are 0
 
 struct AdamTensor {
@@ -49,10 +53,10 @@ struct AdamTensor {
 
 struct AdamArgs {
     const AdamTensor *tensors;
+    const int64_t *first;  // first block of each
     int count;
     int64_t blocks;
-    int steps;  // of each warp
-    float decay, b1, one_b1, b2, one_b2, step_size, bc2_sqrt, eps;
+    float decay, b1, one_b1, b2, one_b2, step_size, bc2_sqrt, inv_bc2, eps;
     uint32_t seed_lo, seed_hi;
     float *m32, *v32;  // adam_read_kernel
 };
@@ -67,19 +71,30 @@ __host__ __device__ __forceinline__ uint32_t adam_mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-template <int K>
-__device__ __forceinline__ float adam_decode(uint32_t code) {
-    const uint32_t low = code & ((1u << K) - 1u), e = code >> K;
-    return e > 0u ? __uint_as_float(((e + 112u) << 23) | (low << (23 - K))) : (float)low * (1.f / (float)(1 << (14 + K)));
+__device__ __forceinline__ float2 adam_two(float v) { return make_float2(v, v); }
+
+// b x + c y with each product and the sum rounded on its own.  (Pairs, mul and add of f32x2, are
+// contracted to one rounding less even as .rn: measured by scales a last bit off.)
+__device__ __forceinline__ float adam_blend(float b, float x, float c, float y) {
+    return __fadd_rn(__fmul_rn(b, x), __fmul_rn(c, y));
+}
+
+// Codes as fp32: their exponent and mantissa bits, at those of an fp32, are the code's value times
+// 2^-112, exponent 0 among fp32's own numbers without a leading one.
+
+// The value of byte j of w, a code (SIGN: with its sign in bit 7).
+template <int K, bool SIGN>
+__device__ __forceinline__ float adam_decode(uint32_t w, int j) {
+    constexpr int up = 23 - K;
+    const uint32_t c = (up >= 8 * j ? w << (up - 8 * j) : w >> (8 * j - up)) & ((16u << K) - 1u) << up;
+    const uint32_t s = SIGN ? (w << (24 - 8 * j)) & 0x80000000u : 0u;
+    return __uint_as_float(c | s) * 0x1p112f;
 }
 
 // The code of a in [0, 2 - 2^-K]; rnd: 23 - K random bits.
 template <int K>
 __device__ __forceinline__ uint32_t adam_encode(float a, uint32_t rnd) {
-    constexpr int cut = 23 - K;
-    const uint32_t big = ((__float_as_uint(a) + rnd) >> cut) - (112u << K);
-    const uint32_t small = ((uint32_t)(a * 0x1p37f) + rnd) >> cut;  // used below 2^-14: under 2^23
-    return min(a >= 0x1p-14f ? big : small, (16u << K) - 1u);
+    return min((__float_as_uint(__fmul_rz(a, 0x1p-112f)) + rnd) >> (23 - K), (16u << K) - 1u);
 }
 
 // A block's scale and its inverse from the bits of its largest size (a NaN's are the largest).
@@ -94,13 +109,17 @@ __device__ __forceinline__ float adam_scale(uint32_t top_bits, float &inv) {
     return s;
 }
 
-// The tensor that has block b: the last one whose first block is not after it.
-__device__ __forceinline__ int adam_find(const AdamTensor *t, int count, int64_t b) {
-    int lo = 0, hi = count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (__ldg(&t[mid].block0) <= b) lo = mid;
-        else hi = mid;
+// The tensor that has block b, the last one whose first block is not after it: 32 candidates at a
+// time, one per lane (a search by halves is a chain of seven loads for 112 tensors, 4 us of a
+// step of 33).
+__device__ __forceinline__ int adam_find(const int64_t *first, int count, int64_t b, int lane) {
+    int lo = 0, n = count;  // it is among [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) / 32, i = lane * step;
+        const bool before = i < n && __ldg(first + lo + i) <= b;  // (lane 0's is)
+        const int k = __popc(__ballot_sync(0xffffffffu, before)) - 1;
+        lo += k * step;
+        n = min(step, n - k * step);
     }
     return lo;
 }
@@ -110,170 +129,220 @@ struct alignas(sizeof(T) * N) AdamRun {
     T v[N];
 };
 
-// Four neighbouring values from i on, those from n on as zeros.
-template <class T>
-__device__ __forceinline__ AdamRun<T, 4> adam_load(const T *p, int64_t i, int64_t n, bool whole) {
-    if (whole) return *reinterpret_cast<const AdamRun<T, 4> *>(p + i);
+// Four neighbouring values from i on.  Not WHOLE: value by value, those from n on as zeros.
+template <bool WHOLE, class T>
+__device__ __forceinline__ AdamRun<T, 4> adam_load(const T *p, int64_t i, int64_t n) {
     AdamRun<T, 4> r{};
+    if constexpr (WHOLE) {
+        r = *reinterpret_cast<const AdamRun<T, 4> *>(p + i);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (i + k < n) r.v[k] = p[i + k];
+        for (int k = 0; k < 4; ++k)
+            if (i + k < n) r.v[k] = p[i + k];
+    }
     return r;
 }
-template <class T>
-__device__ __forceinline__ void adam_store(T *p, int64_t i, int64_t n, bool whole, const AdamRun<T, 4> &r) {
-    if (whole) {
+template <bool WHOLE, class T>
+__device__ __forceinline__ void adam_store(T *p, int64_t i, int64_t n, const AdamRun<T, 4> &r) {
+    if constexpr (WHOLE) {
         *reinterpret_cast<AdamRun<T, 4> *>(p + i) = r;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (i + k < n) p[i + k] = r.v[k];
+        for (int k = 0; k < 4; ++k)
+            if (i + k < n) p[i + k] = r.v[k];
+    }
 }
 
-template <bool BITS8>
-__global__ void __launch_bounds__(32 * kAdamWarps) adam_step_kernel(const __grid_constant__ AdamArgs a) {
+__device__ __forceinline__ uint32_t adam_word(const AdamRun<uint8_t, 4> &r) { return *reinterpret_cast<const uint32_t *>(&r); }
+
+// The step of one block of a tensor, its block `b`, by a warp.  key: BITS8, the random bits' of its first value.
+template <bool BITS8, bool WHOLE>
+__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamTensor &t, int64_t b, uint32_t key, int lane) {
     using State = typename std::conditional<BITS8, uint8_t, float>::type;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t b = ((int64_t)blockIdx.x * a.steps) * kAdamWarps + warp;
-    if (b >= a.blocks) return;
-    int k = adam_find(a.tensors, a.count, b);
-    AdamTensor t = a.tensors[k];
-    int64_t end = k + 1 < a.count ? __ldg(&a.tensors[k + 1].block0) : a.blocks;
-    for (int s = 0; s < a.steps && b < a.blocks; ++s, b += kAdamWarps) {
-        if (b >= end) {  // the warp's next block is in a later tensor
-            k = adam_find(a.tensors, a.count, b);
-            t = a.tensors[k];
-            end = k + 1 < a.count ? __ldg(&a.tensors[k + 1].block0) : a.blocks;
-        }
-        const int64_t i0 = (b - t.block0) * kAdamBlock;
-        const bool whole = t.vec && i0 + kAdamBlock <= t.n;
-        AdamRun<float, 4> p[2], g[2];
-        AdamRun<State, 4> ms[2], vs[2];
-        const State *tm = static_cast<const State *>(t.m), *tv = static_cast<const State *>(t.v);
+    const int64_t i0 = b * kAdamBlock + 4 * lane;
+    AdamRun<float, 4> p[2], g[2];
+    AdamRun<State, 4> m[2], v[2];
+    AdamRun<__nv_bfloat16, 4> h[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int64_t i = i0 + 128 * j;
+        p[j] = adam_load<WHOLE>(t.p, i, t.n);
+        g[j] = adam_load<WHOLE>(t.g, i, t.n);
+        m[j] = adam_load<WHOLE>(static_cast<const State *>(t.m), i, t.n);
+        v[j] = adam_load<WHOLE>(static_cast<const State *>(t.v), i, t.n);
+    }
+    if constexpr (BITS8) {
+        const float sm = t.ms[b], sv = t.vs[b];
+        float2 mn[4], rn[4];
+        uint32_t top_m = 0u, top_r = 0u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int64_t i = i0 + 128 * j + 4 * lane;
-            p[j] = adam_load(t.p, i, t.n, whole);
-            g[j] = adam_load(t.g, i, t.n, whole);
-            ms[j] = adam_load(tm, i, t.n, whole);
-            vs[j] = adam_load(tv, i, t.n, whole);
+            const uint32_t cm = adam_word(m[j]), cv = adam_word(v[j]);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float2 m0 = __fmul2_rn(make_float2(adam_decode<3, true>(cm, e), adam_decode<3, true>(cm, e + 1)),
+                                             adam_two(sm));
+                const float2 r0 = __fmul2_rn(make_float2(adam_decode<4, false>(cv, e), adam_decode<4, false>(cv, e + 1)),
+                                             adam_two(sv));
+                const float2 gr = make_float2(g[j].v[e], g[j].v[e + 1]), v0 = __fmul2_rn(r0, r0), gg = __fmul2_rn(gr, gr);
+                const float2 x = make_float2(adam_blend(a.b1, m0.x, a.one_b1, gr.x),
+                                             adam_blend(a.b1, m0.y, a.one_b1, gr.y));
+                const float2 y = make_float2(__fsqrt_rn(adam_blend(a.b2, v0.x, a.one_b2, gg.x)),
+                                             __fsqrt_rn(adam_blend(a.b2, v0.y, a.one_b2, gg.y)));
+                // m / denom by an approximate reciprocal: what it is off by, 2^-22, is of the
+                // update and not of p, and a moment's own rounding is 2^-4
+                const float2 denom = __ffma2_rn(y, adam_two(a.inv_bc2), adam_two(a.eps));
+                const float2 pn = __ffma2_rn(__fmul2_rn(adam_two(a.step_size), x),
+                                             make_float2(__fdividef(-1.f, denom.x), __fdividef(-1.f, denom.y)),
+                                             __fmul2_rn(make_float2(p[j].v[e], p[j].v[e + 1]), adam_two(a.decay)));
+                p[j].v[e] = pn.x;
+                p[j].v[e + 1] = pn.y;
+                mn[2 * j + e / 2] = x;
+                rn[2 * j + e / 2] = y;
+                top_m = max(top_m, max(__float_as_uint(x.x) & 0x7fffffffu, __float_as_uint(x.y) & 0x7fffffffu));
+                top_r = max(top_r, max(__float_as_uint(y.x) & 0x7fffffffu, __float_as_uint(y.y) & 0x7fffffffu));
+            }
         }
-        float sm = 0.f, sv = 0.f;
-        if (BITS8) {
-            sm = t.ms[b - t.block0];
-            sv = t.vs[b - t.block0];
+        top_m = __reduce_max_sync(0xffffffffu, top_m);
+        top_r = __reduce_max_sync(0xffffffffu, top_r);
+        float inv_m, inv_r;
+        const float new_sm = adam_scale<3>(top_m, inv_m), new_sv = adam_scale<4>(top_r, inv_r);
+        // (the scale of a block that is 0 or NaN has no inverse: its codes are 0)
+        const bool has_m = inv_m > 0.f, has_r = inv_r > 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t wm = 0u, wv = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t bits = adam_mix(key + (uint32_t)(4 * lane + 128 * j + e));
+                const float x = e & 1 ? mn[2 * j + e / 2].y : mn[2 * j + e / 2].x;
+                const float y = e & 1 ? rn[2 * j + e / 2].y : rn[2 * j + e / 2].x;
+                const uint32_t cm = adam_encode<3>(__fmul_rn(fabsf(x), inv_m), bits << 4 & 0xffff0u);
+                const uint32_t cv = adam_encode<4>(__fmul_rn(y, inv_r), bits >> 13 & 0x7fff8u);
+                const uint32_t sign = __float_as_uint(x) >> 24 & 0x80u;
+                wm |= (cm > 0u ? cm | sign : 0u) << (8 * e);
+                wv |= cv << (8 * e);
+            }
+            *reinterpret_cast<uint32_t *>(&m[j]) = has_m ? wm : 0u;
+            *reinterpret_cast<uint32_t *>(&v[j]) = has_r ? wv : 0u;
         }
-        float m[8], root[8];
-        uint32_t top_m = 0u, top_r = 0u;
-        AdamRun<__nv_bfloat16, 4> h[2];
+        if (lane == 0) {
+            t.ms[b] = new_sm;
+            t.vs[b] = new_sv;
+        }
+    } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float m0, v0;
-                if constexpr (BITS8) {
-                    const uint32_t cm = ms[j].v[e];
-                    m0 = __fmul_rn(adam_decode<3>(cm & 127u), sm);
-                    if (cm & 128u) m0 = -m0;
-                    const float r = __fmul_rn(adam_decode<4>(vs[j].v[e]), sv);
-                    v0 = __fmul_rn(r, r);
-                } else {
-                    m0 = ms[j].v[e];
-                    v0 = vs[j].v[e];
-                }
                 const float gr = g[j].v[e];
-                const float mn = __fadd_rn(__fmul_rn(a.b1, m0), __fmul_rn(a.one_b1, gr));
-                const float vn = __fadd_rn(__fmul_rn(a.b2, v0), __fmul_rn(a.one_b2, __fmul_rn(gr, gr)));
-                const float rn = __fsqrt_rn(vn);
-                const float denom = __fadd_rn(__fdiv_rn(rn, a.bc2_sqrt), a.eps);
-                const float pn = __fsub_rn(__fmul_rn(p[j].v[e], a.decay), __fdiv_rn(__fmul_rn(a.step_size, mn), denom));
-                p[j].v[e] = pn;
-                h[j].v[e] = __float2bfloat16_rn(pn);
-                if constexpr (BITS8) {
-                    m[4 * j + e] = mn;
-                    root[4 * j + e] = rn;
-                    top_m = max(top_m, __float_as_uint(mn) & 0x7fffffffu);
-                    top_r = max(top_r, __float_as_uint(rn) & 0x7fffffffu);
-                } else {
-                    ms[j].v[e] = mn;
-                    vs[j].v[e] = vn;
-                }
+                const float mn = adam_blend(a.b1, m[j].v[e], a.one_b1, gr);
+                const float vn = adam_blend(a.b2, v[j].v[e], a.one_b2, __fmul_rn(gr, gr));
+                const float denom = __fadd_rn(__fdiv_rn(__fsqrt_rn(vn), a.bc2_sqrt), a.eps);
+                p[j].v[e] = __fsub_rn(__fmul_rn(p[j].v[e], a.decay), __fdiv_rn(__fmul_rn(a.step_size, mn), denom));
+                m[j].v[e] = mn;
+                v[j].v[e] = vn;
             }
-        if constexpr (BITS8) {
-            top_m = __reduce_max_sync(0xffffffffu, top_m);
-            top_r = __reduce_max_sync(0xffffffffu, top_r);
-            float inv_m, inv_r;
-            sm = adam_scale<3>(top_m, inv_m);
-            sv = adam_scale<4>(top_r, inv_r);
-            const uint32_t tensor = adam_mix(a.seed_lo ^ adam_mix(a.seed_hi ^ adam_mix(t.id + 1u)));
-            const uint32_t key = adam_mix(tensor + (uint32_t)(i0 >> 32));
+    }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+        const int64_t i = i0 + 128 * j;
+        adam_store<WHOLE>(t.p, i, t.n, p[j]);
+        adam_store<WHOLE>(static_cast<State *>(t.m), i, t.n, m[j]);
+        adam_store<WHOLE>(static_cast<State *>(t.v), i, t.n, v[j]);
+        if (t.p16) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t bits = adam_mix((uint32_t)i0 + (uint32_t)(128 * j + 4 * lane + e) + key);
-                    const float mn = m[4 * j + e];
-                    // a scale of 0 or NaN has inv 0 (and a NaN times it is not taken)
-                    const float x = inv_m > 0.f ? __fmul_rn(fabsf(mn), inv_m) : 0.f;
-                    const float y = inv_r > 0.f ? __fmul_rn(root[4 * j + e], inv_r) : 0.f;
-                    const uint32_t cm = adam_encode<3>(x, (bits & 0xffffu) << 4);
-                    ms[j].v[e] = (uint8_t)(cm | (mn < 0.f && cm > 0u ? 128u : 0u));
-                    vs[j].v[e] = (uint8_t)adam_encode<4>(y, (bits >> 16) << 3);
-                }
-            if (lane == 0) {
-                t.ms[b - t.block0] = sm;
-                t.vs[b - t.block0] = sv;
-            }
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<__nv_bfloat162 *>(&h[j].v[e]) = __floats2bfloat162_rn(p[j].v[e], p[j].v[e + 1]);
+            adam_store<WHOLE>(t.p16, i, t.n, h[j]);
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t i = i0 + 128 * j + 4 * lane;
-            adam_store(t.p, i, t.n, whole, p[j]);
-            adam_store(static_cast<State *>(t.m), i, t.n, whole, ms[j]);
-            adam_store(static_cast<State *>(t.v), i, t.n, whole, vs[j]);
-            if (t.p16) adam_store(t.p16, i, t.n, whole, h[j]);
+    }
+}
+
+// Warp w of W takes blocks [blocks w / W, blocks (w + 1) / W), tensor by tensor.
+template <bool BITS8>
+__global__ void __launch_bounds__(32 * kAdamWarps, BITS8 ? kAdamStep8 : kAdamStep32)
+    adam_step_kernel(const __grid_constant__ AdamArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * kAdamWarps + (threadIdx.x >> 5), W = (int64_t)gridDim.x * kAdamWarps;
+    const int64_t last = a.blocks * (w + 1) / W;
+    for (int64_t at = a.blocks * w / W; at < last;) {
+        const AdamTensor t = a.tensors[adam_find(a.first, a.count, at, lane)];
+        int64_t b = at - t.block0;
+        const int64_t whole = t.vec ? t.n / kAdamBlock : 0, end = min(last - t.block0, (t.n + kAdamBlock - 1) / kAdamBlock);
+        at = t.block0 + end;
+        // BITS8: the hash of the seed with the tensor's number, and that with the index' upper half
+        const uint32_t tensor = BITS8 ? adam_mix(a.seed_lo ^ adam_mix(a.seed_hi ^ adam_mix(t.id + 1u))) : 0u;
+        auto key = [&](int64_t k) {
+            return BITS8 ? adam_mix(tensor + (uint32_t)(k * kAdamBlock >> 32)) + (uint32_t)(k * kAdamBlock) : 0u;
+        };
+        // Each lane asks L2 for one 128-byte line of a later block: the loads of a block then wait for L2
+        // instead of HBM, without registers for what is under way.
+        constexpr int kState = BITS8 ? 2 : 8;  // lines of a block's m, and of its v
+        const char *line = lane < 8    ? reinterpret_cast<const char *>(t.p) + 128 * lane
+                           : lane < 16 ? reinterpret_cast<const char *>(t.g) + 128 * (lane - 8)
+                           : lane < 16 + kState ? static_cast<const char *>(t.m) + 128 * (lane - 16)
+                                                : static_cast<const char *>(t.v) + 128 * (lane - 16 - kState);
+        const int pitch = lane < 16 ? 1024 : 128 * kState;
+        for (; b < min(end, whole); ++b) {
+            if (lane < 16 + 2 * kState && b + kAdamAhead < min(end, whole))
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(line + (b + kAdamAhead) * pitch));
+            adam_block<BITS8, true>(a, t, b, key(b), lane);
         }
+        for (; b < end; ++b) adam_block<BITS8, false>(a, t, b, key(b), lane);
     }
 }
 
 // The values that the moments stand for, fp32, every tensor from its first block on.
 template <bool BITS8>
-__global__ void __launch_bounds__(32 * kAdamWarps) adam_read_kernel(const __grid_constant__ AdamArgs a) {
+__global__ void __launch_bounds__(32 * kAdamWarps, kAdamRead) adam_read_kernel(const __grid_constant__ AdamArgs a) {
     using State = typename std::conditional<BITS8, uint8_t, float>::type;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t b = ((int64_t)blockIdx.x * a.steps) * kAdamWarps + warp;
-    for (int s = 0; s < a.steps && b < a.blocks; ++s, b += kAdamWarps) {
-        const AdamTensor t = a.tensors[adam_find(a.tensors, a.count, b)];
-        const int64_t i0 = (b - t.block0) * kAdamBlock;
-        const bool whole = t.vec && i0 + kAdamBlock <= t.n;
-        const float sm = BITS8 ? t.ms[b - t.block0] : 0.f, sv = BITS8 ? t.vs[b - t.block0] : 0.f;
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * kAdamWarps + (threadIdx.x >> 5), W = (int64_t)gridDim.x * kAdamWarps;
+    const int64_t last = a.blocks * (w + 1) / W;
+    for (int64_t at = a.blocks * w / W; at < last;) {
+        const AdamTensor t = a.tensors[adam_find(a.first, a.count, at, lane)];
+        const int64_t whole = t.vec ? t.n / kAdamBlock : 0, end = min(last - t.block0, (t.n + kAdamBlock - 1) / kAdamBlock);
+        for (int64_t b = at - t.block0; b < end; ++b) {
+            const float sm = BITS8 ? t.ms[b] : 0.f, sv = BITS8 ? t.vs[b] : 0.f;
+            const int64_t i0 = b * kAdamBlock + 4 * lane;
+            AdamRun<State, 4> ms[2], vs[2];
+            const State *pm = static_cast<const State *>(t.m), *pv = static_cast<const State *>(t.v);
+            if (b < whole) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t i = i0 + 128 * j + 4 * lane;
-            const AdamRun<State, 4> ms = adam_load(static_cast<const State *>(t.m), i, t.n, whole);
-            const AdamRun<State, 4> vs = adam_load(static_cast<const State *>(t.v), i, t.n, whole);
-            AdamRun<float, 4> m, v;
+                for (int j = 0; j < 2; ++j) {
+                    ms[j] = adam_load<true>(pm, i0 + 128 * j, t.n);
+                    vs[j] = adam_load<true>(pv, i0 + 128 * j, t.n);
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (BITS8) {
-                    const uint32_t c = ms.v[e];
-                    const float x = __fmul_rn(adam_decode<3>(c & 127u), sm), r = __fmul_rn(adam_decode<4>(vs.v[e]), sv);
-                    m.v[e] = c & 128u ? -x : x;
-                    v.v[e] = __fmul_rn(r, r);
-                } else {
-                    m.v[e] = ms.v[e];
-                    v.v[e] = vs.v[e];
+                for (int j = 0; j < 2; ++j) {
+                    ms[j] = adam_load<false>(pm, i0 + 128 * j, t.n);
+                    vs[j] = adam_load<false>(pv, i0 + 128 * j, t.n);
                 }
             }
-            // rows of whole blocks: what lies past a tensor's end is 0
-            const int64_t o = b * kAdamBlock + 128 * j + 4 * lane;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (i + e >= t.n) m.v[e] = v.v[e] = 0.f;
-            if (a.m32) *reinterpret_cast<AdamRun<float, 4> *>(a.m32 + o) = m;
-            if (a.v32) *reinterpret_cast<AdamRun<float, 4> *>(a.v32 + o) = v;
+            for (int j = 0; j < 2; ++j) {
+                float m[4], v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (BITS8) {
+                        m[e] = __fmul_rn(adam_decode<3, true>(adam_word(ms[j]), e), sm);
+                        const float r = __fmul_rn(adam_decode<4, false>(adam_word(vs[j]), e), sv);
+                        v[e] = __fmul_rn(r, r);
+                    } else {
+                        m[e] = ms[j].v[e];
+                        v[e] = vs[j].v[e];
+                    }
+                    // rows of whole blocks: what lies past a tensor's end is 0
+                    if (i0 + 128 * j + e >= t.n) m[e] = v[e] = 0.f;
+                }
+                const int64_t o = t.block0 * kAdamBlock + i0 + 128 * j;
+                if (a.m32) __stcs(reinterpret_cast<float4 *>(a.m32 + o), make_float4(m[0], m[1], m[2], m[3]));
+                if (a.v32) __stcs(reinterpret_cast<float4 *>(a.v32 + o), make_float4(v[0], v[1], v[2], v[3]));
+            }
         }
+        at = t.block0 + end;
     }
 }
 
@@ -282,21 +351,19 @@ __global__ void __launch_bounds__(32 * kAdamWarps) adam_read_kernel(const __grid
 struct attt_adamw {
     int dev, count, bits;
     int64_t blocks;
-    attt::AdamTensor *tensors;  // on the device
+    attt::AdamTensor *tensors;  // on the device, behind them the first block of each
 };
 
 namespace attt {
 
-// Blocks of kAdamWarps warps for the handle's blocks: up to 8 steps a warp, fewer where that
-// would leave SMs without four blocks.
-static unsigned adam_grid(const attt_adamw *h, AdamArgs &a) {
-    const int64_t sets = cdiv(h->blocks, kAdamWarps), want = 4ll * num_sms(h->dev);
-    int64_t steps = sets / want;
-    a.steps = (int)(steps < 1 ? 1 : steps > 8 ? 8 : steps);
+// Fills in the handle's part of a and returns the blocks of kAdamWarps warps: as many as the
+// device holds at once, or a block of values per warp.
+static unsigned adam_grid(const attt_adamw *h, AdamArgs &a, int per_sm) {
     a.tensors = h->tensors;
+    a.first = reinterpret_cast<const int64_t *>(h->tensors + h->count);
     a.count = h->count;
     a.blocks = h->blocks;
-    return (unsigned)cdiv(sets, a.steps);
+    return (unsigned)std::min<int64_t>(cdiv(h->blocks, kAdamWarps), (int64_t)per_sm * num_sms(h->dev));
 }
 
 static attt_status adam_device(const attt_adamw *h) {
@@ -374,22 +441,24 @@ attt_status attt_adamw_create(int count, float *const *d_p, const float *const *
         int dev;
         const attt_status st = current_device(&dev);
         if (st != ATTT_OK) return st;
-        attt_adamw *h = new attt_adamw{dev, (int)list.size(), state_bits, blocks, nullptr};
+        std::unique_ptr<attt_adamw> h(new attt_adamw{dev, (int)list.size(), state_bits, blocks, nullptr});
         if (!list.empty()) {
-            const size_t bytes = list.size() * sizeof(AdamTensor);
+            const size_t table = list.size() * sizeof(AdamTensor), bytes = table + list.size() * sizeof(int64_t);
+            std::vector<char> image(bytes);
+            std::memcpy(image.data(), list.data(), table);
+            for (size_t k = 0; k < list.size(); ++k)
+                std::memcpy(image.data() + table + k * sizeof(int64_t), &list[k].block0, sizeof(int64_t));
             if (fault_take(FAULT_ALLOC) || cudaMalloc(&h->tensors, bytes) != cudaSuccess) {
                 (void)cudaGetLastError();
-                delete h;
                 return ATTT_ERR_CUDA;
             }
-            if (cudaMemcpy(h->tensors, list.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) {
+            if (cudaMemcpy(h->tensors, image.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) {
                 (void)cudaGetLastError();
                 cudaFree(h->tensors);
-                delete h;
                 return ATTT_ERR_CUDA;
             }
         }
-        *out = h;
+        *out = h.release();
         return ATTT_OK;
     } catch (const std::bad_alloc &) {
         return ATTT_ERR_CUDA;
@@ -420,7 +489,7 @@ attt_status attt_adamw_step(attt_adamw *h, double lr, double beta1, double beta2
     if (st != ATTT_OK) return st;
     if (h->blocks == 0) return ATTT_OK;
     AdamArgs a{};
-    const unsigned grid = adam_grid(h, a);
+    const unsigned grid = adam_grid(h, a, h->bits == 8 ? kAdamStep8 : kAdamStep32);
     // the step's scalars in double, rounded once to fp32
     a.decay = (float)(1.0 - lr * weight_decay);
     a.b1 = (float)beta1;
@@ -429,6 +498,7 @@ attt_status attt_adamw_step(attt_adamw *h, double lr, double beta1, double beta2
     a.one_b2 = (float)(1.0 - beta2);
     a.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
     a.bc2_sqrt = (float)std::sqrt(1.0 - std::pow(beta2, (double)step));
+    a.inv_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
     a.eps = (float)eps;
     a.seed_lo = (uint32_t)seed;
     a.seed_hi = (uint32_t)(seed >> 32);
@@ -446,7 +516,7 @@ attt_status attt_adamw_read_state(const attt_adamw *h, float *d_m32, float *d_v3
     if (st != ATTT_OK) return st;
     if (h->blocks == 0) return ATTT_OK;
     AdamArgs a{};
-    const unsigned grid = adam_grid(h, a);
+    const unsigned grid = adam_grid(h, a, kAdamRead);
     a.m32 = d_m32;
     a.v32 = d_v32;
     if (h->bits == 8) adam_read_kernel<true><<<grid, 32 * kAdamWarps, 0, stream>>>(a);

@@ -9,8 +9,9 @@
 // Bound: HBM bytes; below some hundred tokens a launch's latency.  A group of 2 to 32 lanes
 // takes a head, a lane two 16-byte vectors of it: for the halves layout the two that
 // turn together, so that the rotation needs no exchange and the norm one reduction over
-// a few lanes.  The next head's vectors are loaded while one is worked on.  A block takes
-// some tokens with all their heads, so that cosines are formed once per token.
+// a few lanes.  The vectors of the next heads stay in registers as loaded while some are
+// worked on.  A block takes a run of tokens with all their heads and forms their cosines
+// once, into a table whose order is that of the lanes' reads.
 // Angles: w_i is held in turns per position as a 64-bit fraction; pos w_i modulo 2^64
 // is then the exact fraction of a turn whatever the position (fp32 products are off by
 // 0.06 radians at position 10^6), and a quarter turn is taken off before it goes to fp32.
@@ -26,6 +27,9 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeParts = 2;
 constexpr int kRopeMaxD = 512;
 constexpr int kRopeTable = 2048;  // cosines and sines that a block holds
+// Blocks per SM: what the registers of a thread's vectors leave room for.
+constexpr int kRopeForward = 3, kRopeBack = 2;
+constexpr int kRopeMaxBlocks = 160 * kRopeBack;  // of a part in the backward kernel, at most
 
 struct RopeTensor {
     const void *x, *dy;
@@ -33,6 +37,7 @@ struct RopeTensor {
     const float *gamma;
     int64_t x_ld, x_hs, dy_ld, dy_hs, y_ld, y_hs;
     int heads;
+    uint32_t magic;  // of the division by heads (0: one head)
 };
 
 struct RopeArgs {
@@ -40,43 +45,33 @@ struct RopeArgs {
     const int32_t *pos;
     const uint64_t *freq;
     int64_t T;
-    int nparts, D, half, tokens;  // half: rot / 2; tokens: of a block at a time
-    int block0[kRopeParts + 1];   // backward: first block of each part
+    int nparts, D, half;         // half: rot / 2
+    int tokens;                  // that a table holds, at most
+    int block0[kRopeParts + 1];  // backward: first block of each part
     float eps, mscale;
     float *dgamma;                // backward: [blocks, D] partial sums, nullptr: not wanted
 };
 
+// What a lane reads at once: a 16-byte vector or one value.
+template <class T, int V>
+struct RopeRead {
+    using type = uint4;
+};
+template <class T>
+struct RopeRead<T, 1> {
+    using type = T;
+};
 template <class T>
 struct RopeVec {  // values of a 16-byte vector
     static constexpr int n = 16 / sizeof(T);
 };
 
-__device__ __forceinline__ void rope_get(const float *p, float (&v)[4]) {
-    const float4 f = *reinterpret_cast<const float4 *>(p);
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+__device__ __forceinline__ float rope_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float rope_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t rope_pack(float lo, float hi) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b);
 }
-__device__ __forceinline__ void rope_get(const __nv_bfloat16 *p, float (&v)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void rope_get(const float *p, float (&v)[1]) { v[0] = *p; }
-__device__ __forceinline__ void rope_get(const __nv_bfloat16 *p, float (&v)[1]) { v[0] = __bfloat162float(*p); }
-__device__ __forceinline__ void rope_put(float *p, const float (&v)[4]) {
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-__device__ __forceinline__ void rope_put(__nv_bfloat16 *p, const float (&v)[8]) {
-    __nv_bfloat162 b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<uint4 *>(b);
-}
-__device__ __forceinline__ void rope_put(float *p, const float (&v)[1]) { *p = v[0]; }
-__device__ __forceinline__ void rope_put(__nv_bfloat16 *p, const float (&v)[1]) { *p = __float2bfloat16_rn(v[0]); }
 
 // (cos, sin) of pos w, times mscale.  The nearest quarter turn comes off in integers, so
 // that what is left keeps its relative precision.
@@ -92,70 +87,167 @@ __device__ __forceinline__ float2 rope_turn(int32_t pos, uint64_t w, float mscal
 }
 
 // What a lane holds of a head: NS slots of V pairs.  Pair p < half turns: values p and p + half
-// (halves) or 2 p and 2 p + 1 (neighbours); the others are 2 p and 2 p + 1 and do not.
-// V > 1: the pairs of a slot are two vectors, at first() and second().
-template <class T, int V, bool INTER>
+// (halves) or 2 p and 2 p + 1 (neighbours, INTER); the others do not.  V > 1: a slot is two vectors, at
+// first() and second().
+template <int V, bool INTER>
 struct RopeSlot {
     int pair;  // its first pair; at least D / 2: nothing
     __device__ __forceinline__ bool turns(int half) const { return pair < half; }
     __device__ __forceinline__ bool apart(int half) const { return !INTER && pair < half; }
     __device__ __forceinline__ int first(int half) const { return apart(half) ? pair : 2 * pair; }
     __device__ __forceinline__ int second(int half) const { return apart(half) ? pair + half : 2 * pair + V; }
-    // the vectors' values as the two members of each pair, and back
-    __device__ __forceinline__ void split(int half, float (&a)[V], float (&b)[V]) const {
-        if constexpr (V > 1) {
-            if (apart(half)) return;
-            float v[2 * V];
+};
+
+// The values of a slot's two vectors, in fp32, two to a register pair: a holds the first members
+// of its pairs and b the second ones.  (Values that do not turn have no partner: without INTER
+// they are a's and b's as they lie.)
+template <class T, int V, bool INTER>
+struct RopeValues {
+    static constexpr int P = V > 1 ? V / 2 : 1;
+    using R = typename RopeRead<T, V>::type;
+    float2 a[P], b[P];
+
+    __device__ __forceinline__ void unpack(const R &x, const R &y) {
+        if constexpr (V == 1) {
+            a[0] = make_float2((float)x, 0.f);
+            b[0] = make_float2((float)y, 0.f);
+        } else if constexpr (V == 8) {
+            const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int i = 0; i < V; ++i) { v[i] = a[i]; v[V + i] = b[i]; }
-#pragma unroll
-            for (int i = 0; i < V; ++i) { a[i] = v[2 * i]; b[i] = v[2 * i + 1]; }
+            for (int i = 0; i < 4; ++i) {
+                if (INTER) {
+                    const uint32_t w0 = i < 2 ? u[2 * i] : v[2 * i - 4], w1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
+                    a[i] = make_float2(rope_lo(w0), rope_lo(w1));
+                    b[i] = make_float2(rope_hi(w0), rope_hi(w1));
+                } else {
+                    a[i] = make_float2(rope_lo(u[i]), rope_hi(u[i]));
+                    b[i] = make_float2(rope_lo(v[i]), rope_hi(v[i]));
+                }
+            }
+        } else {
+            const float u[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+            const float v[4] = {__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)};
+            a[0] = INTER ? make_float2(u[0], u[2]) : make_float2(u[0], u[1]);
+            b[0] = INTER ? make_float2(u[1], u[3]) : make_float2(v[0], v[1]);
+            a[1] = INTER ? make_float2(v[0], v[2]) : make_float2(u[2], u[3]);
+            b[1] = INTER ? make_float2(v[1], v[3]) : make_float2(v[2], v[3]);
         }
     }
-    __device__ __forceinline__ void join(int half, float (&a)[V], float (&b)[V]) const {
-        if constexpr (V > 1) {
-            if (apart(half)) return;
-            float v[2 * V];
+    __device__ __forceinline__ void pack(R &x, R &y) const {
+        if constexpr (V == 1) {
+            x = (T)a[0].x;
+            y = (T)b[0].x;
+        } else if constexpr (V == 8) {
+            uint32_t u[8];
 #pragma unroll
-            for (int i = 0; i < V; ++i) { v[2 * i] = a[i]; v[2 * i + 1] = b[i]; }
+            for (int i = 0; i < 4; ++i) {
+                if (INTER) {
+                    u[2 * i] = rope_pack(a[i].x, b[i].x);
+                    u[2 * i + 1] = rope_pack(a[i].y, b[i].y);
+                } else {
+                    u[i] = rope_pack(a[i].x, a[i].y);
+                    u[4 + i] = rope_pack(b[i].x, b[i].y);
+                }
+            }
+            x = make_uint4(u[0], u[1], u[2], u[3]);
+            y = make_uint4(u[4], u[5], u[6], u[7]);
+        } else {
+            float u[4], v[4];
+            values(u, v);
+            x = make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3]));
+            y = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        }
+    }
+    // the two vectors' values in their order, and back
+    __device__ __forceinline__ void values(float (&u)[V], float (&v)[V]) const {
+        if constexpr (V == 1) {
+            u[0] = a[0].x;
+            v[0] = b[0].x;
+        } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) { a[i] = v[i]; b[i] = v[V + i]; }
+            for (int i = 0; i < V / 2; ++i) {
+                if (INTER) {
+                    float *w = i < V / 4 ? &u[4 * i] : &v[4 * i - V];
+                    w[0] = a[i].x; w[1] = b[i].x; w[2] = a[i].y; w[3] = b[i].y;
+                } else {
+                    u[2 * i] = a[i].x; u[2 * i + 1] = a[i].y;
+                    v[2 * i] = b[i].x; v[2 * i + 1] = b[i].y;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void from(const float (&u)[V], const float (&v)[V]) {
+        if constexpr (V == 1) {
+            a[0] = make_float2(u[0], 0.f);
+            b[0] = make_float2(v[0], 0.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                if (INTER) {
+                    const float *w = i < V / 4 ? &u[4 * i] : &v[4 * i - V];
+                    a[i] = make_float2(w[0], w[2]);
+                    b[i] = make_float2(w[1], w[3]);
+                } else {
+                    a[i] = make_float2(u[2 * i], u[2 * i + 1]);
+                    b[i] = make_float2(v[2 * i], v[2 * i + 1]);
+                }
+            }
         }
     }
 };
 
-template <int V, int NS>
+__device__ __forceinline__ float2 rope_mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 rope_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 rope_neg(float2 a) { return make_float2(-a.x, -a.y); }
+
+// A lane's vectors of a head, as loaded.
+template <class T, int V, int NS>
 struct RopeHead {
-    float a[NS][V], b[NS][V];
+    typename RopeRead<T, V>::type a[NS], b[NS];
 };
 
 template <class T, int V, int NS, bool INTER>
-__device__ __forceinline__ void rope_load(const void *base, int64_t off, const RopeSlot<T, V, INTER> (&slot)[NS], int half,
-                                          int pairs, RopeHead<V, NS> &h) {
+__device__ __forceinline__ void rope_load(const void *base, int64_t off, const RopeSlot<V, INTER> (&slot)[NS], int half,
+                                          int pairs, RopeHead<T, V, NS> &h) {
+    using R = typename RopeRead<T, V>::type;
     const T *p = static_cast<const T *>(base) + off;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
+        h.a[s] = h.b[s] = R{};
         if (slot[s].pair < pairs) {
-            rope_get(p + slot[s].first(half), h.a[s]);
-            rope_get(p + slot[s].second(half), h.b[s]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) h.a[s][i] = h.b[s][i] = 0.f;
+            h.a[s] = *reinterpret_cast<const R *>(p + slot[s].first(half));
+            h.b[s] = *reinterpret_cast<const R *>(p + slot[s].second(half));
         }
+    }
+}
+
+// A token's table: cosine and sine of every pair, V > 1: of two neighbouring pairs as (cos, cos, sin, sin), those
+// that the lanes read at once side by side.
+template <int V>
+__device__ __forceinline__ void rope_note(float *row, int i, int half, float2 e) {
+    if (V == 1) {
+        reinterpret_cast<float2 *>(row)[i] = e;
+    } else {
+        float *at = row + ((i % V) / 2 * (half / V) + i / V) * 4 + (i & 1);
+        at[0] = e.x;
+        at[2] = e.y;
     }
 }
 
 // BACK: dx (and dgamma) from dy, else y from x.  V values per vector (1: any sizes and
 // alignment), NS slots per lane, G lanes per head.
 template <class T, int V, int NS, int G, bool INTER, bool BACK>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs p) {
-    __shared__ float2 table[kRopeTable];
+__global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK ? kRopeBack : kRopeForward)
+    rope_kernel(const __grid_constant__ RopeArgs p) {
+    __shared__ alignas(16) float table[2 * kRopeTable];
     __shared__ float red[BACK ? kRopeThreads / 32 * kRopeMaxD : 1];
     if (BACK) griddep_launch_dependents();
     constexpr int kGroups = kRopeThreads / G;
+    // heads of a lane at a time: two where its registers hold them
+    constexpr int U = (NS > 1 && (V > 1 || NS >= 4)) || (BACK && INTER && V == 8) ? 1 : 2;
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
     const int half = p.half, pairs = p.D / 2;
-    RopeSlot<T, V, INTER> slot[NS];
+    RopeSlot<V, INTER> slot[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) slot[s].pair = (lane + s * G) * V;
 
@@ -163,133 +255,179 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     const int part1 = BACK ? part0 + 1 : p.nparts;
     const int block = BACK ? (int)blockIdx.x - p.block0[part0] : (int)blockIdx.x;
     const int blocks = BACK ? p.block0[part0 + 1] - p.block0[part0] : (int)gridDim.x;
+    const int64_t begin = p.T * block / blocks, end = p.T * (block + 1) / blocks;  // this block's tokens
     const float inv_d = 1.f / (float)p.D;
-    float sum_a[NS][V], sum_b[NS][V];  // BACK: this lane's share of dgamma
+    using Values = RopeValues<T, V, INTER>;
+    constexpr int P = Values::P;
+    Values sum[NS];  // BACK: this lane's share of dgamma
     if constexpr (BACK) {
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum_a[s][i] = sum_b[s][i] = 0.f;
+            for (int i = 0; i < P; ++i) sum[s].a[i] = sum[s].b[i] = make_float2(0.f, 0.f);
     }
 
-    for (int64_t t0 = (int64_t)block * p.tokens; t0 < p.T; t0 += (int64_t)blocks * p.tokens) {
-        const int nt = (int)min((int64_t)p.tokens, p.T - t0);
-        __syncthreads();  // the table is no longer read
-        for (int i = threadIdx.x; i < nt * half; i += kRopeThreads) {
-            const int t = i / half;
-            table[i] = rope_turn(__ldg(p.pos + t0 + t), __ldg(p.freq + (i - t * half)), p.mscale);
-        }
-        __syncthreads();
+    for (int64_t t0 = begin; t0 < end; t0 += p.tokens) {
+        const int nt = (int)min((int64_t)p.tokens, end - t0);
+        bool filled = false;
         for (int part = part0; part < part1; ++part) {
             const RopeTensor &q = p.part[part];
             const bool norm = q.gamma != nullptr;
-            float ga[NS][V], gb[NS][V];
+            const int n = nt * q.heads;
+            RopeHead<T, V, NS> next[U], next_x[BACK ? U : 1];
+            auto fetch = [&](int i0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = i0 + u * kGroups;
+                    if (i < n) {
+                        const int t = q.magic ? __umulhi((uint32_t)i, q.magic) : i, h = i - t * q.heads;
+                        rope_load<T, V, NS, INTER>(BACK ? q.dy : q.x,
+                                                   BACK ? (t0 + t) * q.dy_ld + h * q.dy_hs : (t0 + t) * q.x_ld + h * q.x_hs,
+                                                   slot, half, pairs, next[u]);
+                        if (BACK && norm)
+                            rope_load<T, V, NS, INTER>(q.x, (t0 + t) * q.x_ld + h * q.x_hs, slot, half, pairs,
+                                                       next_x[BACK ? u : 0]);
+                    }
+                }
+            };
+            fetch(group);
+            if (!filled) {  // with the first loads under way
+                __syncthreads();  // the table is no longer read
+                for (int i = threadIdx.x; i < nt * half; i += kRopeThreads) {
+                    const int t = i / half, k = i - t * half;
+                    float2 e = rope_turn(__ldg(p.pos + t0 + t), __ldg(p.freq + k), p.mscale);
+                    if (BACK) e.y = -e.y;
+                    rope_note<V>(table + 2 * t * half, k, half, e);
+                }
+                __syncthreads();
+                filled = true;
+            }
+            Values gamma[NS];
             if (norm) {
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
+                    float u[V], v[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        ga[s][i] = slot[s].pair < pairs ? __ldg(q.gamma + slot[s].first(half) + i) : 0.f;
-                        gb[s][i] = slot[s].pair < pairs ? __ldg(q.gamma + slot[s].second(half) + i) : 0.f;
+                        u[i] = slot[s].pair < pairs ? __ldg(q.gamma + slot[s].first(half) + i) : 0.f;
+                        v[i] = slot[s].pair < pairs ? __ldg(q.gamma + slot[s].second(half) + i) : 0.f;
                     }
-                    slot[s].split(half, ga[s], gb[s]);
+                    gamma[s].from(u, v);
                 }
             }
-            const int n = nt * q.heads;
-            RopeHead<V, NS> next, next_x;
-            auto fetch = [&](int i) {
-                const int t = i / q.heads, h = i - t * q.heads;
-                if (BACK) rope_load<T, V, NS, INTER>(q.dy, (t0 + t) * q.dy_ld + h * q.dy_hs, slot, half, pairs, next);
-                if (!BACK || norm)
-                    rope_load<T, V, NS, INTER>(q.x, (t0 + t) * q.x_ld + h * q.x_hs, slot, half, pairs,
-                                               BACK ? next_x : next);
-            };
-            if (group < n) fetch(group);
             // whole warps go round together (the reductions are theirs)
-            for (int i0 = 0; i0 < n; i0 += kGroups) {
-                const int i = i0 + group;
-                const bool live = i < n;
-                RopeHead<V, NS> z = next, x = next_x;
-                if (i + kGroups < n) fetch(i + kGroups);
-                const int t = i / q.heads, h = i - t * q.heads;
-                const float2 *cs = table + t * half;
+            for (int i0 = 0; i0 < n; i0 += U * kGroups) {
+                RopeHead<T, V, NS> head[U], head_x[BACK ? U : 1];
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    slot[s].split(half, z.a[s], z.b[s]);
-                    if (BACK && norm) slot[s].split(half, x.a[s], x.b[s]);
+                for (int u = 0; u < U; ++u) {
+                    head[u] = next[u];
+                    if (BACK) head_x[BACK ? u : 0] = next_x[BACK ? u : 0];
                 }
-                if constexpr (!BACK) {
-                    if (norm) {
-                        float ss = 0.f;
+                fetch(i0 + group + U * kGroups);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = i0 + group + u * kGroups;
+                    const bool live = i < n;
+                    const int t = q.magic ? __umulhi((uint32_t)i, q.magic) : i, h = i - t * q.heads;
+                    Values z[NS];
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) z[s].unpack(head[u].a[s], head[u].b[s]);
+                    float2 rstd = make_float2(1.f, 1.f);
+                    if (!BACK && norm) {
+                        float2 ss = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int s = 0; s < NS; ++s)
 #pragma unroll
-                            for (int k = 0; k < V; ++k)
-                                ss = fmaf(z.a[s][k], z.a[s][k], fmaf(z.b[s][k], z.b[s][k], ss));
-#pragma unroll
-                        for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                        const float rstd = __frsqrt_rn(fmaf(ss, inv_d, p.eps));
-#pragma unroll
-                        for (int s = 0; s < NS; ++s)
-#pragma unroll
-                            for (int k = 0; k < V; ++k) {
-                                z.a[s][k] *= rstd * ga[s][k];
-                                z.b[s][k] *= rstd * gb[s][k];
+                            for (int k = 0; k < P; ++k) {
+                                ss = rope_fma(z[s].a[k], z[s].a[k], rope_fma(z[s].b[k], z[s].b[k], ss));
+                                z[s].a[k] = rope_mul(z[s].a[k], gamma[s].a[k]);
+                                z[s].b[k] = rope_mul(z[s].b[k], gamma[s].b[k]);
                             }
+                        float sum2 = ss.x + ss.y;
+#pragma unroll
+                        for (int o = G / 2; o > 0; o >>= 1) sum2 += __shfl_xor_sync(0xffffffffu, sum2, o);
+                        rstd.x = rstd.y = __frsqrt_rn(fmaf(sum2, inv_d, p.eps));
                     }
-                }
-                if (live) {
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-                        if (slot[s].turns(half)) {
-#pragma unroll
-                            for (int k = 0; k < V; ++k) {
-                                const float2 e = cs[slot[s].pair + k];
-                                const float a = z.a[s][k], b = z.b[s][k], sn = BACK ? -e.y : e.y;
-                                z.a[s][k] = fmaf(a, e.x, -(b * sn));
-                                z.b[s][k] = fmaf(a, sn, b * e.x);
-                            }
-                        }
-                }
-                if constexpr (BACK) {
-                    if (norm) {
-                        float ss = 0.f, sg = 0.f;  // sums of x^2 and of g x
+                    if (live) {
 #pragma unroll
                         for (int s = 0; s < NS; ++s)
+                            if (slot[s].turns(half)) {
+                                const float *cs = table + 2 * t * half + (V == 1 ? 2 : 4) * (slot[s].pair / V);
 #pragma unroll
-                            for (int k = 0; k < V; ++k) {
-                                ss = fmaf(x.a[s][k], x.a[s][k], fmaf(x.b[s][k], x.b[s][k], ss));
-                                sg = fmaf(z.a[s][k] * ga[s][k], x.a[s][k], fmaf(z.b[s][k] * gb[s][k], x.b[s][k], sg));
-                            }
-#pragma unroll
-                        for (int o = G / 2; o > 0; o >>= 1) {
-                            ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                            sg += __shfl_xor_sync(0xffffffffu, sg, o);
-                        }
-                        const float rstd = __frsqrt_rn(fmaf(ss, inv_d, p.eps)), m = sg * inv_d * rstd;
-#pragma unroll
-                        for (int s = 0; s < NS; ++s)
-#pragma unroll
-                            for (int k = 0; k < V; ++k) {
-                                const float xa = x.a[s][k] * rstd, xb = x.b[s][k] * rstd;
-                                if (live) {
-                                    sum_a[s][k] = fmaf(z.a[s][k], xa, sum_a[s][k]);
-                                    sum_b[s][k] = fmaf(z.b[s][k], xb, sum_b[s][k]);
+                                for (int k = 0; k < P; ++k) {
+                                    float2 c, sn;
+                                    if constexpr (V == 1) {
+                                        const float2 f = *reinterpret_cast<const float2 *>(cs);
+                                        c = make_float2(f.x, 0.f);
+                                        sn = make_float2(f.y, 0.f);
+                                    } else {
+                                        const float4 f = *reinterpret_cast<const float4 *>(cs + 4 * k * (half / V));
+                                        c = make_float2(f.x, f.y);
+                                        sn = make_float2(f.z, f.w);
+                                    }
+                                    const float2 va = z[s].a[k], vb = z[s].b[k];
+                                    z[s].a[k] = rope_fma(va, c, rope_neg(rope_mul(vb, sn)));
+                                    z[s].b[k] = rope_fma(va, sn, rope_mul(vb, c));
                                 }
-                                z.a[s][k] = rstd * fmaf(-xa, m, z.a[s][k] * ga[s][k]);
-                                z.b[s][k] = rstd * fmaf(-xb, m, z.b[s][k] * gb[s][k]);
                             }
                     }
-                }
-                if (live) {
-                    T *y = static_cast<T *>(q.y) + (t0 + t) * q.y_ld + h * q.y_hs;
+                    if (!BACK && norm) {
 #pragma unroll
-                    for (int s = 0; s < NS; ++s)
-                        if (slot[s].pair < pairs) {
-                            slot[s].join(half, z.a[s], z.b[s]);
-                            rope_put(y + slot[s].first(half), z.a[s]);
-                            rope_put(y + slot[s].second(half), z.b[s]);
+                        for (int s = 0; s < NS; ++s)
+#pragma unroll
+                            for (int k = 0; k < P; ++k) {
+                                z[s].a[k] = rope_mul(z[s].a[k], rstd);
+                                z[s].b[k] = rope_mul(z[s].b[k], rstd);
+                            }
+                    }
+                    if constexpr (BACK) {
+                        if (norm) {
+                            Values x[NS];
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) x[s].unpack(head_x[u].a[s], head_x[u].b[s]);
+                            float2 ss = make_float2(0.f, 0.f), sg = ss;  // sums of x^2 and of g x
+#pragma unroll
+                            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                                for (int k = 0; k < P; ++k) {
+                                    ss = rope_fma(x[s].a[k], x[s].a[k], rope_fma(x[s].b[k], x[s].b[k], ss));
+                                    sg = rope_fma(rope_mul(z[s].a[k], gamma[s].a[k]), x[s].a[k], sg);
+                                    sg = rope_fma(rope_mul(z[s].b[k], gamma[s].b[k]), x[s].b[k], sg);
+                                }
+                            float sum2 = ss.x + ss.y, sumg = sg.x + sg.y;
+#pragma unroll
+                            for (int o = G / 2; o > 0; o >>= 1) {
+                                sum2 += __shfl_xor_sync(0xffffffffu, sum2, o);
+                                sumg += __shfl_xor_sync(0xffffffffu, sumg, o);
+                            }
+                            rstd.x = rstd.y = __frsqrt_rn(fmaf(sum2, inv_d, p.eps));
+                            const float2 m = make_float2(-sumg * inv_d * rstd.x, -sumg * inv_d * rstd.x);
+#pragma unroll
+                            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                                for (int k = 0; k < P; ++k) {
+                                    const float2 ha = rope_mul(x[s].a[k], rstd), hb = rope_mul(x[s].b[k], rstd);
+                                    if (live) {
+                                        sum[s].a[k] = rope_fma(z[s].a[k], ha, sum[s].a[k]);
+                                        sum[s].b[k] = rope_fma(z[s].b[k], hb, sum[s].b[k]);
+                                    }
+                                    z[s].a[k] = rope_mul(rstd, rope_fma(ha, m, rope_mul(z[s].a[k], gamma[s].a[k])));
+                                    z[s].b[k] = rope_mul(rstd, rope_fma(hb, m, rope_mul(z[s].b[k], gamma[s].b[k])));
+                                }
                         }
+                    }
+                    if (live) {
+                        using R = typename RopeRead<T, V>::type;
+                        T *y = static_cast<T *>(q.y) + (t0 + t) * q.y_ld + h * q.y_hs;
+#pragma unroll
+                        for (int s = 0; s < NS; ++s)
+                            if (slot[s].pair < pairs) {
+                                R u0, u1;
+                                z[s].pack(u0, u1);
+                                *reinterpret_cast<R *>(y + slot[s].first(half)) = u0;
+                                *reinterpret_cast<R *>(y + slot[s].second(half)) = u1;
+                            }
+                    }
                 }
             }
         }
@@ -298,27 +436,23 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     if constexpr (BACK) {
         if (!p.dgamma || !p.part[part0].gamma) return;
         // a warp's groups by exchanges, then the warps in order
+        float *mine = red + threadIdx.x / 32 * p.D;
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s) {
+            float u[V], v[V];
+            sum[s].values(u, v);
 #pragma unroll
-            for (int k = 0; k < V; ++k)
+            for (int k = 0; k < V; ++k) {
 #pragma unroll
                 for (int o = 16; o >= G; o >>= 1) {
-                    sum_a[s][k] += __shfl_xor_sync(0xffffffffu, sum_a[s][k], o);
-                    sum_b[s][k] += __shfl_xor_sync(0xffffffffu, sum_b[s][k], o);
+                    u[k] += __shfl_xor_sync(0xffffffffu, u[k], o);
+                    v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
                 }
-        float *mine = red + threadIdx.x / 32 * p.D;
-        if (threadIdx.x % 32 < G) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-                if (slot[s].pair < pairs) {
-                    slot[s].join(half, sum_a[s], sum_b[s]);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        mine[slot[s].first(half) + k] = sum_a[s][k];
-                        mine[slot[s].second(half) + k] = sum_b[s][k];
-                    }
+                if (threadIdx.x % 32 < G && slot[s].pair < pairs) {
+                    mine[slot[s].first(half) + k] = u[k];
+                    mine[slot[s].second(half) + k] = v[k];
                 }
+            }
         }
         __syncthreads();
         for (int c = threadIdx.x; c < p.D; c += kRopeThreads) {
@@ -329,7 +463,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
 }
 
-// dgamma of each part from its blocks' sums, in their order: 8 strands of blocks per column.
+// dgamma of each part from its blocks' sums: 32 strands of blocks per column, each in the
+// blocks' order, then the strands in theirs.
 struct RopeSum {
     const float *part;
     float *out[kRopeParts];
@@ -337,25 +472,31 @@ struct RopeSum {
     int D;
 };
 
-__global__ void __launch_bounds__(256) rope_sum_kernel(const RopeSum a) {
-    __shared__ float red[8][32];
+__global__ void __launch_bounds__(1024) rope_sum_kernel(const RopeSum a) {
+    __shared__ float red[32][33];
     griddep_wait();
-    const int q = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x % 32, strand = threadIdx.x / 32;
+    const int q = blockIdx.y, x = threadIdx.x % 32, c = blockIdx.x * 32 + x, strand = threadIdx.x / 32;
+    if (!a.out[q]) return;
     float v = 0.f;
-    if (a.out[q] && c < a.D)
-#pragma unroll 8
-        for (int b = a.block0[q] + strand; b < a.block0[q + 1]; b += 8) v += __ldcg(a.part + (int64_t)b * a.D + c);
-    red[strand][threadIdx.x % 32] = v;
-    __syncthreads();
-    if (strand == 0 && a.out[q] && c < a.D) {
-        for (int s = 1; s < 8; ++s) v += red[s][threadIdx.x];
-        a.out[q][c] = v;
+    if (c < a.D) {
+        const int b0 = a.block0[q] + strand, b1 = a.block0[q + 1];
+        float w[kRopeMaxBlocks / 32];  // all loads at once: their latency is what this kernel costs
+#pragma unroll
+        for (int k = 0; k < kRopeMaxBlocks / 32; ++k)
+            w[k] = b0 + 32 * k < b1 ? __ldcg(a.part + (int64_t)(b0 + 32 * k) * a.D + c) : 0.f;
+#pragma unroll
+        for (int k = 0; k < kRopeMaxBlocks / 32; ++k) v += w[k];
     }
+    red[strand][x] = v;
+    __syncthreads();
+    v = red[x][strand];  // a warp per column
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (x == 0 && blockIdx.x * 32 + strand < a.D) a.out[q][blockIdx.x * 32 + strand] = v;
 }
 
 // ---------------------------------------------------------------------------
 
-constexpr int kRopeMaxBlocks = 640;  // of the backward kernel, at most: four per SM
 
 template <class T, bool INTER, bool BACK>
 static const void *rope_pick(bool vec, int D) {
@@ -438,21 +579,23 @@ static attt_status rope_run(const attt_rope_part *parts, int nparts, const int32
     a.pos = d_pos; a.freq = d_freq;
     a.T = T; a.nparts = nparts; a.D = (int)D; a.half = (int)(rot / 2);
     a.eps = eps; a.mscale = mscale;
-    // tokens of a block at a time: some 128 heads, as many as its table holds, and no fewer blocks
-    // than two per SM
-    int64_t tokens = std::min<int64_t>(cdiv(128, heads), cdiv(T, 2 * sms));
-    if (a.half > 0) tokens = std::min<int64_t>(tokens, kRopeTable / a.half);
-    a.tokens = (int)std::max<int64_t>(tokens, 1);
-    const int64_t tiles = cdiv(T, a.tokens);
+    a.tokens = a.half > 0 ? std::max(1, kRopeTable / a.half) : 1 << 20;
+    // a block for some 32 heads, as many as are resident together; a run of tokens each
+    for (int i = 0; i < nparts; ++i) {
+        const int64_t h = a.part[i].heads;
+        a.part[i].magic = h > 1 ? (uint32_t)(((1ull << 32) + h - 1) / h) : 0;
+        a.tokens = (int)std::min<int64_t>(a.tokens, std::max<int64_t>(1, 65536 / h));  // the division's range
+    }
     int blocks;
     if (!back) {
-        blocks = (int)std::min<int64_t>(tiles, 1 << 30);
+        blocks = (int)std::min({T, cdiv(T * heads, 32), (int64_t)sms * kRopeForward});
     } else {
         // every part has blocks of its own (their sums stay in registers), by its share of the heads
-        const int all = std::min(4 * sms, kRopeMaxBlocks);
+        const int all = std::min(kRopeBack * sms, kRopeMaxBlocks);
         for (int i = 0; i < nparts; ++i) {
-            int64_t n = nparts == 1 ? all : std::max<int64_t>(1, all * parts[i].heads / heads);
-            a.block0[i + 1] = a.block0[i] + (int)std::min<int64_t>(n, tiles);
+            const int64_t h = parts[i].heads;
+            const int64_t n = nparts == 1 ? all : std::max<int64_t>(1, all * h / heads);
+            a.block0[i + 1] = a.block0[i] + (int)std::min({T, cdiv(T * h, 32), n});
         }
         blocks = a.block0[nparts];
         a.dgamma = sums ? ws : nullptr;
@@ -478,7 +621,7 @@ static attt_status rope_run(const attt_rope_part *parts, int nparts, const int32
     for (int i = 0; i <= nparts; ++i) s.block0[i] = a.block0[i];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)cdiv(D, 32), (unsigned)nparts);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(1024);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

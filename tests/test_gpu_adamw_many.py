@@ -1,6 +1,8 @@
 """attt_adamw_step over many tensors: with moments in 32 bits the bits of
-attt_lora_adamw_step, with moments in 8 those of the oracle, whose fp32 operations are
-the documented ones in their order."""
+attt_lora_adamw_step, with moments in 8 the codes and scales of the oracle, whose fp32
+operations are the documented ones in their order, and parameters whose update m / denom goes
+through an approximate reciprocal: 2 u of its own, five roundings before and after, 2^-21 of
+the update, and two roundings of p (u = 2^-24)."""
 import numpy as np
 import pytest
 import torch
@@ -80,9 +82,12 @@ def test_8_bits(offset):
         _step(opt, t, seed)
         for k in range(len(SIZES)):
             p, m8, v8, sm, sv = bl.adamw8(*(h[k] for h in host), **HYPER, t=t, seed=seed, tensor=k)
-            host[0][k], host[2][k], host[3][k], host[4][k], host[5][k] = p, m8, v8, sm, sv
-            for got, want in zip((ps, ms, vs, sms, svs), (p, m8, v8, sm, sv)):
+            before = host[0][k].astype(np.float64)
+            host[0][k], host[2][k], host[3][k], host[4][k], host[5][k] = ps[k].cpu().numpy(), m8, v8, sm, sv
+            for got, want in zip((ms, vs, sms, svs), (m8, v8, sm, sv)):
                 assert _same(got[k], want), (t, k)
+            update = np.abs(p - before * (1 - HYPER["lr"] * HYPER["wd"]))
+            assert (np.abs(host[0][k].astype(np.float64) - p) <= 2.0 ** -21 * update + 4 * 2.0 ** -24 * np.abs(before)).all()
             assert torch.equal(p16s[k], ps[k].to(torch.bfloat16))
         m32, v32 = attt.attt_adamw_read_state(opt)
         at = 0
