@@ -98,6 +98,9 @@ attt_status batch_input_grad(const attt_bf16 *d_dy, const int64_t *off, int E, c
                              int64_t d, int r, float scale, float *d_dx, int64_t rows_bound, void *d_ws,
                              size_t ws_bytes, cudaStream_t stream);
 
+// Clusters of c CTAs (1 to 8), one CTA per SM, that a device holds at once (lora.cu).
+int resident_clusters(int c, int dev);
+
 // Products of activations with an adapter's matrix (lora.cu): out16[m, i rpad + c] =
 // bf16(scale (a_i M_i)[m, c]), c < rpad = r rounded up to 16, for n <= 2 activations a_i (bf16
 // [L, K]) and M_i [K, r] (mn; r a multiple of 8) or M_i^T [r, K].  `pdl`: launched

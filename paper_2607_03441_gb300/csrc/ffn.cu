@@ -17,6 +17,7 @@
 
 #include "attt_host.h"
 #include "tc_ffn.cuh"
+#include "tc_ffn_few.cuh"
 
 namespace attt {
 
@@ -394,6 +395,178 @@ static attt_status ffn_contract(const FfnProblem &q, int dev, cudaStream_t strea
 }
 
 // ---------------------------------------------------------------------------
+// At most 128 rows
+// ---------------------------------------------------------------------------
+
+// One contraction of a call: activations a[i] [M, K] against weights b (FEW_GLU: gate and up of one
+// segment; FEW_DX: one of each segment) and up to two adapters.
+struct FewProblem {
+    const void *a[2], *b[2];
+    int64_t K;  // of a segment
+    int M, N;
+    struct {
+        const void *first;   // FEW_GLU, FEW_DOWN: A [K, r8]; else B [r, K]
+        const void *second;  // B [r, N] or A [N, r]
+        int slot;            // segment, or half of FEW_GLU
+    } rank[2];
+    int nrank, r, r8;
+    float scale;
+    bool pdl, weights_wait;
+    int act;
+    const __nv_bfloat16 *gate, *up;
+    __nv_bfloat16 *out[3];
+};
+
+// The tile's columns, the CTAs per tile and per SM.  An SM takes a stage's bytes at some 65 a ns; a CTA
+// begins and ends in some 5 us, which waves of CTAs pay one after the other, but for two CTAs
+// per SM, each with half of shared memory and of TMEM.  (Two per SM only for tiles of one CTA that
+// are more than the SMs: a grid of fewer, or one that starts beside the previous one's end, is
+// packed on half of the SMs: y of 64 rows at 5,120 x 27,648 61 -> 109 us.)
+struct FewPlan {
+    int n_tile, cluster, stages, per_sm;
+};
+
+static uint32_t few_w_bytes(int mode, int n_tile, int nrank, int rpad) {
+    const int bn = mode == FEW_GLU ? 2 * n_tile : n_tile;
+    return (uint32_t)bn * 128u + (uint32_t)nrank * (mode == FEW_GLU || mode == FEW_DOWN ? 8192u : (uint32_t)rpad * 128u);
+}
+
+// Shared memory behind the ring: the rank-r products, the second matrices, barriers.
+static uint32_t few_products(int M, int nrank, int rpad) { return (uint32_t)round_up(M, 16) * (nrank * rpad + 8) * 2u; }
+static uint32_t few_second(int n_tile, int nrank, int rpad) { return (uint32_t)(nrank * n_tile * (rpad + 8)) * 2u; }
+static uint32_t few_tail(int M, int n_tile, int nrank, int rpad) {
+    return few_products(M, nrank, rpad) + few_second(n_tile, nrank, rpad) + 8u * (2 * kFewMaxStages + 1) + 16u;
+}
+static uint32_t few_sums(int mode, int M, int n_tile, int nrank, int rpad) {
+    const int cols = (mode == FEW_GLU ? 2 * n_tile : n_tile) + nrank * rpad;
+    return (uint32_t)(M * (cols + 4) * 4);
+}
+
+static FewPlan few_plan(int mode, int M, int64_t N, int64_t kb, int nrank, int rpad, double bytes, bool pdl, int dev) {
+    FewPlan best{64, 1, 2, 1};
+    double best_t = 1e30;
+    const uint32_t a_alloc = (uint32_t)round_up(M, 8) * 128u;
+    for (int per_sm = 1; per_sm <= 2; ++per_sm)
+        for (int n_tile = 128; n_tile >= 64; n_tile /= 2) {
+            const int cols = (mode == FEW_GLU ? 2 * n_tile : n_tile) + nrank * rpad;
+            if (cols * per_sm > 512) continue;
+            const uint32_t w = few_w_bytes(mode, n_tile, nrank, rpad), total = per_sm == 2 ? 115200u : (uint32_t)kMaxSmem,
+                           tail = few_tail(M, n_tile, nrank, rpad) + 2048u;
+            if (tail + few_sums(mode, M, n_tile, nrank, rpad) > total || tail + 2 * (a_alloc + w) > total) continue;
+            const int stages = (int)std::min<uint32_t>(kFewMaxStages, (total - tail) / (a_alloc + w));
+            if (a_alloc + stages * w < 16384u) continue;
+            const int64_t tiles = cdiv(N, n_tile);
+            if (per_sm == 2 && tiles <= resident_clusters(1, dev)) continue;
+            for (int c = 1; c <= (per_sm == 2 ? 1 : kFewMaxCluster) && c <= kb; ++c) {
+                // clusters that start while the previous grid's CTAs leave are not packed as those of an idle
+                // device: with all places needed some ran after the others (28 clusters of 5, dx of 93 rows
+                // at 3,584 x 18,944: 85 us, 62 with seven eighths of the places taken, 112 CTAs)
+                const int held = resident_clusters(c, dev), places = pdl && c > 1 ? std::max(1, held * 7 / 8) : held;
+                const int64_t each = cdiv(tiles, places), waves = cdiv(each, per_sm);
+                const double run = (double)each * cdiv(kb, c) * (a_alloc + w) / 65e9, hbm = bytes / 6.7e12;
+                const double end = M * (double)(mode == FEW_GLU ? 2 : 1) * n_tile * 8 / 100e9;
+                const double t = (run > hbm ? run : hbm) + waves * (5.0e-6 + end) + (c > 1 ? 1.0e-6 : 0.0);
+                if (t < 0.98 * best_t) {
+                    best_t = t;
+                    best = FewPlan{n_tile, c, (int)std::min<int64_t>(stages, cdiv(kb, c)), per_sm};
+                    if (best.stages < 2) best.stages = 2;
+                }
+            }
+        }
+    return best;
+}
+
+template <int MODE>
+static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t stream) {
+    constexpr bool mn = MODE == FEW_GLU || MODE == FEW_DOWN;
+    const int rpad = (int)round_up(q.r, 16), nseg = MODE == FEW_DX ? 2 : 1;
+    const int64_t kbs = cdiv(q.K, 64), kb = kbs * nseg;
+    if (kb > (1ll << 30)) return ATTT_ERR_UNSUPPORTED;
+    const double bytes = 2.0 * q.K * nseg * (q.M + q.N * (MODE == FEW_GLU ? 2.0 : 1.0));
+    const FewPlan t = few_plan(MODE, q.M, q.N, kb, q.nrank, rpad, bytes, q.pdl, dev);
+
+    FewMaps maps;
+    FewArgs p{};
+    p.M = q.M; p.N = q.N; p.n_tile = t.n_tile;
+    p.BN = MODE == FEW_GLU ? 2 * t.n_tile : t.n_tile;
+    p.nseg = nseg;
+    p.kb[0] = p.kb[1] = (int)kbs;
+    p.kb_total = (int)kb;
+    p.nrank = q.nrank; p.r = q.r; p.rpad = rpad;
+    p.scale = q.scale;
+    p.cluster = t.cluster; p.stages = t.stages;
+    p.a_bytes = p.a_alloc = (uint32_t)round_up(q.M, 8) * 128u;
+    p.b_bytes = (uint32_t)p.BN * 128u;
+    p.r_bytes = mn ? 8192u : (uint32_t)rpad * 128u;
+    const uint32_t ring = (uint32_t)t.stages * (p.a_alloc + few_w_bytes(MODE, t.n_tile, q.nrank, rpad));
+    p.ring_bytes = (uint32_t)round_up(std::max({ring, few_sums(MODE, q.M, t.n_tile, q.nrank, rpad), p.a_alloc + 16384u}), 1024);
+    const int cols = p.BN + q.nrank * rpad;
+    p.pitch = cols + 4;
+    p.vpitch = q.nrank * rpad + 8;
+    p.tmem_cols = 32;
+    while ((int)p.tmem_cols < cols) p.tmem_cols <<= 1;
+    p.weights_wait = q.weights_wait ? 1 : 0;
+    p.act = q.act;
+    p.keep = MODE == FEW_GLU && q.out[1] ? 1 : 0;
+    p.gate = q.gate; p.up = q.up;
+    for (int i = 0; i < 3; ++i) p.out[i] = q.out[i];
+    p.status = device_status_word(dev);
+    const uint32_t a_box = (uint32_t)round_up(q.M, 8);
+    for (int i = 0; i < 2; ++i) {
+        const bool seg = i < nseg;
+        if (!seg) maps.a[i] = maps.a[0];
+        else if (!make_tmap_bf16(&maps.a[i], q.a[i], (uint64_t)q.K, (uint64_t)q.M, (uint64_t)q.K * 2, 64, a_box))
+            return ATTT_ERR_INVALID_ARG;
+        const bool has = MODE == FEW_GLU || seg;
+        if (!has) maps.b[i] = maps.b[0];
+        else if (mn ? !make_tmap_bf16(&maps.b[i], q.b[i], (uint64_t)q.N, (uint64_t)q.K, (uint64_t)q.N * 2, 64, 64)
+                    : !make_tmap_bf16(&maps.b[i], q.b[i], (uint64_t)q.K, (uint64_t)q.N, (uint64_t)q.K * 2, 64,
+                                      (uint32_t)t.n_tile))
+            return ATTT_ERR_INVALID_ARG;
+        if (i >= q.nrank) {
+            maps.r[i] = maps.b[0];
+            continue;
+        }
+        if (mn ? !make_tmap_bf16(&maps.r[i], q.rank[i].first, (uint64_t)q.r8, (uint64_t)q.K, (uint64_t)q.r8 * 2, 64, 64)
+               : !make_tmap_bf16(&maps.r[i], q.rank[i].first, (uint64_t)q.K, (uint64_t)q.r, (uint64_t)q.K * 2, 64,
+                                 (uint32_t)rpad))
+            return ATTT_ERR_INVALID_ARG;
+        p.rank[i] = FewRank{MODE == FEW_DX ? q.rank[i].slot : 0, p.BN + i * rpad, MODE == FEW_GLU ? q.rank[i].slot : 0,
+                            static_cast<const __nv_bfloat16 *>(q.rank[i].second), mn ? (int64_t)q.N : (int64_t)q.r};
+    }
+    p.second_at = p.ring_bytes + few_products(q.M, q.nrank, rpad);
+    p.bars_at = p.second_at + few_second(t.n_tile, q.nrank, rpad);
+    size_t smem = 1024 + (size_t)p.ring_bytes + few_tail(q.M, t.n_tile, q.nrank, rpad);
+    if (t.per_sm == 1) smem = std::max<size_t>(smem, 118784);  // so that an SM takes one
+    auto kern = ffn_few_kernel<MODE>;
+    if (smem > kMaxSmem || !set_smem_limit(reinterpret_cast<const void *>(kern), smem, dev)) return ATTT_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(cdiv(q.N, t.n_tile) * t.cluster));
+    cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    unsigned na = 0;
+    if (q.pdl) {
+        attr[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[na].val.programmaticStreamSerializationAllowed = 1;
+        ++na;
+    }
+    if (t.cluster > 1) {
+        attr[na].id = cudaLaunchAttributeClusterDimension;
+        attr[na].val.clusterDim.x = (unsigned)t.cluster;
+        attr[na].val.clusterDim.y = 1;
+        attr[na].val.clusterDim.z = 1;
+        ++na;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = na;
+    if (cudaLaunchKernelEx(&cfg, kern, maps, p) != cudaSuccess) return ATTT_ERR_CUDA;
+    count_launch();
+    return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------------------
 // Arguments
 // ---------------------------------------------------------------------------
 
@@ -469,6 +642,39 @@ attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, 
     st = ffn_pad_adapters(ad, 7, c, d, f, r, dev, launched, stream);
     if (st != ATTT_OK) return st;
 
+    if (L <= kFewRows) {
+        FewProblem q{};
+        q.a[0] = d_x; q.b[0] = d_Wg; q.b[1] = d_Wu;
+        q.K = d; q.M = (int)L; q.N = (int)f;
+        q.r = r; q.r8 = c.r8; q.scale = scale;
+        for (int i = 0; i < 2; ++i)
+            if (ad.A[i]) {
+                q.rank[q.nrank].first = ad.A[i];
+                q.rank[q.nrank].second = ad.B[i];
+                q.rank[q.nrank++].slot = i;
+            }
+        q.pdl = q.weights_wait = launched;
+        q.act = act;
+        q.out[0] = reinterpret_cast<__nv_bfloat16 *>(d_h);
+        q.out[1] = reinterpret_cast<__nv_bfloat16 *>(d_g);
+        q.out[2] = reinterpret_cast<__nv_bfloat16 *>(d_u);
+        st = few_contract<FEW_GLU>(q, dev, stream);
+        if (st != ATTT_OK) return st;
+        FewProblem y{};
+        y.a[0] = d_h; y.b[0] = d_Wd;
+        y.K = f; y.M = (int)L; y.N = (int)d;
+        y.r = r; y.r8 = c.r8; y.scale = scale;
+        if (ad.A[2]) {
+            y.rank[0].first = ad.A[2];
+            y.rank[0].second = ad.B[2];
+            y.nrank = 1;
+        }
+        y.pdl = true;
+        y.weights_wait = launched;
+        y.out[0] = reinterpret_cast<__nv_bfloat16 *>(d_y);
+        return few_contract<FEW_DOWN>(y, dev, stream);
+    }
+
     FfnProblem q{};
     q.M = (int)L; q.N = (int)f;
     q.act = act;
@@ -536,6 +742,37 @@ attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg
     st = current_device(&dev);
     if (st != ATTT_OK) return st;
     const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
+    if (L <= kFewRows) {
+        FewProblem q{};
+        q.a[0] = d_dy; q.b[0] = d_Wd;
+        q.K = d; q.M = (int)L; q.N = (int)f;
+        q.r = r; q.scale = scale;
+        if (ad.A[2]) {
+            q.rank[0].first = ad.B[2];
+            q.rank[0].second = ad.A[2];
+            q.nrank = 1;
+        }
+        q.act = act;
+        q.gate = reinterpret_cast<const __nv_bfloat16 *>(d_g);
+        q.up = reinterpret_cast<const __nv_bfloat16 *>(d_u);
+        q.out[0] = reinterpret_cast<__nv_bfloat16 *>(d_dg);
+        q.out[1] = reinterpret_cast<__nv_bfloat16 *>(d_du);
+        st = few_contract<FEW_GRAD>(q, dev, stream);
+        if (st != ATTT_OK || !d_dx) return st;
+        FewProblem x{};
+        x.a[0] = d_dg; x.a[1] = d_du; x.b[0] = d_Wg; x.b[1] = d_Wu;
+        x.K = f; x.M = (int)L; x.N = (int)d;
+        x.r = r; x.scale = scale;
+        for (int i = 0; i < 2; ++i)
+            if (ad.A[i]) {
+                x.rank[x.nrank].first = ad.B[i];
+                x.rank[x.nrank].second = ad.A[i];
+                x.rank[x.nrank++].slot = i;
+            }
+        x.pdl = true;
+        x.out[0] = reinterpret_cast<__nv_bfloat16 *>(d_dx);
+        return few_contract<FEW_DX>(x, dev, stream);
+    }
     bool launched = false;
     st = ffn_pad_adapters(ad, d_dx ? 7 : 4, c, d, f, r, dev, launched, stream);
     if (st != ATTT_OK) return st;

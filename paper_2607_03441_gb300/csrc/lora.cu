@@ -376,6 +376,8 @@ static int skinny_clusters(int c, int dev) {
     return n;
 }
 
+int resident_clusters(int c, int dev) { return skinny_clusters(c, dev); }
+
 // Microseconds one K block takes a CTA: its operands from L2 (62 bytes a cycle
 // into an SM) or the issue of its loads and MMAs, whichever is longer.
 static double skinny_block(int nb, int n, bool mn) {
