@@ -913,10 +913,10 @@ def _heads(t: torch.Tensor, shape, dtype, name: str):
     if t.shape != shape or t.dtype != dtype:
         _expect(t, shape, dtype, name)
     ld, hs, one = t.stride()
-    if not t.is_cuda:
-        raise ValueError("expected a CUDA tensor")
     if one != 1 and shape[2] > 1:
         raise ValueError(f"{name}: expected heads whose values are contiguous")
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
     return t.data_ptr(), ld, hs
 
 
