@@ -190,7 +190,6 @@ __global__ void __launch_bounds__(ffn_threads(SETS), 1)
             mbar_init(tfull0 + 8 * a, 1);
             mbar_init(tempty0 + 8 * a, (PAIR ? 8 : 4) * SETS);
         }
-        griddep_launch_dependents();
         mbar_init(drain0, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -211,6 +210,9 @@ __global__ void __launch_bounds__(ffn_threads(SETS), 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    // not before TMEM is allocated: a CTA of the next grid that shares the SM could otherwise take the columns
+    // that this one needs, and wait for this grid
+    if (threadIdx.x == 0) griddep_launch_dependents();
 
     const int tiles_m = PAIR ? (g.tiles_m + 1) / 2 : g.tiles_m;  // of the accumulator's height
     const int nwork = work_count(g, tiles_m);

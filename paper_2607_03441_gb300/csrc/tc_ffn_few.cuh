@@ -111,7 +111,6 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(done, 1);
-        griddep_launch_dependents();
         *abort_flag = 0;
         fence_mbar_init();
     }
@@ -128,6 +127,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (threadIdx.x == 0) griddep_launch_dependents();  // not before TMEM is allocated (tc_ffn.cuh)
 
     if (warp == 0 || warp >= 6) {
         if (elect_one()) {

@@ -160,7 +160,6 @@ __global__ void __launch_bounds__(kSkinnyThreads, 1)
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(done, 1);
-        griddep_launch_dependents();
         *abort_flag = 0;
         fence_mbar_init();
     }
@@ -176,6 +175,9 @@ __global__ void __launch_bounds__(kSkinnyThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    // not before TMEM is allocated: where the grid before this one still holds an SM's columns, a CTA of the
+    // grid after it could otherwise take them first, and wait for this grid
+    if (threadIdx.x == 0) griddep_launch_dependents();
 
     if (warp == 0) {
         if (elect_one()) {

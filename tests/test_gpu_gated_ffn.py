@@ -6,6 +6,8 @@ Bounds.  A contraction over K adds K products of bf16 (exact in fp32) on the ten
 rounded to bf16 once, 2^-8 of itself, and so are results.  The activation's exponential is off by
 at most 2 + 1.16 |z| units of 2^-23, z within 40 of zero where its share of the result is not
 below 2^-50: 6e-6 of it; act' is at most 1.13, act at most |g|."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -194,7 +196,7 @@ def test_gradient_against_differences():
     f = [(dy * bl.gated_ffn(x + s * e * v, Wg, Wu, Wd, As, Bs, c.scale)[0]).sum() for s in (1, -1)]
     # dx from g, u, dg, du rounded to bf16 and rounded itself: five roundings of 2^-8 of terms that
     # add up in 384 places with random signs, each of size |dx v|
-    assert abs((f[0] - f[1]) / (2 * e) - (_host(dx) * v).sum()) < 5 * R16 * np.sqrt(384) * np.abs(dx.float().cpu()).max().item() * 3
+    assert abs((f[0] - f[1]) / (2 * e) - (_host(dx) * v).sum()) < 5 * R16 * math.sqrt(384) * dx.float().abs().max().item() * 3
 
 
 def test_rows_behind_the_last_and_outputs_given():
