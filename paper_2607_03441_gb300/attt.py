@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 from typing import Optional, Sequence, Tuple
 
@@ -244,7 +245,7 @@ def _rows_of(t: torch.Tensor, shape, dtype, name: str) -> Tuple[int, int]:
     return _rows_ptr(t, name)
 
 
-_F32 = torch.float32
+_F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
 
 
 def _f32_of(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
@@ -923,7 +924,7 @@ def _heads(t: torch.Tensor, shape, dtype, name: str):
 def _rope_check(xs, pos, freq, gammas):
     """(T, D, type, its name in the C ABI) of a call's heads."""
     k = len(xs)
-    if k < 1 or k > 2:
+    if k != 1 and k != 2:
         raise ValueError("one or two tensors of heads are expected")
     if gammas is not None and len(gammas) != k:
         raise ValueError("gammas must have one entry per tensor")
@@ -938,14 +939,15 @@ def _rope_check(xs, pos, freq, gammas):
         other = xs[1].shape
         if len(other) != 3 or other[0] != T or other[2] != D:
             raise ValueError(f"expected [{T}, heads, {D}] tensors, got shape {tuple(other)}")
-    if pos.shape != (T,) or pos.dtype != torch.int32:
-        _expect(pos, (T,), torch.int32, "pos")
-    if freq.dtype != torch.int64 or freq.dim() != 1:
+    if pos.shape != (T,) or pos.dtype != _I32:
+        _expect(pos, (T,), _I32, "pos")
+    if freq.dtype != _I64 or freq.dim() != 1:
         raise ValueError("freq: expected an int64 vector (attt_rope_frequencies)")
     return T, D, dtype, code
 
 
-_ROPE_PARTS = {k: ctypes.c_int64 * (12 * k) for k in (1, 2)}  # attt_rope_part's words
+# attt_rope_part's words, of one and of two parts (a ctypes array takes 2 us to fill, a packed string half of one)
+_ROPE_PARTS = {k: struct.Struct(f"{12 * k}q").pack for k in (1, 2)}
 
 
 def attt_rope_forward(xs: Sequence[torch.Tensor], pos: torch.Tensor, freq: torch.Tensor,
@@ -969,7 +971,7 @@ def attt_rope_forward(xs: Sequence[torch.Tensor], pos: torch.Tensor, freq: torch
         words += (px, py, 0, 0 if g is None else _f32_of(g, (D,), "gammas"), 0, x_ld, x_hs, y_ld, y_hs, 0, 0, shape[1])
     parts = _ROPE_PARTS[len(xs)](*words)
     _check((_lib or load_library()).attt_rope_forward(
-        ctypes.addressof(parts), len(xs), _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0,
+        parts, len(xs), _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0,
         mscale, code, _stream(stream)), "attt_rope_forward")
     return ys
 
@@ -1020,7 +1022,7 @@ def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Option
     if workspace is None and sums:
         workspace = _empty(attt_rope_workspace_bytes(T, D), dtype=torch.uint8, device=dev, stream=stream)
     _check((_lib or load_library()).attt_rope_backward(
-        ctypes.addressof(parts), k, _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0, mscale,
+        parts, k, _ptr(pos), _ptr(freq), T, D, 2 * freq.shape[0], eps, 1 if interleaved else 0, mscale,
         code, _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)),
         "attt_rope_backward")
     return dxs, dgammas
@@ -1031,6 +1033,7 @@ def attt_rope_backward(dys: Sequence[torch.Tensor], xs: Optional[Sequence[Option
 # --------------------------------------------------------------------------
 
 _ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+_FFN_ADAPTERS = struct.Struct("3q").pack  # a call's array of adapters, gate, up, down
 _BF16 = torch.bfloat16
 
 
@@ -1049,7 +1052,7 @@ def _bf16_of(t: Optional[torch.Tensor], shape, name: str) -> Optional[int]:
 
 def _ffn_check(x: torch.Tensor, Wg: torch.Tensor, Wu, Wd, As, Bs, act: str):
     """(L, d, f, r, code of the activation, addresses of x and the weights, the C call's
-    arrays of adapters with the addresses of A and B)."""
+    arrays of A and of B)."""
     if x.dim() != 2 or Wg.dim() != 2:
         raise ValueError("expected 2-D activations and weights")
     L, d = x.shape
@@ -1065,20 +1068,21 @@ def _ffn_check(x: torch.Tensor, Wg: torch.Tensor, Wu, Wd, As, Bs, act: str):
     if not given:
         if Bs is not None and any(B is not None for B in Bs):
             raise ValueError("As and Bs must have None in the same places")
-        return L, d, f, 0, code, w, None, None, None
+        return L, d, f, 0, code, w, None, None
     if given[0].dim() != 2:
         raise ValueError("As: expected 2-D tensors")
     r = given[0].shape[1]
-    buf = (ctypes.c_int64 * 6)()
-    for i, (A, B) in enumerate(zip(As, Bs)):
-        if (A is None) != (B is None):
-            raise ValueError("As and Bs must have None in the same places")
-        if A is not None:
-            wide, out = (f, d) if i == 2 else (d, f)
-            buf[i] = _bf16_of(A, (wide, r), f"As[{i}]")
-            buf[3 + i] = _bf16_of(B, (r, out), f"Bs[{i}]")
-    at = ctypes.addressof(buf)
-    return L, d, f, r, code, w, buf, at, at + 24
+    at = []
+    for i in range(3):
+        A, B = As[i], Bs[i]
+        if A is None or B is None:
+            if A is not B:
+                raise ValueError("As and Bs must have None in the same places")
+            at += (0, 0)
+            continue
+        wide, out = (f, d) if i == 2 else (d, f)
+        at += (_bf16_of(A, (wide, r), "As"), _bf16_of(B, (r, out), "Bs"))
+    return L, d, f, r, code, w, _FFN_ADAPTERS(*at[::2]), _FFN_ADAPTERS(*at[1::2])
 
 
 def attt_gated_ffn_forward(x: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor,
@@ -1090,7 +1094,7 @@ def attt_gated_ffn_forward(x: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, 
     """The block y = h Wd + s (h A_2) B_2, h = act(g) u, with g and u projections of x (all
     bf16; As and Bs: the adapters of gate, up and down, or None).  Returns (y, h, g, u);
     g and u, which the backward call takes, where `save` asks for them or tensors are given."""
-    L, d, f, r, code, w, keep, pA, pB = _ffn_check(x, Wg, Wu, Wd, As, Bs, act)
+    L, d, f, r, code, w, pA, pB = _ffn_check(x, Wg, Wu, Wd, As, Bs, act)
     dev = x.device
     if y is None:
         y = _empty(L, d, dtype=_BF16, device=dev, stream=stream)
@@ -1119,7 +1123,7 @@ def attt_gated_ffn_backward(dy: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor
     """The block's gradients from dy, with the forward call's g and u.  Returns (dx, dg, du):
     dg and du are the upstream gradients of the gate's and up's adapters.  Without
     `input_grad`, dx is formed only where a tensor for it is given."""
-    L, d, f, r, code, w, keep, pA, pB = _ffn_check(dy, Wg, Wu, Wd, As, Bs, act)
+    L, d, f, r, code, w, pA, pB = _ffn_check(dy, Wg, Wu, Wd, As, Bs, act)
     dev = dy.device
     if dx is None and input_grad:
         dx = _empty(L, d, dtype=_BF16, device=dev, stream=stream)
