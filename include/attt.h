@@ -416,7 +416,7 @@ ATTT_API attt_status attt_adamw_destroy(attt_adamw *h);
  * gives every step another seed, and the same seed repeats a step bit for bit.  A block whose
  * largest value is below 2^-100 becomes zeros, one with a NaN or an infinity NaN as a whole;
  * with 32 bits only its own value feels it.  Requirements: 0 <= b1, b2 < 1, eps > 0 in
- * fp32, weight_decay >= 0, step >= 1, all finite; the handle's device current.  One launch; a
+ * fp32 (8 bits: at least 1e-30), weight_decay >= 0, step >= 1, all finite; the handle's device current.  One launch; a
  * captured step repeats its own `step` and seed.
  */
 ATTT_API attt_status attt_adamw_step(attt_adamw *h, double lr, double beta1, double beta2, double eps,

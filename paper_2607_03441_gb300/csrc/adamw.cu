@@ -485,6 +485,8 @@ attt_status attt_adamw_step(attt_adamw *h, double lr, double beta1, double beta2
     if (!h || step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f) ||
         !(weight_decay >= 0.0) || !std::isfinite(lr) || !std::isfinite(eps) || !std::isfinite(weight_decay))
         return ATTT_ERR_INVALID_ARG;
+    // (8 bits: 1 / eps stays finite, so that a value without moments stays where it is)
+    if (h->bits == 8 && eps < 1e-30) return ATTT_ERR_INVALID_ARG;
     const attt_status st = adam_device(h);
     if (st != ATTT_OK) return st;
     if (h->blocks == 0) return ATTT_OK;

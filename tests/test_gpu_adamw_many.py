@@ -206,6 +206,32 @@ def test_graph_stream_and_many_tensors():
         assert torch.equal(a, b)
 
 
+def test_some_bf16_copies_and_matrices():
+    """Tensors of two dimensions, with and without a bf16 copy, one without values."""
+    ps = [torch.randn(s, device=DEV) for s in ((16, 40), (0, 5), (300,))]
+    gs, ms, vs = ([torch.randn_like(p) if k == 0 else torch.zeros_like(p) for p in ps] for k in range(3))
+    p16s = [torch.zeros(16, 40, dtype=torch.bfloat16, device=DEV), None, None]
+    ref = [p.clone() for p in ps]
+    one = attt.attt_adamw_create(ps, gs, ms, vs, p16s=p16s)
+    _step(one, 1)
+    _step(attt.attt_adamw_create(ref, gs, [torch.zeros_like(p) for p in ps], [torch.zeros_like(p) for p in ps]), 1)
+    assert all(torch.equal(a, b) for a, b in zip(ps, ref)) and torch.equal(p16s[0], ps[0].to(torch.bfloat16))
+    assert attt.attt_adamw_state_values(one) == 256 * (3 + 0 + 2)
+
+
+def test_values_without_gradients_stay_in_8_bits():
+    """No moments, no gradient, no decay: p keeps its bits, whatever eps."""
+    p, g = torch.randn(700, device=DEV), torch.zeros(700, device=DEV)
+    before = p.clone()
+    m, v = (torch.zeros(700, dtype=torch.uint8, device=DEV) for _ in range(2))
+    opt = attt.attt_adamw_create([p], [g], [m], [v], [torch.zeros(3, device=DEV)], [torch.zeros(3, device=DEV)])
+    for eps in (1e-30, 1e-8, 1.0):
+        attt.attt_adamw_step(opt, 0.1, eps=eps, weight_decay=0.0, step=1, seed=1)
+    assert torch.equal(p, before) and not m.any() and not v.any()
+    with pytest.raises(attt.AtttError):
+        attt.attt_adamw_step(opt, 0.1, eps=1e-31)
+
+
 def test_refusals():
     f = lambda n: torch.zeros(n, device=DEV)  # noqa: E731
     b = lambda n: torch.zeros(n, dtype=torch.uint8, device=DEV)  # noqa: E731

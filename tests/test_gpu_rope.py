@@ -4,7 +4,7 @@ Bounds, u = 2^-24: cosine and sine of an exact angle are off by at most 4 u (rou
 what is left of the angle, the function's own 2 u); turning adds two roundings: 8 u of the
 pair's two sizes.  A head's sum of squares goes through at most 16 additions in a lane and
 five between lanes: 32 u of it, 16 u of its root, and 4 u in what follows.  dgamma adds tokens
-and heads in at most 400 steps.  Results rounded to bf16 are off by 2^-8 of themselves."""
+and heads in at most 400 steps (a lane takes at most one of 32 groups' heads of 40,013 / 200 tokens).  Results rounded to bf16 are off by 2^-8 of themselves."""
 import numpy as np
 import pytest
 import torch
@@ -63,6 +63,9 @@ CASES = [  # T, heads, D, rot, interleaved, norm, dtype, form
     (1300, (8, 2), 128, 128, False, True, torch.bfloat16, "rows"), (1201, (6,), 64, 32, False, False, torch.bfloat16, "wide"),
     (2, (300, 1), 16, 16, False, True, torch.bfloat16, "rows"), (333, (1, 5), 48, 16, True, True, torch.float32, "wide"),
     (640, (2, 2), 258, 4, False, True, torch.float32, "rows"),
+    # runs of tokens that a block's table does not hold at once
+    (40013, (2, 1), 64, 64, False, True, torch.bfloat16, "rows"), (9001, (1,), 512, 512, True, True, torch.float32, "rows"),
+    (30011, (1, 1), 34, 34, False, True, torch.float32, "wide"),
 ]
 
 
@@ -167,6 +170,26 @@ def test_gradient_against_differences():
         f = [(dyh * bl.rope(xh + s * e * v * (which == 0), pos, w, gh + (s * e * v if which else 0))).sum() for s in (1, -1)]
         # fp32 gradients of 432 terms of size 1: 1e-5 at most; differences 1e-9 of them
         assert abs((f[0] - f[1]) / (2 * e) - (grad * v).sum()) < 2e-5
+
+
+def test_one_norm_of_two():
+    """Queries normed and keys not, and the other way round: as two calls."""
+    r = np.random.default_rng(6)
+    T, D = 33, 64
+    xs = [_heads(r, T, H, D, torch.bfloat16, "rows") for H in (4, 2)]
+    dys = [_heads(r, T, H, D, torch.bfloat16, "rows") for H in (4, 2)]
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    freq, g = attt.attt_rope_frequencies(D, device=DEV), torch.rand(D, device=DEV) + 0.5
+    for gammas in ([g, None], [None, g]):
+        ys = attt.attt_rope_forward(xs, pos, freq, gammas)
+        dxs, dgs = attt.attt_rope_backward(dys, [x if gm is not None else None for x, gm in zip(xs, gammas)], pos, freq, gammas)
+        for i in range(2):
+            one = [gammas[i]] if gammas[i] is not None else None
+            y, = attt.attt_rope_forward([xs[i]], pos, freq, one)
+            (dx,), (dg,) = attt.attt_rope_backward([dys[i]], [xs[i]], pos, freq, one)
+            assert torch.equal(y, ys[i]) and torch.equal(dx, dxs[i]) and (dg is None) == (dgs[i] is None)
+            if dg is not None:  # other blocks, another order of the sum: 33 x 4 terms
+                assert (dg - dgs[i]).abs().max() <= 132 * U * dgs[i].abs().max() * 4
 
 
 def test_zero_and_nan_heads():
