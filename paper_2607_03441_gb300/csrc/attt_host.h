@@ -27,7 +27,7 @@ int num_sms(int dev);
 int *device_status_word(int dev);
 
 // Encodes a 2-D bf16 tensor map with zero fill for out-of-range elements and
-// a shared-memory swizzle of `swizzle_bytes` (128, 64, or 0 for none).
+// a shared-memory swizzle of `swizzle_bytes` (128, 64, 32, or 0 for none).
 // `inner` is the contiguous extent, `outer` the number of rows, `row_bytes`
 // the row pitch.  Returns false if the driver rejects it.
 bool make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer,

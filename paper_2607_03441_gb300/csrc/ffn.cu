@@ -395,7 +395,7 @@ static attt_status ffn_contract(const FfnProblem &q, int dev, cudaStream_t strea
 }
 
 // ---------------------------------------------------------------------------
-// At most 128 rows
+// At most 32 rows
 // ---------------------------------------------------------------------------
 
 // One contraction of a call: activations a[i] [M, K] against weights b (FEW_GLU: gate and up of one
@@ -421,14 +421,14 @@ struct FewProblem {
 // begins and ends in some 5 us, which waves of CTAs pay one after the other, but for two CTAs
 // per SM, each with half of shared memory and of TMEM.  (Two per SM only for tiles of one CTA that
 // are more than the SMs: a grid of fewer, or one that starts beside the previous one's end, is
-// packed on half of the SMs: y of 64 rows at 5,120 x 27,648 61 -> 109 us.)
+// packed on half of the SMs: y of 64 rows at 5,120 x 27,648 61 -> 109 us when this took as many.)
 struct FewPlan {
     int n_tile, cluster, stages, per_sm;
 };
 
 static uint32_t few_w_bytes(int mode, int n_tile, int nrank, int rpad) {
     const int bn = mode == FEW_GLU ? 2 * n_tile : n_tile;
-    return (uint32_t)bn * 128u + (uint32_t)nrank * (mode == FEW_GLU || mode == FEW_DOWN ? 8192u : (uint32_t)rpad * 128u);
+    return (uint32_t)bn * 128u + (uint32_t)nrank * (uint32_t)(mode == FEW_GLU || mode == FEW_DOWN ? few_rank_cols(rpad) : rpad) * 128u;
 }
 
 // Shared memory behind the ring: the rank-r products, the second matrices, barriers.
@@ -459,8 +459,8 @@ static FewPlan few_plan(int mode, int M, int64_t N, int64_t kb, int nrank, int r
             if (per_sm == 2 && tiles <= resident_clusters(1, dev)) continue;
             for (int c = 1; c <= (per_sm == 2 ? 1 : kFewMaxCluster) && c <= kb; ++c) {
                 // clusters that start while the previous grid's CTAs leave are not packed as those of an idle
-                // device: with all places needed some ran after the others (28 clusters of 5, dx of 93 rows
-                // at 3,584 x 18,944: 85 us, 62 with seven eighths of the places taken, 112 CTAs)
+                // device: with all places needed some ran after the others (28 clusters of 5, dx of 93
+                // rows at 3,584 x 18,944, when this took as many: 85 us, 62 with seven eighths of the places taken, 112 CTAs)
                 const int held = resident_clusters(c, dev), places = pdl && c > 1 ? std::max(1, held * 7 / 8) : held;
                 const int64_t each = cdiv(tiles, places), waves = cdiv(each, per_sm);
                 const double run = (double)each * cdiv(kb, c) * (a_alloc + w) / 65e9, hbm = bytes / 6.7e12;
@@ -497,7 +497,8 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
     p.cluster = t.cluster; p.stages = t.stages;
     p.a_bytes = p.a_alloc = (uint32_t)round_up(q.M, 8) * 128u;
     p.b_bytes = (uint32_t)p.BN * 128u;
-    p.r_bytes = mn ? 8192u : (uint32_t)rpad * 128u;
+    p.r_cols = few_rank_cols(rpad);
+    p.r_bytes = (uint32_t)(mn ? p.r_cols : rpad) * 128u;
     const uint32_t ring = (uint32_t)t.stages * (p.a_alloc + few_w_bytes(MODE, t.n_tile, q.nrank, rpad));
     p.ring_bytes = (uint32_t)round_up(std::max({ring, few_sums(MODE, q.M, t.n_tile, q.nrank, rpad), p.a_alloc + 16384u}), 1024);
     const int cols = p.BN + q.nrank * rpad;
@@ -527,7 +528,8 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
             maps.r[i] = maps.b[0];
             continue;
         }
-        if (mn ? !make_tmap_bf16(&maps.r[i], q.rank[i].first, (uint64_t)q.r8, (uint64_t)q.K, (uint64_t)q.r8 * 2, 64, 64)
+        if (mn ? !make_tmap_bf16(&maps.r[i], q.rank[i].first, (uint64_t)q.r8, (uint64_t)q.K, (uint64_t)q.r8 * 2,
+                                 (uint32_t)p.r_cols, 64, 2 * p.r_cols)
                : !make_tmap_bf16(&maps.r[i], q.rank[i].first, (uint64_t)q.K, (uint64_t)q.r, (uint64_t)q.K * 2, 64,
                                  (uint32_t)rpad))
             return ATTT_ERR_INVALID_ARG;
@@ -564,6 +566,22 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
     if (cudaLaunchKernelEx(&cfg, kern, maps, p) != cudaSuccess) return ATTT_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
+}
+
+// Which calls tc_ffn_few.cuh's kernels take.  Two launches and their wider loads win where the weights
+// and the launches are all there is; the other kernels' chain of up to seven launches loads an adapter's
+// columns once instead of once per cluster and wastes less on more rows.  Times of the chain / of these kernels,
+// us, replayed from a graph, weights not in L2 (d x f, rank; forward, backward):
+//     rows     1,024 x 4,096, 16        3,584 x 18,944, 16      5,120 x 27,648, 0       2,048 x 8,192, 64
+//        1    31.1 / 25.5  27.9 / 23.8   96.7 / 79.4   99 / 81    171 / 128  151 / 134   41.5 / 42.9  42.3 / 40.4
+//        8    29.8 / 26.0  28.5 / 24.4   98.0 / 79.8  100 / 82    167 / 129  152 / 136   39.9 / 44.5  42.9 / 42.4
+//       32    27.8 / 28.8  28.7 / 27.9   98.9 / 82.9  100 / 84    144 / 132  151 / 139   40.8 / 49.8  44.2 / 47.8
+//       64    27.1 / 31.9  29.7 / 30.3  100.4 / 93.3  103 / 90    146 / 149  154 / 160   41.6 / 55.1  45.1 / 55.6
+//      128    27.9 / 38.8  31.1 / 38.0  103.7 / 105   109 / 104   153 / 184  160 / 181   43.6 / 68.3  47.2 / 75.4
+// Up to 8 rows: 7% faster over 12 such shapes each way; 16 and 32 rows: 8% where a matrix has 2^26 values or
+// more and r <= 16, 8% slower elsewhere.
+static bool ffn_few(int64_t L, int64_t d, int64_t f, int r) {
+    return L <= 8 || (L <= kFewRows && r <= 16 && d * f >= (1ll << 26));
 }
 
 // ---------------------------------------------------------------------------
@@ -642,7 +660,7 @@ attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, 
     st = ffn_pad_adapters(ad, 7, c, d, f, r, dev, launched, stream);
     if (st != ATTT_OK) return st;
 
-    if (L <= kFewRows) {
+    if (ffn_few(L, d, f, r)) {
         FewProblem q{};
         q.a[0] = d_x; q.b[0] = d_Wg; q.b[1] = d_Wu;
         q.K = d; q.M = (int)L; q.N = (int)f;
@@ -742,7 +760,7 @@ attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg
     st = current_device(&dev);
     if (st != ATTT_OK) return st;
     const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
-    if (L <= kFewRows) {
+    if (ffn_few(L, d, f, r)) {
         FewProblem q{};
         q.a[0] = d_dy; q.b[0] = d_Wd;
         q.K = d; q.M = (int)L; q.N = (int)f;

@@ -1,4 +1,4 @@
-// tc_ffn_few.cuh -- the gated feed-forward block's contractions for at most 128 rows,
+// tc_ffn_few.cuh -- the gated feed-forward block's contractions for at most 32 rows,
 // where the weights' bytes and the chain of launches are what they cost.
 //
 // A tile of columns belongs to a cluster of C CTAs (1 to 8) that share its K blocks; each
@@ -29,7 +29,7 @@ enum FewMode : int {
 };
 
 constexpr int kFewThreads = 256, kFewMaxStages = 8, kFewMaxCluster = 8;
-constexpr int kFewRows = 128;
+constexpr int kFewRows = 32;  // at most: a row's sums are one warp's lane
 constexpr int kFewStep = 4;  // fragments of a warp at a time
 
 // A rank-r product: of the activations of segment `seg`, with matrix map r[i], into accumulator
@@ -39,6 +39,17 @@ struct FewRank {
     const __nv_bfloat16 *second;
     int64_t ld;
 };
+
+// Weights MN-major: columns of the box that holds a product's matrix, and with it its swizzle, twice that
+// many bytes.  A box 64 wide whatever r is takes as much of a stage as 64 columns of weights, and the SM
+// fills its zeros at the same rate: forward, 1 row at 3,584 x 18,944 with r = 16, 82.3 us (79.4 so).
+constexpr int few_rank_cols(int rpad) { return rpad <= 16 ? 16 : rpad <= 32 ? 32 : 64; }
+
+// A descriptor's bits 61 to 63 for an MN-major matrix in such a box (64, 32 or 128 bytes of swizzle).
+__device__ __forceinline__ uint64_t few_rank_desc(uint32_t addr, int r_cols) {
+    const uint64_t mode = r_cols == 64 ? 2u : r_cols == 32 ? 4u : 6u;
+    return (smem_desc_sw128(addr, 8192u, (uint32_t)r_cols * 16u) & ~(uint64_t(7) << 61)) | mode << 61;
+}
 
 struct FewMaps {
     CUtensorMap a[2], b[2], r[2];
@@ -52,6 +63,7 @@ struct FewArgs {
     float scale;
     int cluster, stages;
     uint32_t a_alloc, a_bytes, b_bytes, r_bytes;  // per stage; r_bytes: of one product
+    int r_cols;            // weights MN-major: columns of a product's box (few_rank_cols)
     uint32_t ring_bytes, tmem_cols;
     int pitch, vpitch;     // of the sums (fp32) and of the rank-r products (bf16) in shared memory
     uint32_t second_at;    // behind the ring: the second matrices, [rank][column of the tile][rpad + 8]
@@ -187,6 +199,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             const int kb0 = p.nseg > 1 ? p.kb[0] : p.kb_total;  // blocks of the first segment
             // the segment whose blocks a product takes, and its first block here; none: past the end
             const int rs0 = p.nrank > 0 ? p.rank[0].seg : 2, rs1 = p.nrank > 1 ? p.rank[1].seg : 2;
+            const uint32_t rstep = B_MN ? (uint32_t)p.r_cols * 2u : step;
             const uint32_t col0 = tmem_base + (uint32_t)p.BN, col1 = col0 + (uint32_t)p.rpad;
             int slot = 0;
             uint32_t phase = 0;
@@ -206,16 +219,18 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 for (int kk = 0; kk < 4; ++kk)
                     umma_bf16(tmem_base, ad + kk * 2u, bd + kk * step, idesc, (kb > k0 || kk > 0) ? 1u : 0u);
                 if (rs0 == seg) {
-                    const uint64_t rd = smem_desc_sw128(b_addr + p.b_bytes, lbo, 1024);
+                    const uint32_t at = b_addr + p.b_bytes;
+                    const uint64_t rd = B_MN ? few_rank_desc(at, p.r_cols) : smem_desc_sw128(at, lbo, 1024);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        umma_bf16(col0, ad + kk * 2u, rd + kk * step, idesc_r, kk > 0 ? 1u : first);
+                        umma_bf16(col0, ad + kk * 2u, rd + kk * rstep, idesc_r, kk > 0 ? 1u : first);
                 }
                 if (rs1 == seg) {
-                    const uint64_t rd = smem_desc_sw128(b_addr + p.b_bytes + p.r_bytes, lbo, 1024);
+                    const uint32_t at = b_addr + p.b_bytes + p.r_bytes;
+                    const uint64_t rd = B_MN ? few_rank_desc(at, p.r_cols) : smem_desc_sw128(at, lbo, 1024);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        umma_bf16(col1, ad + kk * 2u, rd + kk * step, idesc_r, kk > 0 ? 1u : first);
+                        umma_bf16(col1, ad + kk * 2u, rd + kk * rstep, idesc_r, kk > 0 ? 1u : first);
                 }
                 umma_commit(empty0 + 8 * slot);
                 slot = next;
@@ -236,9 +251,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
             umma_commit(done);
         }
         __syncwarp();
-    }
-
-    else {
+    } else {
         // the second matrices' share of the tile, zeros past r and past the result's columns: runs of eight
         // values, four of them under way per thread (one by one, 32 to 128 trips to L2 in a row
         // were longer than the main loop of a small block)
@@ -295,25 +308,22 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     }
     __syncthreads();  // (a producer that gave up has stopped before the ring is written)
     const int cols = p.BN + p.nrank * p.rpad;
-    if (warp >= 2 && warp < 6) {
-        const int q = warp & 3, row = q * 32 + lane;
-        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
-        if (q * 32 < p.M)
-            for (int c = 0; c < cols; c += 16) {
-                float v[16];
-                tmem_ld_x16(taddr + (uint32_t)c, v);
-                // a product whose K blocks are all another CTA's has no sums here
-                bool empty = false;
-                for (int i = 0; i < p.nrank; ++i)
-                    if (c >= p.rank[i].col && c < p.rank[i].col + p.rpad && p.nseg > 1)
-                        empty = p.rank[i].seg == 0 ? k0 >= p.kb[0] : k1 <= p.kb[0];
-                if (row < p.M)
+    if (warp == 0 || warp == 4) {  // the two that may read rows 0 to 31: every other run of 16 columns each
+        for (int c = 16 * (warp >> 2); c < cols; c += 32) {
+            float v[16];
+            tmem_ld_x16(tmem_base + (uint32_t)c, v);
+            // a product whose K blocks are all another CTA's has no sums here
+            bool empty = false;
+            for (int i = 0; i < p.nrank; ++i)
+                if (c >= p.rank[i].col && c < p.rank[i].col + p.rpad && p.nseg > 1)
+                    empty = p.rank[i].seg == 0 ? k0 >= p.kb[0] : k1 <= p.kb[0];
+            if (lane < p.M)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        st_shared_f4(ring + (uint32_t)(row * p.pitch + c + 4 * j) * 4u,
-                                     empty ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                           : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-            }
+                for (int j = 0; j < 4; ++j)
+                    st_shared_f4(ring + (uint32_t)(lane * p.pitch + c + 4 * j) * 4u,
+                                 empty ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                       : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+        }
         tc_fence_before();
     }
     if (C > 1) cluster_sync();  // every CTA's sums are in its shared memory
