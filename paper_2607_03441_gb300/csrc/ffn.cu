@@ -203,9 +203,11 @@ struct FfnProblem {
 // either half), with the bytes that have to come from HBM as a lower bound: few rows
 // take that long however they are cut.
 static TilePlan ffn_plan(int64_t M, int64_t N, int64_t kb, bool dual, double bytes, int sms) {
-    TilePlan best{true, 256, 1};
+    TilePlan best{M > 128, 256, 1};
     double best_t = 1e30;
-    for (int pair = 1; pair >= 0; --pair) {
+    // pairs only where both CTAs have rows: for fewer an empty half is filled with zeros and multiplied (forward at
+    // 5,120 x 27,648: 9 rows 199 us, single CTAs 144; 128 rows 154, 156)
+    for (int pair = M > 128 ? 1 : 0; pair >= 0; --pair) {
         const int64_t rows = pair ? 256 : 128, units = pair ? sms / 2 : sms;
         for (int BN = 256; BN >= 64; BN -= 64) {
             if (dual ? BN % 128 != 0 : pair && BN == 64) continue;
@@ -395,7 +397,7 @@ static attt_status ffn_contract(const FfnProblem &q, int dev, cudaStream_t strea
 }
 
 // ---------------------------------------------------------------------------
-// At most 32 rows
+// Few rows
 // ---------------------------------------------------------------------------
 
 // One contraction of a call: activations a[i] [M, K] against weights b (FEW_GLU: gate and up of one
@@ -418,10 +420,11 @@ struct FewProblem {
 };
 
 // The tile's columns, the CTAs per tile and per SM.  An SM takes a stage's bytes at some 65 a ns; a CTA
-// begins and ends in some 5 us, which waves of CTAs pay one after the other, but for two CTAs
-// per SM, each with half of shared memory and of TMEM.  (Two per SM only for tiles of one CTA that
+// begins and ends in some 5 us, 15 more for every wave after the first (with 5 the estimate took waves where two
+// CTAs per SM, each with half of shared memory and of TMEM, were the faster: 1 row at 8,192 x 22,016
+// forward 185 us, 163 so).  (Two per SM only for tiles of one CTA that
 // are more than the SMs: a grid of fewer, or one that starts beside the previous one's end, is
-// packed on half of the SMs: y of 64 rows at 5,120 x 27,648 61 -> 109 us when this took as many.)
+// packed on half of the SMs: y of 64 rows at 5,120 x 27,648 61 -> 109 us.)
 struct FewPlan {
     int n_tile, cluster, stages, per_sm;
 };
@@ -448,6 +451,9 @@ static FewPlan few_plan(int mode, int M, int64_t N, int64_t kb, int nrank, int r
     const uint32_t a_alloc = (uint32_t)round_up(M, 8) * 128u;
     for (int per_sm = 1; per_sm <= 2; ++per_sm)
         for (int n_tile = 128; n_tile >= 64; n_tile /= 2) {
+            // the second launch, and two CTAs per SM, with narrow tiles: 4 rows at 4,096 x 14,336 with r = 16 forward 88 us
+            // (73 so), backward 94 (73); at 5,120 x 27,648 174 (167)
+            if ((pdl || per_sm == 2) && n_tile == 64) continue;
             const int cols = (mode == FEW_GLU ? 2 * n_tile : n_tile) + nrank * rpad;
             if (cols * per_sm > 512) continue;
             const uint32_t w = few_w_bytes(mode, n_tile, nrank, rpad), total = per_sm == 2 ? 115200u : (uint32_t)kMaxSmem,
@@ -459,13 +465,16 @@ static FewPlan few_plan(int mode, int M, int64_t N, int64_t kb, int nrank, int r
             if (per_sm == 2 && tiles <= resident_clusters(1, dev)) continue;
             for (int c = 1; c <= (per_sm == 2 ? 1 : kFewMaxCluster) && c <= kb; ++c) {
                 // clusters that start while the previous grid's CTAs leave are not packed as those of an idle
-                // device: with all places needed some ran after the others (28 clusters of 5, dx of 93
-                // rows at 3,584 x 18,944, when this took as many: 85 us, 62 with seven eighths of the places taken, 112 CTAs)
-                const int held = resident_clusters(c, dev), places = pdl && c > 1 ? std::max(1, held * 7 / 8) : held;
+                // device: with all places needed some ran after the others (28 clusters of 5, 140 CTAs, dx of 93
+                // rows at 3,584 x 18,944: 85 us, 62 with fewer)
+                const int held = resident_clusters(c, dev), places = pdl && c > 1 ? std::max(1, held * 15 / 16) : held;
                 const int64_t each = cdiv(tiles, places), waves = cdiv(each, per_sm);
+                // and clusters in waves cost more than this estimate: 32 rows at 5,120 x 27,648 with r = 16 backward
+                // 172 us (153 without), 4 rows at 5,120 x 13,824 with r = 64 forward 121 (100)
+                if (c > 1 && each > 1) continue;
                 const double run = (double)each * cdiv(kb, c) * (a_alloc + w) / 65e9, hbm = bytes / 6.7e12;
                 const double end = M * (double)(mode == FEW_GLU ? 2 : 1) * n_tile * 8 / 100e9;
-                const double t = (run > hbm ? run : hbm) + waves * (5.0e-6 + end) + (c > 1 ? 1.0e-6 : 0.0);
+                const double t = (run > hbm ? run : hbm) + waves * (15.0e-6 + end) - 10.0e-6 + (c > 1 ? 1.0e-6 : 0.0);
                 if (t < 0.98 * best_t) {
                     best_t = t;
                     best = FewPlan{n_tile, c, (int)std::min<int64_t>(stages, cdiv(kb, c)), per_sm};
@@ -568,20 +577,28 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
     return cudaGetLastError() == cudaSuccess ? ATTT_OK : ATTT_ERR_CUDA;
 }
 
-// Which calls tc_ffn_few.cuh's kernels take.  Two launches and their wider loads win where the weights
-// and the launches are all there is; the other kernels' chain of up to seven launches loads an adapter's
-// columns once instead of once per cluster and wastes less on more rows.  Times of the chain / of these kernels,
-// us, replayed from a graph, weights not in L2 (d x f, rank; forward, backward):
-//     rows     1,024 x 4,096, 16        3,584 x 18,944, 16      5,120 x 27,648, 0       2,048 x 8,192, 64
-//        1    31.1 / 25.5  27.9 / 23.8   96.7 / 79.4   99 / 81    171 / 128  151 / 134   41.5 / 42.9  42.3 / 40.4
-//        8    29.8 / 26.0  28.5 / 24.4   98.0 / 79.8  100 / 82    167 / 129  152 / 136   39.9 / 44.5  42.9 / 42.4
-//       32    27.8 / 28.8  28.7 / 27.9   98.9 / 82.9  100 / 84    144 / 132  151 / 139   40.8 / 49.8  44.2 / 47.8
-//       64    27.1 / 31.9  29.7 / 30.3  100.4 / 93.3  103 / 90    146 / 149  154 / 160   41.6 / 55.1  45.1 / 55.6
-//      128    27.9 / 38.8  31.1 / 38.0  103.7 / 105   109 / 104   153 / 184  160 / 181   43.6 / 68.3  47.2 / 75.4
-// Up to 8 rows: 7% faster over 12 such shapes each way; 16 and 32 rows: 8% where a matrix has 2^26 values or
-// more and r <= 16, 8% slower elsewhere.
-static bool ffn_few(int64_t L, int64_t d, int64_t f, int r) {
-    return L <= 8 || (L <= kFewRows && r <= 16 && d * f >= (1ll << 26));
+// Which calls tc_ffn_few.cuh's kernels take.  Two launches and wider loads win where the weights'
+// bytes and the launches are what a call costs; the chain of up to seven launches loads an
+// adapter's columns once instead of once per cluster, and its tiles waste less on more rows.
+// Times of the chain / of these kernels, us, replayed from a graph, weights not in L2 (f in tiles of 128: 148, 216, 64):
+//   rows, r      3,584 x 18,944: forward, backward    5,120 x 27,648               2,048 x 8,192
+//     8,  0       73.8 /  68.6    78.0 /  72.6     145.0 / 129.5  154.3 / 137.2    28.4 / 29.9  30.3 / 30.4
+//    32,  0       75.5 /  72.4    80.7 /  76.5     146.5 / 132.9  154.8 / 141.6    28.8 / 31.2  31.5 / 32.7
+//    64,  0       77.3 /  76.5    83.5 /  80.2     149.7 / 143.3  157.1 / 147.8    30.2 / 35.6  32.9 / 33.9
+//    96,  0       78.9 /  80.7    83.8 /  84.5     150.3 / 175.9  159.6 / 178.1    30.2 / 41.0  33.7 / 38.4
+//     8, 16       98.2 /  79.3   100.9 /  81.6     166.7 / 174.7  176.5 / 148.5    39.2 / 39.2  42.6 / 39.0
+//    32, 16      100.3 /  83.8   102.8 /  85.1     168.9 / 178.4  177.8 / 152.8    40.5 / 43.0  43.1 / 40.4
+//    64, 16      100.4 /  89.3   104.9 /  90.5     171.6 / 184.0  179.9 / 162.6    40.6 / 45.6  44.7 / 42.8
+//    96, 16      102.1 /  93.8   106.8 /  96.4     172.3 / 203.7  182.4 / 197.7    41.8 / 52.6  45.7 / 48.6
+//   128, 16      104.1 / 102.2   111.1 / 104.3     176.6 / 218.9  186.3 / 207.4    43.2 / 57.2  46.9 / 52.9
+//     8, 64       99.4 /  90.0   101.2 /  88.8     168.6 / 191.3  177.3 / 162.4    39.9 / 44.5  42.9 / 42.4
+//    32, 64      100.6 /  96.8   104.4 /  94.4     170.4 / 199.9  178.2 / 168.6    41.3 / 50.8  44.5 / 46.6
+//    64, 64      102.0 / 105.0   106.9 / 109.7     173.5 / 215.7  180.3 / 204.4    42.3 / 55.5  45.1 / 54.3
+static bool ffn_few(int64_t L, int64_t d, int64_t f, int r, bool back, int dev) {
+    if (d * f <= 1ll << 24) return L <= 8;
+    const bool fits = cdiv(f, 128) <= num_sms(dev);  // f's tiles on an SM each
+    if (back) return L <= (r > 16 ? 32 : fits ? kFewRows : 64);
+    return (fits || r == 0) && L <= (r > 16 ? 8 : 64);
 }
 
 // ---------------------------------------------------------------------------
@@ -660,7 +677,7 @@ attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, 
     st = ffn_pad_adapters(ad, 7, c, d, f, r, dev, launched, stream);
     if (st != ATTT_OK) return st;
 
-    if (ffn_few(L, d, f, r)) {
+    if (ffn_few(L, d, f, r, false, dev)) {
         FewProblem q{};
         q.a[0] = d_x; q.b[0] = d_Wg; q.b[1] = d_Wu;
         q.K = d; q.M = (int)L; q.N = (int)f;
@@ -760,7 +777,7 @@ attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg
     st = current_device(&dev);
     if (st != ATTT_OK) return st;
     const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
-    if (ffn_few(L, d, f, r)) {
+    if (ffn_few(L, d, f, r, true, dev)) {
         FewProblem q{};
         q.a[0] = d_dy; q.b[0] = d_Wd;
         q.K = d; q.M = (int)L; q.N = (int)f;

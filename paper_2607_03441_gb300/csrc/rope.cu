@@ -243,8 +243,9 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
     __shared__ float red[BACK ? kRopeThreads / 32 * kRopeMaxD : 1];
     if (BACK) griddep_launch_dependents();
     constexpr int kGroups = kRopeThreads / G;
-    // heads of a lane at a time: two where its registers hold them
-    constexpr int U = (NS > 1 && (V > 1 || NS >= 4)) || (BACK && INTER && V == 8) ? 1 : 2;
+    // heads of a lane at a time: two where its registers hold them, one backward (2,048 tokens of 32
+    // heads of 128: 17.6 us, two 19.6)
+    constexpr int U = BACK || (NS > 1 && (V > 1 || NS >= 4)) ? 1 : 2;
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
     const int half = p.half, pairs = p.D / 2;
     RopeSlot<V, INTER> slot[NS];
@@ -274,7 +275,7 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
             const RopeTensor &q = p.part[part];
             const bool norm = q.gamma != nullptr;
             const int n = nt * q.heads;
-            RopeHead<T, V, NS> next[U], next_x[BACK ? U : 1];
+            RopeHead<T, V, NS> next[U], next_x;
             auto fetch = [&](int i0) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -285,8 +286,7 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
                                                    BACK ? (t0 + t) * q.dy_ld + h * q.dy_hs : (t0 + t) * q.x_ld + h * q.x_hs,
                                                    slot, half, pairs, next[u]);
                         if (BACK && norm)
-                            rope_load<T, V, NS, INTER>(q.x, (t0 + t) * q.x_ld + h * q.x_hs, slot, half, pairs,
-                                                       next_x[BACK ? u : 0]);
+                            rope_load<T, V, NS, INTER>(q.x, (t0 + t) * q.x_ld + h * q.x_hs, slot, half, pairs, next_x);
                     }
                 }
             };
@@ -317,11 +317,11 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
             }
             // whole warps go round together (the reductions are theirs)
             for (int i0 = 0; i0 < n; i0 += U * kGroups) {
-                RopeHead<T, V, NS> head[U], head_x[BACK ? U : 1];
+                RopeHead<T, V, NS> head[U], head_x;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     head[u] = next[u];
-                    if (BACK) head_x[BACK ? u : 0] = next_x[BACK ? u : 0];
+                    if (BACK) head_x = next_x;
                 }
                 fetch(i0 + group + U * kGroups);
 #pragma unroll
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
                         if (norm) {
                             Values x[NS];
 #pragma unroll
-                            for (int s = 0; s < NS; ++s) x[s].unpack(head_x[u].a[s], head_x[u].b[s]);
+                            for (int s = 0; s < NS; ++s) x[s].unpack(head_x.a[s], head_x.b[s]);
                             float2 ss = make_float2(0.f, 0.f), sg = ss;  // sums of x^2 and of g x
 #pragma unroll
                             for (int s = 0; s < NS; ++s)

@@ -1,4 +1,4 @@
-// tc_ffn_few.cuh -- the gated feed-forward block's contractions for at most 32 rows,
+// tc_ffn_few.cuh -- the gated feed-forward block's contractions for at most 96 rows,
 // where the weights' bytes and the chain of launches are what they cost.
 //
 // A tile of columns belongs to a cluster of C CTAs (1 to 8) that share its K blocks; each
@@ -29,7 +29,7 @@ enum FewMode : int {
 };
 
 constexpr int kFewThreads = 256, kFewMaxStages = 8, kFewMaxCluster = 8;
-constexpr int kFewRows = 32;  // at most: a row's sums are one warp's lane
+constexpr int kFewRows = 96;  // at most (ffn.cu: which calls)
 constexpr int kFewStep = 4;  // fragments of a warp at a time
 
 // A rank-r product: of the activations of segment `seg`, with matrix map r[i], into accumulator
@@ -308,22 +308,25 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     }
     __syncthreads();  // (a producer that gave up has stopped before the ring is written)
     const int cols = p.BN + p.nrank * p.rpad;
-    if (warp == 0 || warp == 4) {  // the two that may read rows 0 to 31: every other run of 16 columns each
-        for (int c = 16 * (warp >> 2); c < cols; c += 32) {
-            float v[16];
-            tmem_ld_x16(tmem_base + (uint32_t)c, v);
-            // a product whose K blocks are all another CTA's has no sums here
-            bool empty = false;
-            for (int i = 0; i < p.nrank; ++i)
-                if (c >= p.rank[i].col && c < p.rank[i].col + p.rpad && p.nseg > 1)
-                    empty = p.rank[i].seg == 0 ? k0 >= p.kb[0] : k1 <= p.kb[0];
-            if (lane < p.M)
+    {   // a warp's 32 rows (those of its number modulo 4), every other run of 16 columns
+        const int q = warp & 3, row = q * 32 + lane;
+        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
+        if (q * 32 < p.M)
+            for (int c = 16 * (warp >> 2); c < cols; c += 32) {
+                float v[16];
+                tmem_ld_x16(taddr + (uint32_t)c, v);
+                // a product whose K blocks are all another CTA's has no sums here
+                bool empty = false;
+                for (int i = 0; i < p.nrank; ++i)
+                    if (c >= p.rank[i].col && c < p.rank[i].col + p.rpad && p.nseg > 1)
+                        empty = p.rank[i].seg == 0 ? k0 >= p.kb[0] : k1 <= p.kb[0];
+                if (row < p.M)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    st_shared_f4(ring + (uint32_t)(lane * p.pitch + c + 4 * j) * 4u,
-                                 empty ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                       : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-        }
+                    for (int j = 0; j < 4; ++j)
+                        st_shared_f4(ring + (uint32_t)(row * p.pitch + c + 4 * j) * 4u,
+                                     empty ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                           : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+            }
         tc_fence_before();
     }
     if (C > 1) cluster_sync();  // every CTA's sums are in its shared memory

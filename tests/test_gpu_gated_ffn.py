@@ -135,6 +135,21 @@ def test_backward(shape, act):
     assert lean[0] is None and torch.equal(lean[1], out[1]) and torch.equal(lean[2], out[2])
 
 
+WIDE = [  # more than 2^24 values of a weight: which kernels take the rows depends on L, r and f's tiles
+    (9, 4104, 4104, 16), (17, 2056, 8200, 12), (33, 8200, 2056, 8), (64, 4104, 4104, 16), (65, 4104, 4104, 0),
+    (96, 4104, 4104, 16), (97, 4104, 4104, 16), (96, 904, 18952, 15), (8, 904, 18952, 64), (32, 904, 18952, 64),
+    (33, 904, 18952, 40), (40, 904, 19592, 0), (64, 904, 19592, 16), (65, 904, 19592, 16), (5, 904, 24584, 64),
+]
+
+
+@pytest.mark.parametrize("shape", WIDE)
+def test_rows_at_wide_weights(shape):
+    c = Case(*shape)
+    check_forward(c, attt.attt_gated_ffn_forward(c.x, *c.W, **c.kw, save=True))
+    check_backward(c, attt.attt_gated_ffn_backward(c.dy, *c.W, c.g, c.u, **c.kw))
+    assert attt.attt_device_status() == 0
+
+
 @pytest.mark.parametrize("adapted", [(0,), (1,), (2,), (0, 2), (1, 2), (0, 1)])
 @pytest.mark.parametrize("r", [16, 5])
 def test_some_projections_adapted(adapted, r):
