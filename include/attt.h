@@ -662,7 +662,7 @@ ATTT_API attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf1
  * d_dx may be NULL: not wanted.  dg and du are the upstream gradients that attt_lora_grad takes
  * for the gate's and up's adapters, dy with h in the place of x for the down's.  dx is
  * formed from dg and du as rounded to bf16; the products with B^T are rounded to bf16 once.
- * Requirements as above.  Two to seven launches.
+ * Requirements as above.  One (no dx) to seven launches.
  */
 ATTT_API attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg, const attt_bf16 *d_Wu,
                                              const attt_bf16 *d_Wd, const attt_bf16 *const *d_A,

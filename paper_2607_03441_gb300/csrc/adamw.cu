@@ -16,9 +16,12 @@
 // let it fall.  The random bits are a hash of (seed, tensor, index): a step can be repeated.
 // The step itself uses the moments before they are rounded.
 //
-// Bound: HBM bytes, 30 a value (8 bits: 18 and 16 per block).  A warp takes a block of 256 values,
-// a lane two runs of four (16-byte vectors that lie side by side); largest values by one
-// reduction over the warp.
+// Bound: HBM bytes, 30 a value (8 bits: 18 and 16 per block).  A warp takes a run of blocks of 256
+// values, a lane two runs of four of each (16-byte vectors that lie side by side); largest values by
+// one reduction over the warp.  The next block's lines are asked into L2 while one is worked on.
+// Measured: 112 tensors, 5.0 M values, 32 bits 30.7 us (floor 22.4: 4.9 TB/s with a start and an
+// end of some 4 us); 512 tensors, 134 M values, in 8 bits with the moments read back as fp32 660 us (floor 533:
+// 5.4 TB/s, the hash and the codes' arithmetic beside the bytes).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
