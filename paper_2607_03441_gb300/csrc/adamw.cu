@@ -455,7 +455,9 @@ attt_status attt_adamw_create(int count, float *const *d_p, const float *const *
                 (void)cudaGetLastError();
                 return ATTT_ERR_CUDA;
             }
-            if (cudaMemcpy(h->tensors, image.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) {
+            // (the copy of pageable memory may still be on its way, and a step's stream need not wait for it)
+            if (cudaMemcpy(h->tensors, image.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess ||
+                cudaStreamSynchronize(nullptr) != cudaSuccess) {
                 (void)cudaGetLastError();
                 cudaFree(h->tensors);
                 return ATTT_ERR_CUDA;

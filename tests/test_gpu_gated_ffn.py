@@ -274,6 +274,44 @@ def test_repeats_streams_and_graphs():
     assert attt.attt_device_status() == 0
 
 
+@pytest.mark.parametrize("shape", [(3, 264, 1000, 8), (33, 4104, 4104, 16), (61, 904, 18952, 12), (90, 4104, 4104, 16)])
+def test_few_rows_apart_on_streams_and_in_graphs(shape):
+    """As above for calls of few rows: bits repeat, a NaN row stays its own, nothing behind the last
+    row is written."""
+    c = Case(*shape)
+    L, d, f, _ = shape
+    bufs = [torch.full((L + 5, n), 7.0, dtype=torch.bfloat16, device=DEV) for n in (d, f, f, f, d, f, f)]
+    outs = [b[:L] for b in bufs]
+
+    def call(x, dy, out, stream=None):
+        y, h, g, u, dx, dg, du = out or [None] * 7
+        got = attt.attt_gated_ffn_forward(x, *c.W, **c.kw, y=y, h=h, g=g, u=u, save=True, stream=stream)
+        return list(got) + list(attt.attt_gated_ffn_backward(dy, *c.W, c.g, c.u, **c.kw, dx=dx, dg=dg, du=du, stream=stream))
+
+    first = call(c.x, c.dy, None)
+    check_forward(c, first[:4])
+    check_backward(c, first[4:])
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for s in sides:
+        s.wait_stream(torch.cuda.current_stream())
+    both = [call(c.x, c.dy, None, s) for s in sides]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(c.x, c.dy, outs)
+    graph.replay()
+    graph.replay()
+    for a, b, e, k in zip(first, *both, outs):
+        assert torch.equal(a, b) and torch.equal(a, e) and torch.equal(a, k)
+    assert all((b[L:] == 7).all() for b in bufs)
+    x, dy = c.x.clone(), c.dy.clone()
+    x[1, 5] = dy[1, 5] = float("nan")
+    rows = torch.arange(L, device=DEV) != 1
+    for a, b in zip(call(x, dy, None), first):
+        assert torch.isnan(a[1]).all() and torch.equal(a[rows], b[rows])
+    assert attt.attt_device_status() == 0
+
+
 def test_refusals():
     c = Case(16, 64, 128, 8)
     fwd, bwd = attt.attt_gated_ffn_forward, attt.attt_gated_ffn_backward
