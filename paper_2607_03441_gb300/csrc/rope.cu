@@ -499,9 +499,6 @@ __global__ void __launch_bounds__(1024) rope_sum_kernel(const RopeSum a) {
     if (x == 0 && blockIdx.x * 32 + strand < a.D) a.out[q][blockIdx.x * 32 + strand] = v;
 }
 
-// ---------------------------------------------------------------------------
-
-
 template <class T, bool INTER, bool BACK>
 static const void *rope_pick(bool vec, int D) {
     constexpr int V = RopeVec<T>::n;

@@ -84,6 +84,13 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
     return v;
 }
 
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
 // d += a b for a 16 x 16 block of a (rows) and 16 x 8 of b.
 __device__ __forceinline__ void few_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -355,11 +362,23 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     };
     griddep_wait();  // what is read and overwritten from here on may be the previous grid's
     if (p.nrank > 0) {
-        const int vc = p.nrank * p.rpad / 2;
+        const int vc = p.nrank * p.rpad / 4;  // four columns at a time: with two, 1 to 4 us more of a call
         for (int i = threadIdx.x; i < p.M * vc; i += kFewThreads) {
-            const int row = i / vc, c = 2 * (i - row * vc);
-            const float2 v = sum2(row, p.BN + c);
+            const int row = i / vc, c = 4 * (i - row * vc);
+            const uint32_t at = (uint32_t)(row * p.pitch + p.BN + c) * 4u;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (C == 1) {
+                v = *reinterpret_cast<const float4 *>(smem + at);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kFewMaxCluster; ++j)
+                    if (j < C) {
+                        const float4 w = ld_cluster_f4(base[j] + at);
+                        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                    }
+            }
             few_put2(sv + row * p.vpitch + c, p.scale * v.x, p.scale * v.y);
+            few_put2(sv + row * p.vpitch + c + 2, p.scale * v.z, p.scale * v.w);
         }
         __syncthreads();
     }
