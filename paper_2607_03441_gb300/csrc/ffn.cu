@@ -14,8 +14,8 @@
 //             dg Wg^T + du Wu^T as one contraction over both K ranges.
 // Adapters add a 64-deep K block or two, after a launch that forms the rank-r products.  A few rows take two
 // launches that form them too (tc_ffn_few.cuh; which calls: ffn_few).
-// Measured, 3,584 x 18,944, r 16: 2,048 rows forward 531 us (1,571 TFLOP/s; burst rate of a library's
-// product 1,928, sustained 1,735); 8,192 rows at 5,120 x 27,648, r 64 backward 4,330 (1,608); 403
+// Measured, 3,584 x 18,944, r 16: 2,048 rows forward 531 to 545 us (1,571 TFLOP/s; burst rate of a library's
+// product 1,928, sustained 1,735); 8,192 rows at 5,120 x 27,648, r 64 backward 4,330 to 4,490 (1,608); 403
 // rows at 4,096 x 14,336, r 32 forward 140 (512 rows of tiles, the products' launches 20); 1 row
 // forward 69 (5.9 TB/s), 93 backward 97 (4.2 TB/s).
 #include <algorithm>
