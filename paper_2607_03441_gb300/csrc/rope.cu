@@ -15,9 +15,9 @@
 // Angles: w_i is held in turns per position as a 64-bit fraction; pos w_i modulo 2^64
 // is then the exact fraction of a turn whatever the position (fp32 products are off by
 // 0.06 radians at position 10^6), and a quarter turn is taken off before it goes to fp32.
-// Measured: 8,192 tokens of 40 and 8 heads of 128, bf16 with norm, forward 37 us (5.5 TB/s, 81% of the copy
+// Measured: 8,192 tokens of 40 and 8 heads of 128, bf16 with norm, forward 36 us (5.5 TB/s, 82% of the copy
 // rate: a chain of load, reduction over lanes, store per head is left); 2,048 tokens of 28 and 4,
-// backward with the norms' gradients 17.6 (floor 7.5: two launches, the table, the sums' way through
+// backward with the norms' gradients 17.0 (floor 7.5: two launches, the table, the sums' way through
 // memory are some 8 of it); 16 tokens forward 4.0.
 #include <algorithm>
 #include <cmath>
@@ -202,7 +202,6 @@ struct RopeValues {
 
 __device__ __forceinline__ float2 rope_mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 rope_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
-__device__ __forceinline__ float2 rope_neg(float2 a) { return make_float2(-a.x, -a.y); }
 
 // A lane's vectors of a head, as loaded.
 template <class T, int V, int NS>
@@ -350,7 +349,7 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
                         float sum2 = ss.x + ss.y;
 #pragma unroll
                         for (int o = G / 2; o > 0; o >>= 1) sum2 += __shfl_xor_sync(0xffffffffu, sum2, o);
-                        rstd.x = rstd.y = __frsqrt_rn(fmaf(sum2, inv_d, p.eps));
+                        rstd.x = rstd.y = rsqrtf(fmaf(sum2, inv_d, p.eps));
                     }
                     if (live) {
 #pragma unroll
@@ -370,7 +369,8 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
                                         sn = make_float2(f.z, f.w);
                                     }
                                     const float2 va = z[s].a[k], vb = z[s].b[k];
-                                    z[s].a[k] = rope_fma(va, c, rope_neg(rope_mul(vb, sn)));
+                                    // (a pair has no negation of its own; times -1 is one instruction, not two)
+                                    z[s].a[k] = rope_fma(rope_mul(vb, sn), make_float2(-1.f, -1.f), rope_mul(va, c));
                                     z[s].b[k] = rope_fma(va, sn, rope_mul(vb, c));
                                 }
                             }
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kRopeThreads, NS > 1 && NS * V >= 8 ? 1 : BACK
                                 sum2 += __shfl_xor_sync(0xffffffffu, sum2, o);
                                 sumg += __shfl_xor_sync(0xffffffffu, sumg, o);
                             }
-                            rstd.x = rstd.y = __frsqrt_rn(fmaf(sum2, inv_d, p.eps));
+                            rstd.x = rstd.y = rsqrtf(fmaf(sum2, inv_d, p.eps));
                             const float2 m = make_float2(-sumg * inv_d * rstd.x, -sumg * inv_d * rstd.x);
 #pragma unroll
                             for (int s = 0; s < NS; ++s)

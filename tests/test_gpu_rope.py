@@ -3,7 +3,8 @@
 Bounds, u = 2^-24: cosine and sine of an exact angle are off by at most 4 u (rounding of
 what is left of the angle, the function's own 2 u); turning adds two roundings: 8 u of the
 pair's two sizes.  A head's sum of squares goes through at most 16 additions in a lane and
-five between lanes: 32 u of it, 16 u of its root, and 4 u in what follows.  dgamma adds tokens
+five between lanes: 32 u of it, 16 u of its root, and 4 u in what follows (22 additions are
+11 u of the root, its function 2 ulp = 4 u, two products 2 u: 17 of these 20).  dgamma adds tokens
 and heads in at most 400 steps (a lane takes at most one of 32 groups' heads of 40,013 / 200 tokens).  Results rounded to bf16 are off by 2^-8 of themselves."""
 import numpy as np
 import pytest
