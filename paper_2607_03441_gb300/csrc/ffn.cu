@@ -587,23 +587,27 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
 // adapter's columns once instead of once per cluster, and its tiles waste less on more rows.
 // Times of the chain / of these kernels, us, replayed from a graph, weights not in L2 (f in tiles of 128: 148, 216, 64):
 //   rows, r      3,584 x 18,944: forward, backward    5,120 x 27,648               2,048 x 8,192
-//     8,  0       73.8 /  68.6    78.0 /  72.6     145.0 / 129.5  154.3 / 137.2    28.4 / 29.9  30.3 / 30.4
-//    32,  0       75.5 /  72.4    80.7 /  76.5     146.5 / 132.9  154.8 / 141.6    28.8 / 31.2  31.5 / 32.7
-//    64,  0       77.3 /  76.5    83.5 /  80.2     149.7 / 143.3  157.1 / 147.8    30.2 / 35.6  32.9 / 33.9
-//    96,  0       78.9 /  80.7    83.8 /  84.5     150.3 / 175.9  159.6 / 178.1    30.2 / 41.0  33.7 / 38.4
-//     8, 16       98.2 /  79.3   100.9 /  81.6     166.7 / 174.7  176.5 / 148.5    39.2 / 39.2  42.6 / 39.0
-//    32, 16      100.3 /  83.8   102.8 /  85.1     168.9 / 178.4  177.8 / 152.8    40.5 / 43.0  43.1 / 40.4
-//    64, 16      100.4 /  89.3   104.9 /  90.5     171.6 / 184.0  179.9 / 162.6    40.6 / 45.6  44.7 / 42.8
-//    96, 16      102.1 /  93.8   106.8 /  96.4     172.3 / 203.7  182.4 / 197.7    41.8 / 52.6  45.7 / 48.6
-//   128, 16      104.1 / 102.2   111.1 / 104.3     176.6 / 218.9  186.3 / 207.4    43.2 / 57.2  46.9 / 52.9
-//     8, 64       99.4 /  90.0   101.2 /  88.8     168.6 / 191.3  177.3 / 162.4    39.9 / 44.5  42.9 / 42.4
-//    32, 64      100.6 /  96.8   104.4 /  94.4     170.4 / 199.9  178.2 / 168.6    41.3 / 50.8  44.5 / 46.6
-//    64, 64      102.0 / 105.0   106.9 / 109.7     173.5 / 215.7  180.3 / 204.4    42.3 / 55.5  45.1 / 54.3
+//     8,  0      75.1 /  69.6   79.6 /  74.1   144.6 / 129.3  154.2 / 137.5    28.4 /  28.2   30.7 /  29.9
+//    32,  0      75.9 /  72.5   80.7 /  76.7   146.7 / 132.4  154.9 / 141.7    29.1 /  30.0   31.4 /  32.5
+//    64,  0      77.4 /  75.9   81.9 /  80.7   149.2 / 144.9  157.5 / 148.4    29.7 /  34.2   33.0 /  33.7
+//    96,  0      79.6 /  79.8   85.6 /  84.5   152.8 / 151.9  159.2 / 156.2    30.2 /  39.5   33.9 /  38.3
+//     8, 16      98.7 /  80.1  101.1 /  82.0   166.2 / 166.4  176.2 / 148.7    39.3 /  37.9   43.2 /  37.7
+//    32, 16      99.6 /  82.5  103.9 /  84.3   168.7 / 169.6  176.7 / 153.0    39.5 /  40.8   43.6 /  39.5
+//    64, 16     100.2 /  87.2  104.3 /  89.7   171.9 / 179.6  178.2 / 162.2    40.3 /  43.2   44.6 /  41.8
+//    96, 16     102.0 /  91.6  109.0 /  95.5   174.5 / 189.7  181.8 / 172.1    41.5 /  49.8   45.7 /  47.8
+//     8, 32      99.0 /  81.5  101.8 /  83.1   167.1 / 171.2  176.9 / 150.0    39.4 /  39.1   43.1 /  37.9
+//    32, 32     100.5 /  84.0  103.2 /  86.4   169.0 / 174.7  177.2 / 155.1    40.0 /  42.6   44.3 /  40.9
+//    64, 32     100.8 /  89.3  105.5 /  92.9   171.8 / 183.7  180.3 / 166.6    40.9 /  45.2   44.7 /  44.1
+//    96, 32     102.6 /  97.1  109.0 / 100.0   174.8 / 204.2  181.9 / 190.9    42.2 /  53.9   46.0 /  51.6
+//     8, 64     100.0 /  90.6  102.2 /  88.4   168.3 / 188.8  177.7 / 162.1    40.0 /  42.9   43.5 /  40.4
+//    32, 64     101.2 /  91.1  104.2 /  92.6   170.1 / 195.3  177.7 / 167.4    40.7 /  47.0   44.6 /  44.5
+//    64, 64     101.9 /  97.8  106.1 / 106.4   173.0 / 206.3  180.3 / 200.8    41.8 /  51.2   45.1 /  51.3
+//    96, 64     103.7 / 120.3  109.5 / 122.2   176.4 / 265.2  182.4 / 228.5    42.7 /  64.9   46.1 /  63.2
 static bool ffn_few(int64_t L, int64_t d, int64_t f, int r, bool back, int dev) {
     if (d * f <= 1ll << 24) return L <= 8;
     const bool fits = cdiv(f, 128) <= num_sms(dev);  // f's tiles on an SM each
-    if (back) return L <= (r > 16 ? 32 : fits ? kFewRows : 64);
-    return (fits || r == 0) && L <= (r > 16 ? 8 : 64);
+    if (back) return L <= (r > 32 ? 32 : fits ? kFewRows : 64);
+    return (fits || r == 0) && L <= (r > 32 ? 32 : 64);
 }
 
 // ---------------------------------------------------------------------------

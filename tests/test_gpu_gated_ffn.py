@@ -139,6 +139,7 @@ WIDE = [  # more than 2^24 values of a weight: which kernels take the rows depen
     (9, 4104, 4104, 16), (17, 2056, 8200, 12), (33, 8200, 2056, 8), (64, 4104, 4104, 16), (65, 4104, 4104, 0),
     (96, 4104, 4104, 16), (97, 4104, 4104, 16), (96, 904, 18952, 15), (8, 904, 18952, 64), (32, 904, 18952, 64),
     (33, 904, 18952, 40), (40, 904, 19592, 0), (64, 904, 19592, 16), (65, 904, 19592, 16), (5, 904, 24584, 64),
+    (64, 4104, 4104, 32), (96, 904, 18952, 32), (32, 4104, 4104, 48), (33, 904, 19592, 0),
 ]
 
 
