@@ -58,11 +58,11 @@ struct FfnArgs {
 // a = act(g), slope = act'(g).  Both activations are g p(z), p the logistic function:
 // z = g (SiLU), z = 2 sqrt(2 / pi) (g + 0.044715 g^3) (GELU by tanh, since (1 + tanh(y)) / 2 =
 // p(2 y)).  Past |g| = 16 the latter's p is 0 or 1 in fp32, so z and the slope's factors
-// stop there and stay finite whatever g.
+// stop there and stay finite for every number g (a NaN stays one: not by fminf and fmaxf, which drop it).
 __device__ __forceinline__ void ffn_act(int act, float g, float &a, float &slope) {
     float z = g, zp = 1.f, c = g;
     if (act == FFN_GELU_TANH) {
-        c = fminf(fmaxf(g, -16.f), 16.f);
+        c = fabsf(g) > 16.f ? copysignf(16.f, g) : g;
         const float q = c * c;
         z = 1.5957691216057308f * c * fmaf(0.044715f, q, 1.f);
         zp = 1.5957691216057308f * fmaf(3.f * 0.044715f, q, 1.f);
