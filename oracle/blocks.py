@@ -139,8 +139,9 @@ def _scale(x, mant):
     return s, np.float32(np.float32(1) / s)
 
 
-def quantise(x, mant, rnd):
-    """(codes, scales) of sizes x (fp32 [n]) with 23 - mant random bits each."""
+def quantise(x, mant, rnd, least=0):
+    """(codes, scales) of sizes x (fp32 [n]) with 23 - mant random bits each; sizes above 0 get
+    the code `least` at least."""
     codes, scales = np.zeros(len(x), np.uint8), []
     values, cut = code_values(mant), 23 - mant
     for b in range(0, len(x), BLOCK):
@@ -153,7 +154,7 @@ def quantise(x, mant, rnd):
         step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(a, 1e-300))), -14) - mant)
         units = np.floor(a / step * 2.0 ** cut) + rnd[b:b + BLOCK]
         up = np.minimum(np.floor(units / 2.0 ** cut) * step, values[-1])
-        codes[b:b + BLOCK] = np.searchsorted(values, up)
+        codes[b:b + BLOCK] = np.maximum(np.searchsorted(values, up), least * (v > 0))
     return codes, np.array(scales, np.float32)
 
 
@@ -182,5 +183,5 @@ def adamw8(p, g, m8, v8, ms, vs, lr, b1, b2, eps, wd, t, seed, tensor):
     p, m, _, r = adamw(p, g, *read_state(m8, v8, ms, vs), lr, b1, b2, eps, wd, t)
     bits = random_bits(len(p), tensor, seed)
     cm, ms = quantise(np.abs(m), 3, (bits & np.uint32(0xFFFF)).astype(np.float64) * 16)
-    cv, vs = quantise(r, 4, (bits >> np.uint32(16)).astype(np.float64) * 8)
+    cv, vs = quantise(r, 4, (bits >> np.uint32(16)).astype(np.float64) * 8, least=1)
     return p, (cm | np.where((m < 0) & (cm > 0), 128, 0)).astype(np.uint8), cv, ms, vs

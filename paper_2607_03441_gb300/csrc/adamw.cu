@@ -14,14 +14,17 @@
 // of its size: with b2 = 0.999 a step without gradient takes 1/2000 of sqrt(v), a
 // sixtieth of the distance to the next code or less, and rounding to nearest would never
 // let it fall.  The random bits are a hash of (seed, tensor, index): a step can be repeated.
+// A root above 0 is never stored as 0 but as the smallest code at least: beside values 2^18 times
+// its size it would be 0 while its m still rounds up to a code now and then, and the step would divide
+// that m by little more than sqrt(1 - b2) |g| (gradients of 1 and 2^-20 in a block: steps of 430 lr).
 // The step itself uses the moments before they are rounded.
 //
 // Bound: HBM bytes, 30 a value (8 bits: 18 and 16 per block).  A warp takes a run of blocks of 256
 // values, a lane two runs of four of each (16-byte vectors that lie side by side); largest values by
 // one reduction over the warp.  The next block's lines are asked into L2 while one is worked on.
 // Measured: 112 tensors, 5.0 M values, 32 bits 30.7 us (floor 22.4: 4.9 TB/s with a start and an
-// end of some 4 us); 512 tensors, 134 M values, in 8 bits with the moments read back as fp32 660 us (floor 533:
-// 5.4 TB/s, the hash and the codes' arithmetic beside the bytes).
+// end of some 4 us); 512 tensors, 134 M values, in 8 bits with the moments read back as fp32 662 us (floor 533:
+// 5.3 TB/s, the hash and the codes' arithmetic beside the bytes).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -225,6 +228,15 @@ __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamTensor &
                 const uint32_t sign = __float_as_uint(x) >> 24 & 0x80u;
                 wm |= (cm > 0u ? cm | sign : 0u) << (8 * e);
                 wv |= cv << (8 * e);
+            }
+            // Roots above 0 with the code 0.  (The four codes together are asked for a 0 first: a comparison per
+            // value takes a step over 512 tensors from 656 us to 668, this to 662.)
+            if ((wv - 0x01010101u) & ~wv & 0x80808080u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y = e & 1 ? rn[2 * j + e / 2].y : rn[2 * j + e / 2].x;
+                    if (y > 0.f && (wv >> (8 * e) & 0xffu) == 0u) wv |= 1u << (8 * e);
+                }
             }
             *reinterpret_cast<uint32_t *>(&m[j]) = has_m ? wm : 0u;
             *reinterpret_cast<uint32_t *>(&v[j]) = has_r ? wv : 0u;
