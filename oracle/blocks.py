@@ -13,14 +13,18 @@ import numpy as np
 # norm of the heads and position rotation
 # --------------------------------------------------------------------------
 
-def rope_frequencies(rot, base=10000.0, factor=1.0, context=0.0, low=1.0, high=32.0):
+def rope_frequencies(rot, base=10000.0, factor=1.0, context=0.0, low=1.0, high=32.0, by_index=False):
     """Radians per position of each pair."""
     w = base ** (-2.0 * np.arange(rot // 2) / rot)
     if factor == 1.0:
         return w
     if context == 0.0:
         return w / factor
-    keep = np.clip((context * w / (2 * math.pi) - low) / (high - low), 0, 1)
+    turns = context * w / (2 * math.pi)
+    keep = np.clip((turns - low) / (high - low), 0, 1)
+    if by_index:  # log(turns) falls by ln(base) / (rot / 2) from pair to pair
+        first, last = (np.log(turns[0] / n) / np.log(base) * rot / 2 for n in (high, low))
+        keep = np.interp(np.arange(rot // 2), [max(0, math.floor(first)), min(rot - 1, math.ceil(last))], [1, 0])
     return w * keep + w / factor * (1 - keep)
 
 

@@ -138,6 +138,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "attt_layer_norm_workspace_bytes": (sz, [i64, i64]),
             "attt_layer_norm_backward": (i32, [P, i64, P, i64, P, P, P, i64, i64, i32, P, i64, P, P, P, sz, P]),
             "attt_rope_frequencies": (i32, [i64, f64, f64, f64, f64, f64, P]),
+            "attt_rope_frequencies_by_index": (i32, [i64, f64, f64, f64, f64, f64, P]),
             "attt_rope_forward": (i32, [P, i32, P, P, i64, i64, i64, f32, i32, f32, i32, P]),
             "attt_rope_workspace_bytes": (sz, [i64, i64]),
             "attt_rope_backward": (i32, [P, i32, P, P, i64, i64, i64, f32, i32, f32, i32, P, sz, P]),
@@ -898,13 +899,15 @@ def attt_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Ten
 # --------------------------------------------------------------------------
 
 def attt_rope_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, context: float = 0.0, low: float = 1.0,
-                          high: float = 32.0, device=None) -> torch.Tensor:
+                          high: float = 32.0, device=None, by_index: bool = False) -> torch.Tensor:
     """Rotation frequencies (int64 [rot / 2], 2^-64 turns per position), made once: `factor`
-    and `context` scale them for longer contexts.  On `device` (None: the CPU)."""
+    and `context` scale them for longer contexts, between `high` and `low` turns linearly in the turns
+    or, `by_index`, in the pair's index (attt_rope_frequencies_by_index).  On `device` (None: the CPU)."""
     rot = int(rot)
     out = torch.empty(max(rot // 2, 0), dtype=torch.int64)
-    _check(load_library().attt_rope_frequencies(rot, float(base), float(factor), float(context), float(low),
-                                                float(high), out.data_ptr()), "attt_rope_frequencies")
+    name = "attt_rope_frequencies_by_index" if by_index else "attt_rope_frequencies"
+    _check(getattr(load_library(), name)(rot, float(base), float(factor), float(context), float(low), float(high),
+                                         out.data_ptr()), name)
     return out if device is None else out.to(device)
 
 

@@ -636,25 +636,50 @@ static attt_status rope_run(const attt_rope_part *parts, int nparts, const int32
 
 }  // namespace attt
 
-extern "C" {
+namespace attt {
 
-attt_status attt_rope_frequencies(int64_t rot, double base, double factor, double context, double low, double high,
-                                  uint64_t *host_freq) {
-    if (rot < 2 || rot % 2 != 0 || rot > attt::kRopeMaxD || !host_freq) return ATTT_ERR_INVALID_ARG;
+// The table of attt_rope_frequencies, or of attt_rope_frequencies_by_index.
+static attt_status rope_table(int64_t rot, double base, double factor, double context, double low, double high,
+                              bool by_index, uint64_t *host_freq) {
+    if (rot < 2 || rot % 2 != 0 || rot > kRopeMaxD || !host_freq) return ATTT_ERR_INVALID_ARG;
     if (!(base >= 1.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor) || !(context >= 0.0) ||
         !std::isfinite(context))
         return ATTT_ERR_INVALID_ARG;
     if (context > 0.0 && !(low >= 0.0 && high > low && std::isfinite(high))) return ATTT_ERR_INVALID_ARG;
     const double two_pi = 6.283185307179586476925;
+    double i0 = 0.0, i1 = 0.0;  // by_index: w_i is kept up to i0, divided from i1 on
+    if (by_index) {
+        if (!(context > 0.0 && low > 0.0 && base > 1.0)) return ATTT_ERR_INVALID_ARG;
+        // the (fractional) pair that turns n times over the context
+        auto pair = [&](double n) { return (double)rot * std::log(context / (two_pi * n)) / (2.0 * std::log(base)); };
+        i0 = std::max(0.0, std::floor(pair(high)));
+        i1 = std::min((double)(rot - 1), std::ceil(pair(low)));
+        if (!(i1 > i0)) return ATTT_ERR_INVALID_ARG;
+    }
     for (int64_t i = 0; i < rot / 2; ++i) {
         const double w = std::pow(base, -2.0 * (double)i / (double)rot);
         double keep = 0.0;  // the share of w that the stretched context leaves as it was
-        if (context > 0.0) keep = std::min(1.0, std::max(0.0, (context * w / two_pi - low) / (high - low)));
+        if (by_index) keep = std::min(1.0, std::max(0.0, (i1 - (double)i) / (i1 - i0)));
+        else if (context > 0.0) keep = std::min(1.0, std::max(0.0, (context * w / two_pi - low) / (high - low)));
         if (factor == 1.0) keep = 1.0;
         const double turns = (w * keep + w / factor * (1.0 - keep)) / two_pi;  // below 0.16
         host_freq[i] = (uint64_t)std::llround(turns * 9223372036854775808.0) * 2;
     }
     return ATTT_OK;
+}
+
+}  // namespace attt
+
+extern "C" {
+
+attt_status attt_rope_frequencies(int64_t rot, double base, double factor, double context, double low, double high,
+                                  uint64_t *host_freq) {
+    return attt::rope_table(rot, base, factor, context, low, high, false, host_freq);
+}
+
+attt_status attt_rope_frequencies_by_index(int64_t rot, double base, double factor, double context, double low,
+                                           double high, uint64_t *host_freq) {
+    return attt::rope_table(rot, base, factor, context, low, high, true, host_freq);
 }
 
 attt_status attt_rope_forward(const attt_rope_part *parts, int nparts, const int32_t *d_pos, const uint64_t *d_freq,
