@@ -663,7 +663,8 @@ ATTT_API size_t attt_gated_ffn_workspace_bytes(int64_t L, int64_t d, int64_t f, 
  * s (h A_2) are rounded to bf16 once, as h is for y; products are bf16, sums fp32.
  * Requirements: L >= 0 (0 launches nothing), d, f >= 8 and multiples of 8, 0 <= r <= 64,
  * tensor pointers 16-byte aligned, d_ws at least attt_gated_ffn_workspace_bytes(L, d, f, r)
- * bytes and 256-byte aligned.  Two to seven launches.
+ * bytes and 256-byte aligned, results and workspace without a byte in common with each other or
+ * with what the call reads, but for y, which may lie in x.  Two to seven launches.
  */
 ATTT_API attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, const attt_bf16 *d_Wu,
                                             const attt_bf16 *d_Wd, const attt_bf16 *const *d_A,
@@ -680,7 +681,8 @@ ATTT_API attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf1
  * d_dx may be NULL: not wanted.  dg and du are the upstream gradients that attt_lora_grad takes
  * for the gate's and up's adapters, dy with h in the place of x for the down's.  dx is
  * formed from dg and du as rounded to bf16; the products with B^T are rounded to bf16 once.
- * Requirements as above.  One (no dx) to seven launches.
+ * Requirements as above, but dx may lie in dy, g or u, dg may be g itself and du u.  One (no
+ * dx) to seven launches.
  */
 ATTT_API attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg, const attt_bf16 *d_Wu,
                                              const attt_bf16 *d_Wd, const attt_bf16 *const *d_A,

@@ -134,6 +134,15 @@ template <class... T>
 bool aligned_to(size_t bytes, const T *...p) {
     return ((reinterpret_cast<uintptr_t>(p) % bytes == 0) && ...);
 }
+// n bytes from `at` on (NULL: none), and whether two of them share one.
+struct ByteRange {
+    const void *at;
+    int64_t n;
+};
+inline bool share_a_byte(const ByteRange &a, const ByteRange &b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.at && b.at && a.n > 0 && b.n > 0 && x < y + (uintptr_t)b.n && y < x + (uintptr_t)a.n;
+}
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
 

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(256) ffn_pad_kernel(const FfnPad a) {
 struct FfnReduce {
     const float *part;
     int M, N, BN, n_tile, pieces, rows, tiles_m, act;
-    const __nv_bfloat16 *gate, *up;     // backward: the factors
+    const __nv_bfloat16 *gate, *up;     // backward: the factors (out0 and out1 may be they)
     __nv_bfloat16 *out0, *out1, *out2;  // forward: h, g, u (g and u or neither); backward: dg, du
 };
 
@@ -111,7 +111,7 @@ __device__ __forceinline__ void ffn_put4(__nv_bfloat16 *p, const float (&v)[4]) 
 }
 
 __device__ __forceinline__ void ffn_get4(const __nv_bfloat16 *p, float (&v)[4]) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p));
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
     const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.x));
     const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&u.y));
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
@@ -631,6 +631,33 @@ static bool ffn_adapters(const attt_bf16 *const *d_A, const attt_bf16 *const *d_
     return true;
 }
 
+// What a call reads of the weights and adapters.
+static void ffn_reads(const void *Wg, const void *Wu, const void *Wd, const FfnAdapters &ad, int64_t d, int64_t f, int r,
+                      ByteRange (&in)[9]) {
+    int n = 0;
+    for (const void *w : {Wg, Wu, Wd}) in[n++] = ByteRange{w, 2 * d * f};
+    for (int i = 0; i < 3; ++i) {
+        in[n++] = ByteRange{ad.A[i], 2 * (i < 2 ? d : f) * r};
+        in[n++] = ByteRange{ad.B[i], 2 * r * (i < 2 ? f : d)};
+    }
+}
+
+// Whether a call's results share no byte with each other or with what it reads: out[0] is the
+// last launch's, when `before` is read no more; out[j] may be same[j] itself.
+template <int NO, int NB>
+static bool ffn_apart(const ByteRange (&out)[NO], const void *const (&same)[NO], const ByteRange (&in)[9],
+                      const ByteRange (&before)[NB]) {
+    for (int j = 0; j < NO; ++j) {
+        for (int k = 0; k < j; ++k)
+            if (share_a_byte(out[j], out[k])) return false;
+        for (const ByteRange &b : in)
+            if (share_a_byte(out[j], b)) return false;
+        for (const ByteRange &b : before)
+            if (j > 0 && share_a_byte(out[j], b) && !(same[j] && same[j] == b.at && out[j].at == b.at)) return false;
+    }
+    return true;
+}
+
 // Copies of the adapters' A whose rows TMA cannot read; `mask`: of which projections.
 // `launched`: whether that took a launch.
 static attt_status ffn_pad_adapters(FfnAdapters &ad, int mask, const FfnLayout &c, int64_t d, int64_t f, int r, int dev,
@@ -678,10 +705,19 @@ attt_status attt_gated_ffn_forward(const attt_bf16 *d_x, const attt_bf16 *d_Wg, 
     if (!aligned_to(16, d_x, d_Wg, d_Wu, d_Wd, d_y, d_h, d_g, d_u)) return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_gated_ffn_workspace_bytes(L, d, f, r)) return ATTT_ERR_WORKSPACE;
     if (L == 0) return ATTT_OK;
+    const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
+    {
+        ByteRange in[9];
+        ffn_reads(d_Wg, d_Wu, d_Wd, ad, d, f, r, in);
+        const ByteRange out[5] = {{d_y, 2 * L * d}, {d_h, 2 * L * f}, {d_g, 2 * L * f}, {d_u, 2 * L * f},
+                                  {d_ws, (int64_t)c.bytes}};
+        const ByteRange before[1] = {{d_x, 2 * L * d}};
+        const void *const same[5] = {};
+        if (!ffn_apart(out, same, in, before)) return ATTT_ERR_INVALID_ARG;
+    }
     int dev;
     st = current_device(&dev);
     if (st != ATTT_OK) return st;
-    const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
     bool launched = false;  // whether this call has launched a kernel that the next one may depend on
     st = ffn_pad_adapters(ad, 7, c, d, f, r, dev, launched, stream);
     if (st != ATTT_OK) return st;
@@ -782,10 +818,18 @@ attt_status attt_gated_ffn_backward(const attt_bf16 *d_dy, const attt_bf16 *d_Wg
     if (!aligned_to(16, d_dy, d_Wg, d_Wu, d_Wd, d_g, d_u, d_dx, d_dg, d_du)) return ATTT_ERR_INVALID_ARG;
     if (!d_ws || !aligned256(d_ws) || ws_bytes < attt_gated_ffn_workspace_bytes(L, d, f, r)) return ATTT_ERR_WORKSPACE;
     if (L == 0) return ATTT_OK;
+    const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
+    {
+        ByteRange in[9];
+        ffn_reads(d_Wg, d_Wu, d_Wd, ad, d, f, r, in);
+        const ByteRange out[4] = {{d_dx, 2 * L * d}, {d_dg, 2 * L * f}, {d_du, 2 * L * f}, {d_ws, (int64_t)c.bytes}};
+        const ByteRange before[3] = {{d_dy, 2 * L * d}, {d_g, 2 * L * f}, {d_u, 2 * L * f}};
+        const void *const same[4] = {nullptr, d_g, d_u, nullptr};
+        if (!ffn_apart(out, same, in, before)) return ATTT_ERR_INVALID_ARG;
+    }
     int dev;
     st = current_device(&dev);
     if (st != ATTT_OK) return st;
-    const FfnLayout c = ffn_layout(d_ws, L, d, f, r);
     if (ffn_few(L, d, f, r, true, dev)) {
         FewProblem q{};
         q.a[0] = d_dy; q.b[0] = d_Wd;

@@ -52,7 +52,9 @@ struct FfnArgs {
     FfnSeg seg[kFfnSegs];
     int act;
     int keep;  // FFN_GLU: g and u are stored too (maps c[1], c[2])
-    const __nv_bfloat16 *gate, *up;  // FFN_GLU_GRAD: the factors, [M, N]
+    // FFN_GLU_GRAD: the factors, [M, N].  dg and du may be written to where they lie (a warp has its 32 x 32 values
+    // before it stores over them), so that they are not read as what no one writes (__ldg).
+    const __nv_bfloat16 *gate, *up;
 };
 
 // a = act(g), slope = act'(g).  Both activations are g p(z), p the logistic function:
@@ -86,7 +88,7 @@ struct FfnRow {
     __device__ __forceinline__ void load(const __nv_bfloat16 *row, int x, int n) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            q[i] = row && x + 8 * i < n ? __ldg(reinterpret_cast<const uint4 *>(row + x + 8 * i)) : make_uint4(0, 0, 0, 0);
+            q[i] = row && x + 8 * i < n ? *reinterpret_cast<const uint4 *>(row + x + 8 * i) : make_uint4(0, 0, 0, 0);
     }
     __device__ __forceinline__ float2 pair(int i) const {  // values 2 i, 2 i + 1
         const uint4 &u = q[i >> 2];

@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 for (int e = 0; e < 2; ++e) {
                     gv[j][e] = uv[j][e] = 0u;
                     if (there(j, e)) {
-                        gv[j][e] = __ldg(reinterpret_cast<const uint32_t *>(p.gate + at(j, e)));
-                        uv[j][e] = __ldg(reinterpret_cast<const uint32_t *>(p.up + at(j, e)));
+                        gv[j][e] = *reinterpret_cast<const uint32_t *>(p.gate + at(j, e));  // (not __ldg: tc_ffn.cuh)
+                        uv[j][e] = *reinterpret_cast<const uint32_t *>(p.up + at(j, e));
                     }
                 }
         }
