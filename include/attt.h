@@ -610,7 +610,8 @@ typedef struct attt_rope_part {
  * pair i being values i and i + rot / 2, or 2 i and 2 i + 1 (interleaved != 0); the other
  * D - rot values stay z's.  d_pos int32 [T] (any values), d_freq uint64 [rot / 2]
  * (attt_rope_frequencies).  fp32 arithmetic, angles exact to 2^-64 of a turn per position,
- * one rounding at the end.  y may be x itself, with the same strides.  Requirements:
+ * one rounding at the end.  y may be x itself, with the same strides; apart from that the results share no
+ * byte with each other or with the heads that are read (ATTT_ERR_INVALID_ARG).  Requirements:
  * 1 <= nparts <= 2, T >= 0 (0 launches nothing), D even, 2 <= D <= 512, rot even,
  * 0 <= rot <= D (0: the norm alone), 1 <= heads <= 65,536, eps >= 0, mscale finite,
  * strides >= 0, results' heads apart from each other, pointers aligned to their type.
@@ -630,7 +631,8 @@ ATTT_API size_t attt_rope_workspace_bytes(int64_t T, int64_t D);
  *   dx = (dz gamma - xh mean(dz gamma xh)) / sqrt(mean(x^2) + eps)    (`dtype`; no norm: dz)
  *   dgamma = sum over tokens and heads of dz xh                        (fp32, in a fixed order;
  *                                                                       zeros for T = 0)
- * d_y may be d_dy or d_x itself, with the same strides.  d_ws, at least
+ * d_y may be d_dy or d_x itself, with the same strides, and the two parts' dgamma are apart (a weight that both
+ * share has the sum of the two as its gradient).  d_ws, at least
  * attt_rope_workspace_bytes(T, D) bytes and 256-byte aligned, may be NULL where no dgamma is
  * wanted.  One launch, or two with a dgamma.
  */

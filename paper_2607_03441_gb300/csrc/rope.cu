@@ -529,6 +529,94 @@ static bool rope_apart(int64_t T, int64_t heads, int64_t D, int64_t ld, int64_t 
     return (hs >= D && ld >= (heads - 1) * hs + D) || (ld >= D && hs >= (T - 1) * ld + D);
 }
 
+// The bytes of a tensor's heads: `outer` runs `pitch` bytes apart, of `inner` rows `step` apart, from `at` on.
+// Runs and rows follow one another without sharing bytes; heads that do share some (operands with
+// strides of 0 or below D) are taken as one row from the first to the last byte.
+struct RopeBytes {
+    int64_t at, outer, pitch, inner, step, row;
+    int64_t run() const { return (inner - 1) * step + row; }
+    int64_t end() const { return at + (outer - 1) * pitch + run(); }
+};
+
+static RopeBytes rope_bytes(const void *p, int64_t T, int64_t heads, int64_t D, int64_t ld, int64_t hs, int64_t es) {
+    const int64_t row = D * es, at = (int64_t)reinterpret_cast<uintptr_t>(p);
+    if (T == 1 || ld == 0) T = 1, ld = 0;
+    if (heads == 1 || hs == 0) heads = 1, hs = 0;
+    ld *= es; hs *= es;
+    if ((heads == 1 || hs >= row) && (T == 1 || ld >= (heads - 1) * hs + row)) return {at, T, ld, heads, hs, row};
+    if (ld >= row && hs >= (T - 1) * ld + row) return {at, heads, hs, T, ld, row};
+    return {at, 1, 0, 1, 0, (T - 1) * ld + (heads - 1) * hs + row};
+}
+
+// The two whole numbers c for which off - c pitch lies within a pitch of 0: the first of them.
+static int64_t rope_floor(int64_t off, int64_t pitch) {
+    return off >= 0 ? off / pitch : -((-off + pitch - 1) / pitch);
+}
+
+// Whether rows of a run of a and of one of b share a byte where b's begins `off` bytes behind a's.
+static bool rope_runs_meet(const RopeBytes &a, const RopeBytes &b, int64_t off) {
+    if (off >= a.run() || off + b.run() <= 0) return false;
+    if (a.inner > 1 && b.inner > 1 && a.step == b.step) {  // row j of b by a's rows j + c, for every j
+        const int64_t k = rope_floor(off, a.step);
+        for (int64_t c = k; c <= k + 1; ++c)
+            if (c < a.inner && c > -b.inner && off - c * a.step < a.row && off - c * a.step + b.row > 0) return true;
+        return false;
+    }
+    for (int64_t j = 0; j < b.inner; ++j) {
+        const int64_t x = off + j * b.step;  // b's row j; a's first row that ends behind its begin
+        if (x + b.row <= 0 || x >= a.run()) continue;
+        const int64_t i = x < a.row ? 0 : (x - a.row) / std::max<int64_t>(a.step, 1) + 1;
+        if (i < a.inner && i * a.step < x + b.row) return true;
+    }
+    return false;
+}
+
+static bool rope_meet(const RopeBytes &a, const RopeBytes &b) {
+    if (a.end() <= b.at || b.end() <= a.at) return false;
+    // Runs of one pitch (q and k in the rows of one projection): run j of b by a's runs j + c, for every j.
+    if (a.outer > 1 && b.outer > 1 && a.pitch == b.pitch) {
+        const int64_t diff = b.at - a.at, k = rope_floor(diff, a.pitch);
+        for (int64_t c = k; c <= k + 1; ++c)
+            if (c < a.outer && c > -b.outer && rope_runs_meet(a, b, diff - c * a.pitch)) return true;
+        return false;
+    }
+    const int64_t pitch = std::max<int64_t>(a.pitch, 1);
+    for (int64_t j = 0; j < b.outer; ++j) {
+        const int64_t x = b.at + j * b.pitch - a.at;
+        if (x + b.run() <= 0) continue;
+        for (int64_t i = x < a.run() ? 0 : (x - a.run()) / pitch + 1; i < a.outer && i * a.pitch < x + b.run(); ++i)
+            if (rope_runs_meet(a, b, x - i * a.pitch)) return true;
+    }
+    return false;
+}
+
+// Whether no result shares a byte with the other one, or with an operand that is not the same
+// heads: blocks and warps read and write at times of their own.
+static bool rope_results_apart(const attt_rope_part *parts, int nparts, int64_t T, int64_t D, size_t es, bool back) {
+    RopeBytes y[kRopeParts], in[kRopeParts][2];
+    bool has[kRopeParts][2];
+    for (int i = 0; i < nparts; ++i) {
+        const attt_rope_part &q = parts[i];
+        y[i] = rope_bytes(q.d_y, T, q.heads, D, q.y_ld, q.y_hs, es);
+        has[i][0] = !back || q.d_gamma;
+        has[i][1] = back;
+        in[i][0] = rope_bytes(q.d_x, T, q.heads, D, q.x_ld, q.x_hs, es);
+        in[i][1] = rope_bytes(q.d_dy, T, q.heads, D, q.dy_ld, q.dy_hs, es);
+    }
+    for (int i = 0; i < nparts; ++i) {
+        for (int j = 0; j < nparts; ++j)
+            for (int k = 0; k < 2; ++k) {
+                if (!has[j][k]) continue;
+                const RopeBytes &a = y[i], &b = in[j][k];
+                const bool same = i == j && a.at == b.at && a.outer == b.outer && a.inner == b.inner &&
+                                  a.pitch == b.pitch && a.step == b.step;
+                if (!same && rope_meet(a, b)) return false;
+            }
+        if (i > 0 && rope_meet(y[0], y[i])) return false;
+    }
+    return !(nparts == 2 && share_a_byte({parts[0].d_dgamma, 4 * D}, {parts[1].d_dgamma, 4 * D}));
+}
+
 static attt_status rope_check(const attt_rope_part *parts, int nparts, const int32_t *d_pos, const uint64_t *d_freq,
                               int64_t T, int64_t D, int64_t rot, float eps, float mscale, int dtype, bool back) {
     if (!parts || nparts < 1 || nparts > kRopeParts || T < 0 || D < 2 || D % 2 != 0 || rot < 0 || rot > D ||
@@ -550,9 +638,11 @@ static attt_status rope_check(const attt_rope_part *parts, int nparts, const int
         for (int64_t v : {q.x_ld, q.x_hs, q.y_ld, q.y_hs, q.dy_ld, q.dy_hs})
             if (v < 0) return ATTT_ERR_INVALID_ARG;
             else if (v > most) return ATTT_ERR_UNSUPPORTED;
+        for (int64_t ld : {q.x_ld, q.y_ld, q.dy_ld})  // farther than addresses reach
+            if ((double)ld * (double)T > 0x1p48) return ATTT_ERR_UNSUPPORTED;
         if (!rope_apart(T, q.heads, D, q.y_ld, q.y_hs)) return ATTT_ERR_INVALID_ARG;
     }
-    return ATTT_OK;
+    return T == 0 || rope_results_apart(parts, nparts, T, D, es, back) ? ATTT_OK : ATTT_ERR_INVALID_ARG;
 }
 
 static attt_status rope_run(const attt_rope_part *parts, int nparts, const int32_t *d_pos, const uint64_t *d_freq,
