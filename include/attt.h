@@ -432,7 +432,8 @@ ATTT_API int64_t attt_adamw_state_values(const attt_adamw *h);
 /*
  * The moments as fp32 values (for a checkpoint, or to go on in 32 bits): tensor k's from value
  * ATTT_ADAMW_BLOCK (sum of ceil(n[j] / ATTT_ADAMW_BLOCK), j < k) on, zeros behind its last.  Either
- * array may be NULL, not both; 16-byte aligned.
+ * array may be NULL, not both; 16-byte aligned, apart from each other (ATTT_ERR_INVALID_ARG) and from the
+ * handle's tensors.
  */
 ATTT_API attt_status attt_adamw_read_state(const attt_adamw *h, float *d_m32, float *d_v32, attt_stream stream);
 

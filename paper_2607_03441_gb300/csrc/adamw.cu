@@ -531,6 +531,8 @@ attt_status attt_adamw_read_state(const attt_adamw *h, float *d_m32, float *d_v3
     ATTT_NVTX_RANGE();
     using namespace attt;
     if (!h || (!d_m32 && !d_v32) || !aligned_to(16, d_m32, d_v32)) return ATTT_ERR_INVALID_ARG;
+    const int64_t bytes = h->blocks * kAdamBlock * (int64_t)sizeof(float);
+    if (share_a_byte({d_m32, bytes}, {d_v32, bytes})) return ATTT_ERR_INVALID_ARG;
     const attt_status st = adam_device(h);
     if (st != ATTT_OK) return st;
     if (h->blocks == 0) return ATTT_OK;
