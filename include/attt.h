@@ -394,7 +394,8 @@ typedef struct attt_adamw attt_adamw;
  *     bits 0 to 6 with k = 3 and its sign in bit 7; sqrt(v) in 8 bits with k = 4.
  * Requirements: count >= 1, n[k] >= 0, pointers aligned to their type, and no two of the
  * arrays that a step writes sharing a byte, nor a gradient lying in one of them
- * (ATTT_ERR_INVALID_ARG).  Allocates and copies a table (not during a stream capture).
+ * (ATTT_ERR_INVALID_ARG).  Allocates and copies a table (not during a stream capture): some 0.2 ms and
+ * more for many tensors, once for tensors and gradients that stay where they are.
  * *out is set on success.
  */
 ATTT_API attt_status attt_adamw_create(int count, float *const *d_p, const float *const *d_g, void *const *d_m,
@@ -610,9 +611,10 @@ typedef struct attt_rope_part {
  *       (a, b) -> mscale (a cos - b sin, a sin + b cos)
  * pair i being values i and i + rot / 2, or 2 i and 2 i + 1 (interleaved != 0); the other
  * D - rot values stay z's.  d_pos int32 [T] (any values), d_freq uint64 [rot / 2]
- * (attt_rope_frequencies).  fp32 arithmetic, angles exact to 2^-64 of a turn per position,
- * one rounding at the end.  y may be x itself, with the same strides; apart from that the results share no
- * byte with each other or with the heads that are read (ATTT_ERR_INVALID_ARG).  Requirements:
+ * (attt_rope_frequencies: formed in fp64, to some 2^-50 of each).  fp32 arithmetic; an angle is the table's
+ * frequency times the position without rounding, modulo a turn; one rounding at the end.
+ * y may be x itself, with the same strides; apart from that the results share no byte with each
+ * other or with the heads that are read (ATTT_ERR_INVALID_ARG).  Requirements:
  * 1 <= nparts <= 2, T >= 0 (0 launches nothing), D even, 2 <= D <= 512, rot even,
  * 0 <= rot <= D (0: the norm alone), 1 <= heads <= 65,536, eps >= 0, mscale finite,
  * strides >= 0, results' heads apart from each other, pointers aligned to their type.
@@ -661,7 +663,8 @@ ATTT_API size_t attt_gated_ffn_workspace_bytes(int64_t L, int64_t d, int64_t f, 
  *   h = act(g) u                    (bf16 [L, f] into d_h, wanted by the adapters' gradients)
  *   y = h Wd + s (h A_2) B_2        (bf16 [L, d] into d_y)
  * d_g and d_u (bf16 [L, f], both or neither) receive g and u for the backward call; h is
- * formed from them in fp32.  d_A and d_B are HOST arrays of three device pointers, NULL both
+ * formed from them in fp32.  (Where a row's s (x A_0) or s (x A_1) has a NaN or an infinity, g and u of that
+ * row may both be NaN: they share a contraction.)  d_A and d_B are HOST arrays of three device pointers, NULL both
  * (and r = 0) for no adapters; a projection without one has NULL in both.  s (x A) and
  * s (h A_2) are rounded to bf16 once, as h is for y; products are bf16, sums fp32.
  * Requirements: L >= 0 (0 launches nothing), d, f >= 8 and multiples of 8, 0 <= r <= 64,

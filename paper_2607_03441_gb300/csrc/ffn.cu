@@ -15,7 +15,7 @@
 // Adapters add a 64-deep K block or two, after a launch that forms the rank-r products.  A few rows take two
 // launches that form them too (tc_ffn_few.cuh; which calls: ffn_few).
 // Measured, 3,584 x 18,944, r 16: 2,048 rows forward 531 to 545 us (1,571 TFLOP/s; burst rate of a library's
-// product 1,928, sustained 1,735); 8,192 rows at 5,120 x 27,648, r 64 backward 4,330 to 4,490 (1,608); 403
+// product 1,928, sustained 1,735); 8,192 rows at 5,120 x 27,648, r 64 backward 4,330 to 4,580 (1,540 to 1,630); 403
 // rows at 4,096 x 14,336, r 32 forward 140 (512 rows of tiles, the products' launches 20); 1 row
 // forward 69 (5.9 TB/s), 93 backward 97 (4.2 TB/s).
 #include <algorithm>
@@ -603,6 +603,11 @@ static attt_status few_contract(const FewProblem &q, int dev, cudaStream_t strea
 //    32, 64     101.2 /  91.1  104.2 /  92.6   170.1 / 195.3  177.7 / 167.4    40.7 /  47.0   44.6 /  44.5
 //    64, 64     101.9 /  97.8  106.1 / 106.4   173.0 / 206.3  180.3 / 200.8    41.8 /  51.2   45.1 /  51.3
 //    96, 64     103.7 / 120.3  109.5 / 122.2   176.4 / 265.2  182.4 / 228.5    42.7 /  64.9   46.1 /  63.2
+// The limits go by d f, r, direction and whether f's tiles fit the SMs, not cell by cell, and an adapted forward call
+// whose tiles do not fit takes the chain at any number of rows (166 to 173 us against 166 to 206 at 5,120 x 27,648).  Where the table's
+// rows take the slower side by more than 2%: forward 3,584 x 18,944, 96 rows, r 16 (11%) and 32 (6%), 64 rows, r 64 (4%);
+// 2,048 x 8,192, 8 rows, r 64 (7%); backward 2,048 x 8,192, 32 and 64 rows, r 16 (10%, 7%), 32 rows, r 32 (8%);
+// 5,120 x 27,648, 96 rows, r 16 (6%).
 static bool ffn_few(int64_t L, int64_t d, int64_t f, int r, bool back, int dev) {
     if (d * f <= 1ll << 24) return L <= 8;
     const bool fits = cdiv(f, 128) <= num_sms(dev);  // f's tiles on an SM each

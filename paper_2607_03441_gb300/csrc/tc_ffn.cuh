@@ -18,8 +18,8 @@
 //     if wanted both factors;
 //   * FFN_GLU_GRAD: from the product's gradient (the accumulator) and the two
 //     factors, those of the factors.
-// Bound: tensor cores.  1,024 rows at 3,584 x 18,944: FFN_GLU 152 us (tensor pipe 91% busy), FFN_OUT over both
-// K ranges 149 (94%), FFN_GLU_GRAD 93 (74%: per tile 2 bytes of each factor in and of each gradient out
+// Bound: tensor cores.  1,024 rows at 3,584 x 18,944: FFN_GLU 152 to 156 us (tensor pipe 91% busy), FFN_OUT over both
+// K ranges 149 to 153 (94%), FFN_GLU_GRAD 93 (74%: per tile 2 bytes of each factor in and of each gradient out
 // for 2 d operations; with a second set of epilogue warps the same).
 #pragma once
 

@@ -15,8 +15,8 @@
 // grid; warp 6 loads activations once that grid has ended: the second of a call's two
 // launches streams weights while the first one ends.  Warps 2 to 5 bring the second matrices'
 // share of the tile into shared memory meanwhile.
-// Bound: HBM bytes.  1 row at 3,584 x 18,944: FEW_GLU 46.8 us (271.7 MB: 5.8 TB/s), FEW_DOWN 28.7 (135.9 MB: 4.7; the
-// two overlap, 69 together); 93 rows with r = 16: FEW_GRAD 38.7, FEW_DX 62.2.  What is left is each
+// Bound: HBM bytes.  1 row at 3,584 x 18,944: FEW_GLU 46.6 us (271.7 MB: 5.8 TB/s), FEW_DOWN 27.9 (135.9 MB: 4.9; the
+// two overlap, 69 together); 93 rows with r = 16: FEW_GRAD 38.7, FEW_DX 60.6.  What is left is each
 // launch's begin and end, some 5 us, and the sums' way through distributed shared memory.
 #pragma once
 
